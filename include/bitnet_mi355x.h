@@ -249,6 +249,153 @@ bitnet_status bitnet_mpgemm_fused(int layout, int n_linears, const void* const* 
 bitnet_status bitnet_elut_tables(const int8_t* xq, int64_t M, int64_t K, int16_t* lut, int16_t* lut1,
                                  void* stream);
 
+/*
+ * The paged key-value cache and the attention that reads it: what stands between the q/k/v products of a layer and its o
+ * product.  The fp32 outputs of bitnet_mpgemm_fused ([tokens, heads * head_dim]) are q, k and v as they are, and out is
+ * the fp32 activation that the o product reads.
+ *
+ * bitnet_kv_cache describes one layer's cache.  A page holds page_size consecutive tokens of every kv head:
+ *   k     [n_pages, n_kv_heads, C, page_size, 8], C = ceil(head_dim / 8): chunk c of a token is its channels 8c .. 8c+7
+ *         (zeros past head_dim);
+ *   v     [n_pages, n_kv_heads, page_size / 8, head_dim, 8]: a channel of eight consecutive tokens side by side.
+ *   table device int32 [n_seqs, max_pages]: the page that holds tokens t page_size .. of sequence s at [s, t].  An entry
+ *         outside [0, n_pages) (-1 by convention) stands for tokens that are not there: no call reads or writes them.
+ *   kv_len device int32 [n_seqs]: tokens of the sequence in the cache.
+ *   dtype BITNET_DTYPE_BF16 or BITNET_DTYPE_F16.  page_size 16, 32, 64, 128 or 256; head_dim a multiple of 4 up to 256;
+ *         max_pages * page_size <= 2^24; n_pages < 2^30, n_seqs <= 2^20, n_kv_heads <= 1024.  k and v may pass 4 GiB.
+ * Offsets and lengths on the device are checked there: what would fall outside the tables or tensors is left out.
+ */
+typedef enum {
+    BITNET_DTYPE_F32 = 0,
+    BITNET_DTYPE_BF16 = 1,
+    BITNET_DTYPE_F16 = 2
+} bitnet_dtype;
+
+typedef struct {
+    void* k;
+    void* v;
+    const int32_t* table;
+    const int32_t* kv_len;
+    int64_t n_pages, n_seqs, max_pages;
+    int32_t page_size, n_kv_heads, head_dim, dtype;
+} bitnet_kv_cache;
+
+/* Bytes of one page's keys (values == 0) or values (values != 0); 0 if the sizes or the type are unsupported. */
+size_t bitnet_kv_page_bytes(int dtype, int64_t page_size, int64_t n_kv_heads, int64_t head_dim, int values);
+
+/*
+ * bitnet_kv_append -- keys and values of new tokens written into their pages, rounded to the cache's type (nearest even).
+ *   k, v      device [n_tokens, n_kv_heads, head_dim] of src_dtype (BITNET_DTYPE_F32 or the cache's).
+ *   q_start   device int32 [n_seqs + 1]: tokens q_start[s] .. q_start[s+1] - 1 belong to sequence s (first 0, last n_tokens,
+ *             never decreasing); NULL: one token a sequence (n_tokens == n_seqs).
+ *   The n new tokens of a sequence go to positions kv_len[s] - n .. kv_len[s] - 1: kv_len already counts them
+ *   (bitnet_kv_reserve).  Positions below 0 and those without a page are left out.
+ *   k, v and the cache 16-byte aligned.  n_tokens <= 2^24.
+ */
+bitnet_status bitnet_kv_append(const bitnet_kv_cache* cache, const void* k, const void* v, int src_dtype,
+                               const int32_t* q_start, int64_t n_tokens, void* stream);
+
+/* Workspace bytes bitnet_attn_decode needs (0 is a valid answer; 0 also for unsupported sizes). */
+size_t bitnet_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,
+                                          int64_t page_size, int64_t max_pages, int64_t window, int64_t n_sink);
+
+/*
+ * bitnet_attn_decode -- attention of one new token per sequence, the last in its cache:
+ *   out[s, h] = sum_j p_j v_j, p = softmax over the visible j of scale * (q[s, h] . k_j), in the kv head h / (n_heads / n_kv_heads).
+ *   Visible: j < kv_len[s], and with window > 0 also j >= kv_len[s] - window or j < n_sink (n_sink first tokens stay in
+ *   sight).  window 0: no window.  Where nothing is visible (kv_len 0, no pages) out is 0.
+ *   q, out    device [n_seqs, n_heads, head_dim] of dtype BITNET_DTYPE_F32 or the cache's.  With F32 the products and the
+ *             softmax keep 32-bit precision whatever the cache's type; softmax statistics and sums are 32 bits always.
+ *   ws        bitnet_attn_decode_workspace_bytes(...) bytes (partial results of long sequences, which are split and joined),
+ *             any contents on entry, nothing kept between calls; NULL where that is 0.
+ *   n_heads % n_kv_heads == 0, n_heads <= 1024.  Reductions run in a fixed order: the same call gives the same bits.
+ *   Values that are not finite reach only the outputs of heads whose query sees them.
+ */
+bitnet_status bitnet_attn_decode(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads, float scale,
+                                 int64_t window, int64_t n_sink, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * bitnet_attn_prefill -- attention of a ragged batch of new tokens over the cache that already holds them (and what came
+ * before): the n tokens of sequence s are at positions p = kv_len[s] - n + i and see j <= p, with window > 0 only
+ * j > p - window or j < n_sink.  A position below 0 sees nothing (out 0).
+ *   q, out    device [n_tokens, n_heads, head_dim]; q_start device int32 [n_seqs + 1] as in bitnet_kv_append (not NULL).
+ *   dtype     BITNET_DTYPE_F32: 32-bit precision throughout (about a third of the speed: products in parts);
+ *             the cache's type: the weights are rounded to it once before the second product, their sum is not.
+ *   Rows of out that no sequence owns are not written.  Other arguments as bitnet_attn_decode; no workspace.
+ *   n_tokens <= 2^24, n_tokens * n_heads <= 2^30, n_seqs * n_kv_heads <= 2^22.
+ */
+bitnet_status bitnet_attn_prefill(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads,
+                                  const int32_t* q_start, int64_t n_tokens, float scale, int64_t window, int64_t n_sink,
+                                  void* out, void* stream);
+
+/*
+ * Pages.  bitnet_kv_pool: the caches of n_layers layers that share one table, k [n_layers, n_pages, k_page_bytes] and v
+ * likewise (layer l's bitnet_kv_cache has k + l * n_pages * k_page_bytes).  bitnet_kv_tables: table and kv_len as above and
+ * refs, device int32 [n_pages]: how many table entries name the page (0: free).  No call waits for the host: all page
+ * numbers are worked out on the device, and pages are handed out lowest number first, in the order of the call's sequences.
+ * Lists (seqs, parents, ...) are device int32 [n], n <= n_seqs; numbers outside [0, n_seqs) are left out.  ws:
+ * bitnet_kv_workspace_bytes(n_pages, n_seqs) bytes, any contents, nothing kept.
+ */
+typedef struct {
+    void* k;
+    void* v;
+    int64_t n_layers, n_pages;
+    int64_t k_page_bytes, v_page_bytes;   /* multiples of 16, up to 2^30 */
+} bitnet_kv_pool;
+
+typedef struct {
+    int32_t* table;
+    int32_t* kv_len;
+    int32_t* refs;
+    int64_t n_seqs, max_pages, n_pages;
+} bitnet_kv_tables;
+
+size_t bitnet_kv_workspace_bytes(int64_t n_pages, int64_t n_seqs);
+
+/*
+ * bitnet_kv_copy_pages -- page src[i] copied to page dst[i] in every layer, i < n; pairs with a number outside
+ * [0, n_pages) are left out.  No page may be in both lists, or twice in dst.
+ */
+bitnet_status bitnet_kv_copy_pages(const bitnet_kv_pool* pool, const int32_t* src, const int32_t* dst, int64_t n,
+                                   void* stream);
+
+/*
+ * bitnet_kv_reserve -- n_new[i] more tokens for sequence seqs[i]: pages for them in its row, kv_len += n_new[i].  A
+ * sequence that cannot have them (too few free pages left by those before it in the list, its row too short, n_new < 0)
+ * stays as it is.  n_short (device int32 [1]): how many did not get theirs.  No sequence may be named twice.
+ */
+bitnet_status bitnet_kv_reserve(const bitnet_kv_tables* tables, const int32_t* seqs, const int32_t* n_new, int64_t n,
+                                int64_t page_size, int32_t* n_short, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * bitnet_kv_fork -- sequence children[i] becomes a copy of parents[i]: full pages are shared (refs + 1), a last page that
+ * is not full is copied into a page of the child's own, so both can be appended to.  A child's row is overwritten: it must
+ * hold no pages (new, or bitnet_kv_free).  A child for which no page is left becomes empty and counts in n_short.  No
+ * child may be named twice or be a parent in the same call.
+ */
+bitnet_status bitnet_kv_fork(const bitnet_kv_pool* pool, const bitnet_kv_tables* tables, const int32_t* parents,
+                             const int32_t* children, int64_t n, int64_t page_size, int32_t* n_short, void* ws,
+                             size_t ws_bytes, void* stream);
+
+/* bitnet_kv_free -- the pages of the listed sequences given back (refs - 1), their rows -1, kv_len 0. */
+bitnet_status bitnet_kv_free(const bitnet_kv_tables* tables, const int32_t* seqs, int64_t n, void* stream);
+
+/*
+ * bitnet_kv_trim -- pages that no later token of the listed sequences sees given back: all tokens of the page at n_sink or
+ * past it and before kv_len + 1 - window.  kv_len stays; the entries become -1.  window >= 1.
+ */
+bitnet_status bitnet_kv_trim(const bitnet_kv_tables* tables, const int32_t* seqs, int64_t n, int64_t page_size,
+                             int64_t window, int64_t n_sink, void* stream);
+
+/*
+ * bitnet_kv_compact -- the live pages (refs > 0) moved to the numbers below their count, in every layer, table and refs
+ * following: the k-th lowest free number below the count takes the k-th highest live page at or above it.  n_live (device
+ * int32 [1]) receives the count.  Pages are copied, not exchanged: what is left behind at freed numbers is unspecified.
+ * kv_len is not needed (it may be NULL).
+ */
+bitnet_status bitnet_kv_compact(const bitnet_kv_pool* pool, const bitnet_kv_tables* tables, int32_t* n_live, void* ws,
+                                size_t ws_bytes, void* stream);
+
 /* Static description of a status code. */
 const char* bitnet_status_string(int status);
 

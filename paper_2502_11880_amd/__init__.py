@@ -60,6 +60,31 @@ _SIGNATURES = [
       ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     ("bitnet_elut_tables", ctypes.c_int,
      [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
+    ("bitnet_kv_page_bytes", ctypes.c_size_t,
+     [ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int]),
+    ("bitnet_kv_append", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    ("bitnet_attn_decode_workspace_bytes", ctypes.c_size_t, [ctypes.c_int64] * 8),
+    ("bitnet_attn_decode", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_int64, ctypes.c_int64,
+      ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    ("bitnet_attn_prefill", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_float,
+      ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]),
+    ("bitnet_kv_workspace_bytes", ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int64]),
+    ("bitnet_kv_copy_pages", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    ("bitnet_kv_reserve", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+      ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    ("bitnet_kv_fork", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
+      ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    ("bitnet_kv_free", ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    ("bitnet_kv_trim", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p]),
+    ("bitnet_kv_compact", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     ("bitnet_status_string", ctypes.c_char_p, [ctypes.c_int]),
     ("bitnet_last_error", ctypes.c_char_p, []),
 ]
@@ -252,6 +277,220 @@ def bitnet_elut_tables(xq, lut, lut1=None, stream=None) -> None:
     st = lib().bitnet_elut_tables(_ptr(xq, "xq", torch.int8), M, K, _ptr(lut, "lut", torch.int16),
                                   _ptr(lut1, "lut1", torch.int16), _stream(stream))
     _check("bitnet_elut_tables", st)
+
+
+# ------------------------------------------------------------------------------------------------
+# The paged key-value cache and its attention
+# ------------------------------------------------------------------------------------------------
+BITNET_DTYPE_F32 = 0
+BITNET_DTYPE_BF16 = 1
+BITNET_DTYPE_F16 = 2
+
+
+class _KvCache(ctypes.Structure):          # bitnet_kv_cache
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("n_seqs", ctypes.c_int64), ("max_pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class _KvPool(ctypes.Structure):           # bitnet_kv_pool
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_layers", ctypes.c_int64), ("n_pages", ctypes.c_int64),
+                ("k_page_bytes", ctypes.c_int64), ("v_page_bytes", ctypes.c_int64)]
+
+
+class _KvTables(ctypes.Structure):         # bitnet_kv_tables
+    _fields_ = [("table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("n_pages", ctypes.c_int64)]
+
+
+def _dtype(t, name) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return BITNET_DTYPE_F32
+    if t.dtype == torch.bfloat16:
+        return BITNET_DTYPE_BF16
+    if t.dtype == torch.float16:
+        return BITNET_DTYPE_F16
+    raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+
+
+def _cache(k_cache, v_cache, table, kv_len):
+    """The C description of one layer's cache, from tensors k_cache [n_pages, Hkv, ceil(D / 8), page_size, 8] and
+    v_cache [n_pages, Hkv, page_size / 8, D, 8] (bfloat16 or float16), table int32 [n_seqs, max_pages] and kv_len int32
+    [n_seqs]."""
+    import torch
+    if k_cache.dim() != 5 or v_cache.dim() != 5 or table.dim() != 2:
+        raise ValueError("k_cache and v_cache must have 5 dimensions and table 2")
+    pages, heads, chunks, ps, eight = k_cache.shape
+    dim = v_cache.shape[3]
+    if eight != 8 or chunks != -(-dim // 8) or v_cache.shape != (pages, heads, ps // 8, dim, 8):
+        raise ValueError(f"k_cache {tuple(k_cache.shape)} and v_cache {tuple(v_cache.shape)} are not "
+                         "[pages, heads, ceil(dim / 8), page_size, 8] and [pages, heads, page_size / 8, dim, 8]")
+    if v_cache.dtype != k_cache.dtype:
+        raise TypeError(f"v_cache must be {k_cache.dtype}, got {v_cache.dtype}")
+    seqs, width = table.shape
+    if kv_len.numel() != seqs:
+        raise ValueError(f"kv_len must have one entry for each of the {seqs} rows of table, got {kv_len.numel()}")
+    return _KvCache(_ptr(k_cache, "k_cache"), _ptr(v_cache, "v_cache"), _ptr(table, "table", torch.int32),
+                    _ptr(kv_len, "kv_len", torch.int32), pages, seqs, width, ps, heads, dim, _dtype(k_cache, "k_cache"))
+
+
+def _q_start(q_start, seqs):
+    import torch
+    if q_start.numel() != seqs + 1:
+        raise ValueError(f"q_start must have {seqs + 1} entries, got {q_start.numel()}")
+    return _ptr(q_start, "q_start", torch.int32)
+
+
+def _rows(t, name, heads_dim):
+    """Tokens of a [tokens, heads, dim] or [tokens, heads * dim] tensor."""
+    n = t.shape[0]
+    if t.numel() != n * heads_dim:
+        raise ValueError(f"{name} {tuple(t.shape)} must have rows of {heads_dim} values")
+    return n
+
+
+def bitnet_kv_page_bytes(dtype: int, page_size: int, n_kv_heads: int, head_dim: int, values: bool) -> int:
+    return int(lib().bitnet_kv_page_bytes(dtype, page_size, n_kv_heads, head_dim, 1 if values else 0))
+
+
+def bitnet_kv_append(k, v, q_start, k_cache, v_cache, table, kv_len, stream=None) -> None:
+    """Write k and v ([tokens, Hkv * D], float32 or the cache's type) into the pages of their sequences: tokens
+    q_start[s] .. q_start[s + 1] - 1 become the last ones of sequence s, whose kv_len counts them already.  q_start
+    None: one token a sequence."""
+    c = _cache(k_cache, v_cache, table, kv_len)
+    n = _rows(k, "k", c.n_kv_heads * c.head_dim)
+    if v.numel() != k.numel() or v.dtype != k.dtype:
+        raise ValueError("k and v must have one size and type")
+    st = lib().bitnet_kv_append(ctypes.byref(c), _ptr(k, "k"), _ptr(v, "v"), _dtype(k, "k"),
+                                None if q_start is None else _q_start(q_start, c.n_seqs), n, _stream(stream))
+    _check("bitnet_kv_append", st)
+
+
+def bitnet_attn_decode_workspace_bytes(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int,
+                                       max_pages: int, window: int = 0, n_sink: int = 0) -> int:
+    return int(lib().bitnet_attn_decode_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim, page_size, max_pages,
+                                                        window, n_sink))
+
+
+def _heads(q, out, c, n):
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must have q's size and type")
+    if n == 0:
+        return c.n_kv_heads
+    heads, rest = divmod(q.numel(), n * c.head_dim)
+    if rest:
+        raise ValueError(f"q {tuple(q.shape)} must have rows of whole heads of {c.head_dim}")
+    return heads
+
+
+def bitnet_attn_decode(q, k_cache, v_cache, table, kv_len, out, scale: float, window: int = 0, n_sink: int = 0, ws=None,
+                       stream=None) -> None:
+    """out[s] = attention of q[s] ([n_seqs, H * D], float32 or the cache's type) over the kv_len[s] cached tokens, or
+    with window > 0 over the last `window` and the first `n_sink` of them."""
+    c = _cache(k_cache, v_cache, table, kv_len)
+    if q.shape[0] != c.n_seqs:
+        raise ValueError(f"q must have one row for each of the {c.n_seqs} sequences, got {q.shape[0]}")
+    st = lib().bitnet_attn_decode(ctypes.byref(c), _ptr(q, "q"), _dtype(q, "q"), _heads(q, out, c, c.n_seqs), scale, window,
+                                  n_sink, _ptr(out, "out"), _ptr(ws, "ws"),
+                                  0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
+    _check("bitnet_attn_decode", st)
+
+
+def bitnet_attn_prefill(q, q_start, k_cache, v_cache, table, kv_len, out, scale: float, window: int = 0, n_sink: int = 0,
+                        stream=None) -> None:
+    """Causal attention of the new tokens q ([tokens, H * D], float32 or the cache's type), which the cache already holds:
+    rows q_start[s] .. q_start[s + 1] - 1 are the last tokens of sequence s."""
+    c = _cache(k_cache, v_cache, table, kv_len)
+    n = q.shape[0]
+    st = lib().bitnet_attn_prefill(ctypes.byref(c), _ptr(q, "q"), _dtype(q, "q"), _heads(q, out, c, n),
+                                   _q_start(q_start, c.n_seqs), n, scale, window, n_sink, _ptr(out, "out"),
+                                   _stream(stream))
+    _check("bitnet_attn_prefill", st)
+
+
+def _pool(k_pool, v_pool):
+    """The C description of the caches of all layers: k_pool [layers, *k_cache.shape], v_pool [layers, *v_cache.shape]."""
+    if k_pool.dim() != 6 or v_pool.dim() != 6 or v_pool.shape[:3] != k_pool.shape[:3]:
+        raise ValueError("k_pool and v_pool must be [layers, n_pages, heads, ...] with 6 dimensions")
+    layers, pages = k_pool.shape[:2]
+    n = max(1, layers * pages)
+    return _KvPool(_ptr(k_pool, "k_pool"), _ptr(v_pool, "v_pool"), layers, pages,
+                   k_pool.numel() // n * k_pool.element_size(), v_pool.numel() // n * v_pool.element_size())
+
+
+def _tables(table, kv_len, refs):
+    import torch
+    if table.dim() != 2 or (kv_len is not None and kv_len.numel() != table.shape[0]):
+        raise ValueError("table must be [n_seqs, max_pages] and kv_len [n_seqs]")
+    return _KvTables(_ptr(table, "table", torch.int32), _ptr(kv_len, "kv_len", torch.int32),
+                     _ptr(refs, "refs", torch.int32), table.shape[0], table.shape[1], refs.numel())
+
+
+def _list(t, name, n=None):
+    import torch
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{name} must have {n} entries, got {t.numel()}")
+    return _ptr(t, name, torch.int32)
+
+
+def bitnet_kv_workspace_bytes(n_pages: int, n_seqs: int) -> int:
+    return int(lib().bitnet_kv_workspace_bytes(n_pages, n_seqs))
+
+
+def bitnet_kv_copy_pages(k_pool, v_pool, src, dst, stream=None) -> None:
+    """Copy page src[i] to page dst[i] (int32 device lists) in every layer."""
+    p = _pool(k_pool, v_pool)
+    n = src.numel()
+    st = lib().bitnet_kv_copy_pages(ctypes.byref(p), _list(src, "src"), _list(dst, "dst", n), n, _stream(stream))
+    _check("bitnet_kv_copy_pages", st)
+
+
+def bitnet_kv_reserve(table, kv_len, refs, seqs, n_new, page_size: int, n_short, ws, stream=None) -> None:
+    """Pages for n_new[i] more tokens of sequence seqs[i], counted in kv_len; n_short (int32 [1]) receives the number of
+    sequences that could not have them and stayed as they were."""
+    t = _tables(table, kv_len, refs)
+    n = seqs.numel()
+    st = lib().bitnet_kv_reserve(ctypes.byref(t), _list(seqs, "seqs"), _list(n_new, "n_new", n), n, page_size,
+                                 _list(n_short, "n_short", 1), _ptr(ws, "ws"), ws.numel() * ws.element_size(),
+                                 _stream(stream))
+    _check("bitnet_kv_reserve", st)
+
+
+def bitnet_kv_fork(k_pool, v_pool, table, kv_len, refs, parents, children, n_short, ws, stream=None) -> None:
+    """Sequence children[i] becomes a copy of parents[i]: full pages shared, a last partial page copied in every layer."""
+    p = _pool(k_pool, v_pool)
+    t = _tables(table, kv_len, refs)
+    n = children.numel()
+    st = lib().bitnet_kv_fork(ctypes.byref(p), ctypes.byref(t), _list(parents, "parents", n), _list(children, "children"),
+                              n, k_pool.shape[4], _list(n_short, "n_short", 1), _ptr(ws, "ws"),
+                              ws.numel() * ws.element_size(), _stream(stream))
+    _check("bitnet_kv_fork", st)
+
+
+def bitnet_kv_free(table, kv_len, refs, seqs, stream=None) -> None:
+    """Give back the pages of the listed sequences."""
+    t = _tables(table, kv_len, refs)
+    st = lib().bitnet_kv_free(ctypes.byref(t), _list(seqs, "seqs"), seqs.numel(), _stream(stream))
+    _check("bitnet_kv_free", st)
+
+
+def bitnet_kv_trim(table, kv_len, refs, seqs, page_size: int, window: int, n_sink: int = 0, stream=None) -> None:
+    """Give back the listed sequences' pages that lie wholly behind the window of their next token and past the sinks."""
+    t = _tables(table, kv_len, refs)
+    st = lib().bitnet_kv_trim(ctypes.byref(t), _list(seqs, "seqs"), seqs.numel(), page_size, window, n_sink,
+                              _stream(stream))
+    _check("bitnet_kv_trim", st)
+
+
+def bitnet_kv_compact(k_pool, v_pool, table, refs, n_live, ws, stream=None) -> None:
+    """Move the live pages to the lowest numbers, in every layer; n_live (int32 [1]) receives their count."""
+    p = _pool(k_pool, v_pool)
+    t = _tables(table, None, refs)
+    st = lib().bitnet_kv_compact(ctypes.byref(p), ctypes.byref(t), _list(n_live, "n_live", 1), _ptr(ws, "ws"),
+                                 ws.numel() * ws.element_size(), _stream(stream))
+    _check("bitnet_kv_compact", st)
 
 
 def bitnet_status_string(status: int) -> str:

@@ -144,6 +144,20 @@ size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 }  // namespace
 
+namespace bitnet {
+
+int fail(int status, const char* fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
+    va_end(ap);
+    return status;
+}
+
+int hip_status(hipError_t e, const char* what) { return ::hip_status(e, what); }
+
+}  // namespace bitnet
+
 extern "C" {
 
 size_t bitnet_packed_bytes(int layout, int64_t N, int64_t K) {

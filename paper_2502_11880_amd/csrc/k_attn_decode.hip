@@ -1,0 +1,551 @@
+// Attention of one new token per sequence over the paged cache:
+//   out[b, h] = sum_j p_j v_j,  p = softmax over the visible keys j of scale q[b, h] . k_j
+// (visible: j < L, and with a window j >= L - window or j < n_sink; nothing visible: zeros).
+//
+// The cache's bytes bound it: 4 Hkv D bytes a key for 4 Hq D operations.  Keys go through in units of 32, all query heads of
+// a kv head (up to 16, a "row") at once on the 16 columns of the matrix instruction: S^T = K Q^T (two tiles of 16 keys) and
+// O^T = V^T P^T.  The rows of the two key tiles are chosen so that a lane's eight scores are those of eight consecutive keys,
+// which is its operand of the second product: the weights never leave their lane.  Maximum and sum of the softmax run along
+// (one pass over the cache), in 32 bits; the matrix instructions have so much room here that q and the weights go in as sums
+// of parts of the cache's type (see Elem), which keeps 32-bit inputs exact.
+//
+// Work is split evenly whatever the lengths: all units of the launch in one line (sequence, kv head, unit), one share of equal
+// length for every work group, which its four waves take in turn.  A row that crosses shares leaves partial results (maximum,
+// sum, unnormalised output) in the workspace, and a second launch joins them.
+#include "kv_cache.hpp"
+
+namespace bitnet {
+namespace {
+
+constexpr int kUnit = 32;            // keys of a unit
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kMaxGroups = 1024;     // work groups of a split launch
+constexpr int kMaxSeqs = 1024;       // sequences of a split launch (more go in several)
+constexpr int kMinShare = 4;         // units of a share, at least: one for each wave
+constexpr int kWholeUnits = 8;       // rows of up to so many units are never split
+
+// The keys that the last position of a sequence of length L sees: [0, sinks) and [lo, L).
+struct Sight {
+    int len, lo, sinks, sink_units, first_unit, units;   // units of the sinks, first unit of the window, all units
+};
+__host__ __device__ __forceinline__ Sight sight_of(int len, int window, int n_sink) {
+    Sight s;
+    s.len = len;
+    s.lo = window > 0 && len > window ? len - window : 0;
+    s.sinks = n_sink < s.lo ? n_sink : s.lo;
+    s.first_unit = s.lo / kUnit;
+    s.sink_units = (s.sinks + kUnit - 1) / kUnit;
+    if (s.sink_units > s.first_unit) s.sink_units = s.first_unit;
+    s.units = s.sink_units + (len + kUnit - 1) / kUnit - s.first_unit;
+    return s;
+}
+__device__ __forceinline__ int unit_key(const Sight& s, int u) {
+    return (u < s.sink_units ? u : u - s.sink_units + s.first_unit) * kUnit;
+}
+
+// Workspace of a split launch: header ints {share, units of all rows}, prefix of the units of the sequences, then two slots
+// a work group of {max[16], sum[16], output [rows16, D]} floats.
+constexpr int kHeadInts = 64;
+__host__ __device__ __forceinline__ int64_t slot_floats(int rows, int dim) { return 32 + (int64_t)rows * dim; }
+constexpr int64_t kPrefixBytes = 4 * (kHeadInts + ((kMaxSeqs + 1 + 63) / 64) * 64);
+
+struct DecodeArgs {
+    KvCache c;
+    const void* q;
+    void* out;
+    int heads, group, tiles, rows;   // query heads, of a kv head, 16-head tiles of those, heads of a tile at most (<= 16)
+    float scale2;                    // scale * log2 e
+    int window, n_sink;
+    int first_seq, n_seqs;           // of this launch
+    int32_t* ws;                     // null: one work group a row
+};
+
+// A wave's state of one row: running maximum, sum and unnormalised output; lane (n = lane & 15, g = lane >> 4) holds head n,
+// channels 16 t + 4 g + i of o[t].
+template <int DP>
+struct Row {
+    float m, l;
+    v4f o[DP / 16];
+};
+
+template <int T, int DP, bool F32>
+struct Decode {
+    static constexpr int kQParts = F32 ? Elem<T>::kExactParts : 1;
+    static constexpr int kPParts = F32 ? Elem<T>::kExactParts : 2;
+    static constexpr int kChunks = DP / 8;
+    static constexpr int kQBytes = kQParts * kChunks * 16 * 16;
+
+    // q of up to 16 heads as operands in LDS: [part][chunk][head][8]; zeros past D and past the row's heads.  Returns the
+    // factor of the scores of this lane's head (its column n).
+    static __device__ __forceinline__ void stage_q(const DecodeArgs& a, int b, int head0, int count, uint4* qs, float* gain) {
+        const int n = threadIdx.x >> 4, sub = threadIdx.x & 15;
+        const int64_t at = ((int64_t)b * a.heads + head0 + n) * a.c.dim;
+        float x[DP / 128 ? DP / 128 : 1][8];
+        float top = 0.0f;
+#pragma unroll
+        for (int r = 0; r < (DP + 127) / 128; ++r) {
+            const int d = 8 * (sub + 16 * r);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (n < count && d + 4 * half < a.c.dim) v = load4<T, F32>(a.q, at + d + 4 * half);
+                x[r][4 * half] = v.x;
+                x[r][4 * half + 1] = v.y;
+                x[r][4 * half + 2] = v.z;
+                x[r][4 * half + 3] = v.w;
+                top = fmaxf(top, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
+            }
+        }
+        float up = 1.0f;
+        if constexpr (F32 && T == kF16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, __int_as_float(dpp_row_step(__float_as_int(top), i)));
+            up = row_gain(top);
+        }
+        if (sub == 0) gain[n] = a.scale2 / up;
+#pragma unroll
+        for (int r = 0; r < (DP + 127) / 128; ++r) {
+            const int c = sub + 16 * r;
+            if (c >= kChunks) continue;
+            if constexpr (F32 && T == kF16) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[r][e] *= up;
+            }
+#pragma unroll
+            for (int p = 0; p < kQParts; ++p) {
+                uint4 w;
+                if constexpr (kQParts == 1) {   // values of the cache's type: exact
+                    w = make_uint4(Elem<T>::pack(x[r][0], x[r][1]), Elem<T>::pack(x[r][2], x[r][3]),
+                                   Elem<T>::pack(x[r][4], x[r][5]), Elem<T>::pack(x[r][6], x[r][7]));
+                } else {
+                    w.x = Elem<T>::part(x[r][0], x[r][1]);
+                    w.y = Elem<T>::part(x[r][2], x[r][3]);
+                    w.z = Elem<T>::part(x[r][4], x[r][5]);
+                    w.w = Elem<T>::part(x[r][6], x[r][7]);
+                }
+                qs[(p * kChunks + c) * 16 + n] = w;
+            }
+        }
+    }
+
+    // Units u0 .. u1 - 1 of a row, this wave's every fourth, into its state.
+    static __device__ __forceinline__ void run(const DecodeArgs& a, int b, int kvh, const Sight& sight, int u0, int u1,
+                                               const uint4* qs, float gain, Row<DP>& row) {
+        const KvCache& c = a.c;
+        const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int ps = 1 << c.shift;
+        const bool full = DP == c.dim;
+        const int32_t* table = c.table + (int64_t)b * c.max_pages;
+        const int first = u0 + wave;
+        const int count = first < u1 ? (u1 - first + kWaves - 1) / kWaves : 0;
+        if (count == 0) return;
+        const uint16_t* kbase = c.k + (int64_t)kvh * c.chunks * ps * 8;
+        const uint16_t* vbase = c.v + (int64_t)kvh * c.dim * ps;
+
+        int id0 = -1, id1 = -1;           // the pages of 64 of this wave's units, one a lane (and of their upper halves)
+        auto fetch_ids = [&](int it) {
+            const int u = first + kWaves * (it + lane);
+            id0 = id1 = -1;
+            if (u < u1) {
+                const int key = unit_key(sight, u), at = key >> c.shift;
+                id0 = table[at];
+                const int next = (key + 16) >> c.shift;
+                id1 = next == at ? id0 : next < c.max_pages ? table[next] : -1;
+            }
+        };
+        v4u kf[2][DP / 32], vf[DP / 16];
+        auto issue_k = [&](int it) {
+            const int key = unit_key(sight, first + kWaves * it);
+            const int p0 = __builtin_amdgcn_readlane(id0, it & 63), p1 = __builtin_amdgcn_readlane(id1, it & 63);
+            int page = m < 8 ? p0 : p1;
+            page = page_ok(c, page) ? page : 0;
+            const uint16_t* kp = kbase + (int64_t)page * c.k_page;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int in_page = (key + 8 * (m >> 2) + 4 * t + (m & 3)) & (ps - 1);
+#pragma unroll
+                for (int j = 0; j < DP / 32; ++j) {
+                    const int chunk = 4 * j + g;
+                    v4u w = {0u, 0u, 0u, 0u};
+                    if (full || chunk < c.chunks) w = *reinterpret_cast<const v4u*>(kp + (chunk * ps + in_page) * 8);
+                    kf[t][j] = w;
+                }
+            }
+        };
+        auto issue_v = [&](int it) {
+            const int key = unit_key(sight, first + kWaves * it);
+            const int p0 = __builtin_amdgcn_readlane(id0, it & 63), p1 = __builtin_amdgcn_readlane(id1, it & 63);
+            int page = g < 2 ? p0 : p1;
+            page = page_ok(c, page) ? page : 0;
+            const uint16_t* vp = vbase + (int64_t)page * c.v_page + ((key + 8 * g) & (ps - 1)) * c.dim;
+#pragma unroll
+            for (int t = 0; t < DP / 16; ++t) {
+                const int d = 16 * t + m;
+                v4u w = {0u, 0u, 0u, 0u};
+                if (full || d < c.dim) w = *reinterpret_cast<const v4u*>(vp + d * 8);
+                vf[t] = w;
+            }
+        };
+
+        fetch_ids(0);
+        issue_k(0);
+        issue_v(0);
+        for (int it = 0; it < count; ++it) {
+            const int key = unit_key(sight, first + kWaves * it);
+            const bool ok0 = page_ok(c, __builtin_amdgcn_readlane(id0, it & 63));
+            const bool ok1 = page_ok(c, __builtin_amdgcn_readlane(id1, it & 63));
+            v4f s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+            for (int p = 0; p < kQParts; ++p) {
+#pragma unroll
+                for (int j = 0; j < DP / 32; ++j) {
+                    const uint4 qw = qs[(p * kChunks + 4 * j + g) * 16 + m];
+                    const v4u qf = {qw.x, qw.y, qw.z, qw.w};
+                    s[0] = Elem<T>::mfma16(kf[0][j], qf, s[0]);
+                    s[1] = Elem<T>::mfma16(kf[1][j], qf, s[1]);
+                }
+            }
+            const bool more = it + 1 < count;
+            if (more) {
+                if (((it + 1) & 63) == 0) fetch_ids(it + 1);
+                issue_k(it + 1);
+            }
+            // scores of the keys key + 8 g + e, e = 4 t + i
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * gain;
+            const bool whole = ok0 && ok1 && key + kUnit <= sight.len && (key >= sight.lo || key + kUnit <= sight.sinks);
+            if (!whole) {
+                const bool there = g < 2 ? ok0 : ok1;
+                uint32_t seen = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int j = key + 8 * g + e;
+                    const bool in = there && j < sight.len && (j >= sight.lo || j < sight.sinks);
+                    seen |= in ? 1u << e : 0u;
+                    x[e] = in ? x[e] : kNegInf;
+                }
+                // nothing that is not visible enters the second product: 0 times an infinity would be no 0
+                v4u keep;
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    keep[w] = ((seen >> (2 * w)) & 1 ? 0x0000FFFFu : 0u) | ((seen >> (2 * w)) & 2 ? 0xFFFF0000u : 0u);
+#pragma unroll
+                for (int t = 0; t < DP / 16; ++t) vf[t] &= keep;
+            }
+            float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            top = max_xor32(max_xor16(top));
+            const float m_new = fmaxf(row.m, top);
+            if (__any(m_new > row.m)) {
+                const float alpha = m_new == kNegInf ? 1.0f : exp2_fast(row.m - m_new);
+                row.l *= alpha;
+#pragma unroll
+                for (int t = 0; t < DP / 16; ++t) row.o[t] *= alpha;
+                row.m = m_new;
+            }
+            const float base = (row.m == kNegInf ? 0.0f : row.m) - kLift<T>;
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = exp2_fast(x[e] - base);
+                sum += x[e];
+            }
+            row.l += sum;
+#pragma unroll
+            for (int p = 0; p < kPParts; ++p) {
+                const v4u pf = {Elem<T>::part(x[0], x[1]), Elem<T>::part(x[2], x[3]), Elem<T>::part(x[4], x[5]),
+                                Elem<T>::part(x[6], x[7])};
+#pragma unroll
+                for (int t = 0; t < DP / 16; ++t) row.o[t] = Elem<T>::mfma16(vf[t], pf, row.o[t]);
+            }
+            if (more) issue_v(it + 1);
+        }
+    }
+};
+
+template <int T, int DP, bool F32>
+__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_decode_kernel(DecodeArgs a) {
+    using D = Decode<T, DP, F32>;
+    __shared__ uint4 qs[D::kQBytes / 16];
+    __shared__ float gain[16];
+    __shared__ float wave_m[kWaves][16], wave_l[kWaves][16];
+    __shared__ int prefix[kMaxSeqs + 1];
+    __shared__ int wave_total[kWaves];
+    extern __shared__ float wave_o[];                     // [wave][head][channel]
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int per_seq = a.c.kv_heads * a.tiles;           // rows of a sequence
+    const int dim = a.c.dim;
+
+    int64_t pos, end;
+    int share = 0;
+    if (a.ws) {
+        // units of all sequences before each of them
+        int carry = 0;
+        for (int s0 = 0; s0 < a.n_seqs; s0 += kThreads) {
+            const int s = s0 + tid;
+            int u = 0;
+            if (s < a.n_seqs) {
+                u = sight_of(seq_len(a.c, a.first_seq + s), a.window, a.n_sink).units;
+                u = u > 0 ? u : 1;
+            }
+            int sum = u;
+#pragma unroll
+            for (int i = 1; i < 64; i <<= 1) {
+                const int other = __shfl_up(sum, i);
+                if (lane >= i) sum += other;
+            }
+            if (lane == 63) wave_total[wave] = sum;
+            __syncthreads();
+            int before = carry;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) before += w < wave ? wave_total[w] : 0;
+            if (s < a.n_seqs) prefix[s] = before + sum - u;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) carry += wave_total[w];
+            __syncthreads();
+        }
+        if (tid == 0) prefix[a.n_seqs] = carry;
+        __syncthreads();
+        const int64_t all = (int64_t)carry * per_seq;
+        share = (int)((all + gridDim.x - 1) / gridDim.x);
+        share = share < kMinShare ? kMinShare : share;
+        if (blockIdx.x == 0) {
+            if (tid == 0) a.ws[0] = share;
+            for (int s = tid; s <= a.n_seqs; s += kThreads) a.ws[kHeadInts + s] = prefix[s];
+        }
+        pos = (int64_t)blockIdx.x * share;
+        end = pos + share < all ? pos + share : all;
+    } else {
+        pos = 0;
+        end = 1;
+    }
+    const int64_t start = pos;
+
+    while (pos < end) {
+        int s, row, u0, u1, units;
+        Sight sight;
+        if (a.ws) {
+            int lo = 0, hi = a.n_seqs - 1;                // the last sequence that starts at pos or before
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if ((int64_t)prefix[mid] * per_seq <= pos) lo = mid;
+                else hi = mid - 1;
+            }
+            s = lo;
+            units = prefix[s + 1] - prefix[s];
+            const int at = (int)(pos - (int64_t)prefix[s] * per_seq);
+            row = at / units;
+            u0 = at - row * units;
+            u1 = end - pos < units - u0 ? u0 + (int)(end - pos) : units;
+        } else {
+            s = blockIdx.x / per_seq;
+            row = blockIdx.x - s * per_seq;
+            u0 = 0;
+        }
+        const int b = a.first_seq + s;
+        sight = sight_of(seq_len(a.c, b), a.window, a.n_sink);
+        if (!a.ws) u1 = units = sight.units;
+        const int kvh = row / a.tiles, tile = row - kvh * a.tiles;
+        const int head0 = kvh * a.group + tile * 16;
+        const int count = a.group - tile * 16 < 16 ? a.group - tile * 16 : 16;
+        D::stage_q(a, b, head0, count, qs, gain);
+        __syncthreads();
+
+        Row<DP> r;
+        r.m = kNegInf;
+        r.l = 0.0f;
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t) r.o[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        D::run(a, b, kvh, sight, u0, u1 < sight.units ? u1 : sight.units, qs, gain[n], r);
+
+        // the four waves' states become one
+        r.l = sum_xor32(sum_xor16(r.l));
+        if (g == 0) {
+            wave_m[wave][n] = r.m;
+            wave_l[wave][n] = r.l;
+        }
+        __syncthreads();
+        float top = wave_m[0][n];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, wave_m[w][n]);
+        const float f = r.m == kNegInf ? 0.0f : exp2_fast(r.m - top);
+        if (n < count) {
+#pragma unroll
+            for (int t = 0; t < DP / 16; ++t) {
+                const v4f o = r.o[t] * f;
+                *reinterpret_cast<v4f*>(&wave_o[(wave * a.rows + n) * DP + 16 * t + 4 * g]) = o;
+            }
+        }
+        __syncthreads();
+        const bool complete = u0 == 0 && u1 == units;
+        float* slot = nullptr;
+        if (!complete) {
+            slot = reinterpret_cast<float*>(a.ws) + kPrefixBytes / 4 +
+                   (2 * (int64_t)blockIdx.x + (pos == start ? 0 : 1)) * slot_floats(a.rows, dim);
+            if (tid < 16) {
+                float mm = kNegInf, ll = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, wave_m[w][tid]);
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w)
+                    ll += wave_l[w][tid] * (wave_m[w][tid] == kNegInf ? 0.0f : exp2_fast(wave_m[w][tid] - mm));
+                slot[tid] = mm;
+                slot[16 + tid] = ll;
+            }
+        }
+        const int quads = dim >> 2;
+        for (int i = tid; i < count * quads; i += kThreads) {
+            const int head = i / quads, d = 4 * (i - head * quads);
+            v4f o = *reinterpret_cast<const v4f*>(&wave_o[head * DP + d]);
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) o += *reinterpret_cast<const v4f*>(&wave_o[(w * a.rows + head) * DP + d]);
+            if (complete) {
+                float mm = kNegInf, ll = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, wave_m[w][head]);
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w)
+                    ll += wave_l[w][head] * (wave_m[w][head] == kNegInf ? 0.0f : exp2_fast(wave_m[w][head] - mm));
+                const bool none = ll == 0.0f;             // nothing visible
+                store4<T, F32>(a.out, ((int64_t)b * a.heads + head0 + head) * dim + d, none ? 0.0f : o[0] / ll,
+                               none ? 0.0f : o[1] / ll, none ? 0.0f : o[2] / ll, none ? 0.0f : o[3] / ll);
+            } else {
+                *reinterpret_cast<v4f*>(slot + 32 + (int64_t)head * dim + d) = o;
+            }
+        }
+        if (!a.ws) break;
+        pos += u1 - u0;
+        __syncthreads();
+    }
+}
+
+// Rows that crossed shares: their partial results, in the order of the keys.  One work group a row and 64 quads of channels
+// (head, 4 channels); its four waves take the parts in turn and are added up in order.
+template <int T, bool F32>
+__global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
+    __shared__ v4f part_o[4][64];
+    __shared__ float part_m[4][64], part_l[4][64];
+    const int per_seq = a.c.kv_heads * a.tiles, dim = a.c.dim;
+    const int s = blockIdx.x / per_seq, row = blockIdx.x - s * per_seq;
+    const int kvh = row / a.tiles, tile = row - kvh * a.tiles;
+    const int count = a.group - tile * 16 < 16 ? a.group - tile * 16 : 16;
+    const int share = a.ws[0];
+    const int64_t before = a.ws[kHeadInts + s];
+    const int units = a.ws[kHeadInts + s + 1] - (int)before;
+    const int64_t first = before * per_seq + (int64_t)row * units, last = first + units - 1;
+    const int w0 = (int)(first / share), w1 = (int)(last / share);
+    if (w0 == w1) return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int i = blockIdx.y * 64 + lane, quads = dim >> 2;
+    const bool in = i < count * quads;
+    const int head = in ? i / quads : 0, d = in ? 4 * (i - head * quads) : 0;
+    const float* slots = reinterpret_cast<const float*>(a.ws) + kPrefixBytes / 4;
+    const int64_t step = slot_floats(a.rows, dim);
+    float m = kNegInf, l = 0.0f;
+    v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int w = w0 + wave; w <= w1; w += 4) {
+        const int which = w == w0 && first != (int64_t)w0 * share ? 1 : 0;
+        const float* slot = slots + (2 * (int64_t)w + which) * step;
+        const float pm = slot[head], pl = slot[16 + head];
+        const v4f po = *reinterpret_cast<const v4f*>(slot + 32 + (int64_t)head * dim + d);
+        const float top = fmaxf(m, pm);
+        const float fa = m == kNegInf ? 0.0f : exp2_fast(m - top), fb = pm == kNegInf ? 0.0f : exp2_fast(pm - top);
+        o = o * fa + po * fb;
+        l = l * fa + pl * fb;
+        m = top;
+    }
+    part_m[wave][lane] = m;
+    part_l[wave][lane] = l;
+    part_o[wave][lane] = o;
+    __syncthreads();
+    if (wave != 0 || !in) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        const float pm = part_m[w][lane];
+        const float top = fmaxf(m, pm);
+        const float fa = m == kNegInf ? 0.0f : exp2_fast(m - top), fb = pm == kNegInf ? 0.0f : exp2_fast(pm - top);
+        o = o * fa + part_o[w][lane] * fb;
+        l = l * fa + part_l[w][lane] * fb;
+        m = top;
+    }
+    const bool none = l == 0.0f;
+    const int64_t at = ((int64_t)(a.first_seq + s) * a.heads + kvh * a.group + tile * 16 + head) * dim + d;
+    store4<T, F32>(a.out, at, none ? 0.0f : o[0] / l, none ? 0.0f : o[1] / l, none ? 0.0f : o[2] / l,
+                   none ? 0.0f : o[3] / l);
+}
+
+template <int T, int DP, bool F32>
+hipError_t launch(DecodeArgs a, bool split, hipStream_t s) {
+    const size_t lds = (size_t)kWaves * a.rows * DP * 4;
+    const int rows = a.c.kv_heads * a.tiles;
+    const int total = a.n_seqs, first = a.first_seq;
+    if (!split) {
+        a.ws = nullptr;
+        const int64_t most = (1 << 23) / rows;            // a grid has fewer than 2^32 threads
+        for (int64_t at = 0; at < total; at += most) {
+            a.first_seq = first + (int)at;
+            a.n_seqs = (int)(total - at < most ? total - at : most);
+            hipLaunchKernelGGL((attn_decode_kernel<T, DP, F32>), dim3((unsigned)(a.n_seqs * rows)), dim3(kThreads), lds, s, a);
+        }
+        return hipGetLastError();
+    }
+    for (int at = 0; at < total; at += kMaxSeqs) {
+        a.first_seq = first + at;
+        a.n_seqs = total - at < kMaxSeqs ? total - at : kMaxSeqs;
+        hipLaunchKernelGGL((attn_decode_kernel<T, DP, F32>), dim3(kMaxGroups), dim3(kThreads), lds, s, a);
+        hipLaunchKernelGGL((attn_join_kernel<T, F32>), dim3((unsigned)(a.n_seqs * rows), (unsigned)((a.rows * a.c.dim / 4 + 63) / 64)),
+                           dim3(256), 0, s, a);
+    }
+    return hipGetLastError();
+}
+
+template <int T, bool F32>
+hipError_t launch_dim(const DecodeArgs& a, bool split, hipStream_t s) {
+    if (a.c.dim <= 64) return launch<T, 64, F32>(a, split, s);
+    if (a.c.dim <= 128) return launch<T, 128, F32>(a, split, s);
+    return launch<T, 256, F32>(a, split, s);
+}
+
+int most_units(int64_t max_pages, int page_size, int window, int n_sink) {
+    const int64_t keys = max_pages * page_size;
+    int64_t units = (keys + kUnit - 1) / kUnit;
+    if (window > 0) {
+        const int64_t near = (window + kUnit - 1) / kUnit + 1 + ((int64_t)n_sink + kUnit - 1) / kUnit;
+        units = near < units ? near : units;
+    }
+    return (int)units;
+}
+
+}  // namespace
+
+size_t attn_decode_workspace_bytes(int64_t, int heads, int kv_heads, int dim, int page_size, int64_t max_pages, int window,
+                                   int n_sink) {
+    if (most_units(max_pages, page_size, window, n_sink) <= kWholeUnits) return 0;
+    const int group = heads / kv_heads;
+    return (size_t)kPrefixBytes + (size_t)(2 * kMaxGroups * slot_floats(group < 16 ? group : 16, dim)) * 4;
+}
+
+hipError_t launch_attn_decode(const KvCache& c, int dtype, const AttnArgs& args, void* ws, hipStream_t s) {
+    DecodeArgs a{};
+    a.c = c;
+    a.q = args.q;
+    a.out = args.out;
+    a.heads = args.heads;
+    a.group = args.heads / c.kv_heads;
+    a.tiles = (a.group + 15) / 16;
+    a.rows = a.group < 16 ? a.group : 16;
+    a.scale2 = args.scale * kLog2e;
+    a.window = args.window;
+    a.n_sink = args.n_sink;
+    a.n_seqs = c.n_seqs;
+    a.ws = static_cast<int32_t*>(ws);
+    const bool split = most_units(c.max_pages, 1 << c.shift, args.window, args.n_sink) > kWholeUnits;
+    if (dtype == kBf16) return args.f32 ? launch_dim<kBf16, true>(a, split, s) : launch_dim<kBf16, false>(a, split, s);
+    return args.f32 ? launch_dim<kF16, true>(a, split, s) : launch_dim<kF16, false>(a, split, s);
+}
+
+}  // namespace bitnet

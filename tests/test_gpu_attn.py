@@ -1,0 +1,298 @@
+"""GPU parity of the attention over the paged cache against a plain 64-bit implementation: lengths from none to tens of
+thousands, every page size and type, odd head counts and sizes, windows and sinks, pages that are not there, and values that
+are not finite wherever nothing may read them.  Tolerances follow from the arithmetic (tests/kv_model.py)."""
+import math
+
+import pytest
+import torch
+
+import paper_2502_11880_amd as B
+from tests import kv_model as M
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def _announce(*what):
+    print("case:", *what, flush=True)
+
+
+def _ws(n, H, Hkv, D, page, width, window, sinks):
+    need = B.bitnet_attn_decode_workspace_bytes(n, H, Hkv, D, page, width, window, sinks)
+    return torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device=DEV)     # NaN patterns: nothing in it may matter
+
+
+def _decode(b, H, q, scale, window=0, sinks=0, tensors=None, stream=None):
+    k, v, table, lens = tensors or b.on(DEV)
+    out = torch.full_like(q, float("nan"))
+    B.bitnet_attn_decode(q, k, v, table, lens, out, scale, window, sinks,
+                         _ws(len(b.lens), H, b.heads, b.dim, b.page, table.shape[1], window, sinks), stream)
+    torch.cuda.synchronize()
+    return out
+
+
+def _check_decode(b, H, io, seed, window=0, sinks=0, scale=None, rows=None):
+    scale = 1 / math.sqrt(b.dim) if scale is None else scale
+    q = torch.randn(len(b.lens), H * b.dim, generator=torch.Generator().manual_seed(seed)).to(M.DTYPES[io])
+    out = _decode(b, H, q.to(DEV), scale, window, sinks).cpu().view(-1, H, b.dim)
+    for s in range(len(b.lens)) if rows is None else rows:
+        n = b.lens[s]
+        if n == 0:
+            assert not out[s].any(), "an empty sequence gives zeros"
+            continue
+        there = (b.table[s].repeat_interleave(b.page)[:n] >= 0)[None]
+        seen = M.visible(torch.tensor([n - 1]), n, window, sinks) & there
+        want, tol = M.attention(q[s].view(1, H, b.dim), b.k[s], b.v[s], seen, scale, M.io_eps(io), 2.0 ** -15 if io != "f32" else 0.0)
+        M.check(out[s][None], want, tol, f"sequence {s} of {n}")
+
+
+LENS = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100, 129, 255, 257, 300, 520]
+
+
+@pytest.mark.parametrize("io", ["f32", "cache"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("H,Hkv,D,page", [(4, 1, 128, 16), (32, 8, 128, 32), (3, 3, 100, 64), (6, 2, 64, 128), (5, 1, 256, 256),
+                                          (16, 1, 80, 16), (17, 1, 20, 32), (40, 1, 132, 16), (4, 2, 4, 16)])
+def test_decode_lengths(H, Hkv, D, page, dtype, io):
+    _announce("decode", H, Hkv, D, page, dtype, io)
+    b = M.Batch(LENS, Hkv, D, page, dtype, seed=H + D)
+    _check_decode(b, H, dtype if io == "cache" else io, seed=1)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 4), (31, 70), (64, 32), (100, 33), (1000, 5), (200, 10 ** 9), (10 ** 12, 3)])
+@pytest.mark.parametrize("H,Hkv,D,page,dtype,io", [(8, 2, 128, 16, "bf16", "f32"), (4, 4, 100, 64, "f16", "f32"), (4, 1, 64, 32, "bf16", "bf16")])
+def test_decode_window_and_sinks(H, Hkv, D, page, dtype, io, window, sinks):
+    _announce("decode window", H, Hkv, D, page, dtype, io, window, sinks)
+    b = M.Batch(LENS + [1100, 2049], Hkv, D, page, dtype, seed=D + 7)
+    _check_decode(b, H, io, seed=2, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("lens,H,Hkv,D,page,dtype,io", [([40001], 4, 1, 64, 16, "bf16", "f32"), ([20000, 7, 0, 3333], 8, 2, 128, 128, "f16", "f16"),
+                                                        ([9000] * 3, 2, 2, 256, 64, "bf16", "bf16"), ([5000, 1, 5000], 32, 1, 36, 32, "f16", "f32")])
+def test_decode_long(lens, H, Hkv, D, page, dtype, io):
+    _announce("decode long", lens, H, Hkv, D, page, dtype, io)
+    _check_decode(M.Batch(lens, Hkv, D, page, dtype, seed=3), H, io, seed=3)
+
+
+def test_decode_more_sequences_than_one_launch_splits():
+    _announce("decode 2500 sequences")
+    lens = [(37 * i) % 400 for i in range(2500)]
+    b = M.Batch(lens, 1, 64, 32, "bf16", seed=4, width=13)
+    _check_decode(b, 2, "f32", seed=4, rows=[0, 1, 2, 1023, 1024, 1025, 2047, 2048, 2499])
+
+
+def test_decode_missing_pages_and_bad_lengths():
+    _announce("decode missing pages")
+    b = M.Batch([300, 300, 300, 64], 2, 64, 32, "bf16", seed=5)
+    b.table[0, 2:5] = -1                     # taken out of the middle
+    b.table[1, 0] = 10 ** 6                  # no page of the pool
+    b.table[2, :] = -1                       # none left at all: zeros
+    b.table[3, 1] = -2 ** 31
+    q = torch.randn(4, 4 * 64, generator=torch.Generator().manual_seed(6))
+    out = _decode(b, 4, q.to(DEV), 0.125).cpu().view(4, 4, 64)
+    for s in (0, 1, 3):
+        there = (b.table[s].repeat_interleave(32)[:b.lens[s]])
+        seen = ((there >= 0) & (there < b.pages))[None]
+        want, tol = M.attention(q[s].view(1, 4, 64), b.k[s], b.v[s], seen, 0.125, M.io_eps("f32"), 0.0)
+        M.check(out[s][None], want, tol, f"sequence {s}")
+    assert not out[2].any()
+    k, v, table, lens = b.on(DEV)            # lengths that no row of the table holds: what it holds counts
+    lens[0], lens[3] = -5, 10 ** 9
+    out = _decode(b, 4, q.to(DEV), 0.125, tensors=(k, v, table, lens)).cpu()
+    assert not out[0].any() and torch.isfinite(out[1]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_decode_extreme_values(dtype):
+    _announce("decode extremes", dtype)
+    big = torch.finfo(M.DTYPES[dtype]).max / 128         # the scores stay finite
+    b = M.Batch([70, 70, 70, 40], 1, 64, 16, dtype, seed=8)
+    b.k[0][5] = big                          # one key whose score dwarfs the others'
+    b.k[1][:] = 0.0                          # all scores alike
+    b.v[2][3, 0, 7] = float("inf")           # seen: reaches channel 7 alone
+    b.v[2][4, 0, 9] = float("nan")
+    b.k[3][:] = -big                         # all scores at the type's lowest value
+    for s in range(4):
+        b.write(s, 0, b.k[s], b.v[s])
+    q = torch.ones(4, 2 * 64)
+    out = _decode(b, 2, q.to(DEV), 0.125).cpu().view(4, 2, 64)
+    for s in (0, 1, 3):
+        want, tol = M.attention(q[s].view(1, 2, 64), b.k[s], b.v[s], torch.ones(1, b.lens[s], dtype=torch.bool), 0.125, 2.0 ** -23, 0.0)
+        M.check(out[s][None], want, tol, f"sequence {s}")
+    bad = ~torch.isfinite(out[2])
+    assert bad[:, 7].all() and bad[:, 9].all() and int(bad.sum()) == 4
+
+
+def test_decode_tiny_and_huge_queries_keep_their_precision():
+    _announce("decode query ranges")
+    for dtype in ("bf16", "f16"):
+        b = M.Batch([90] * 4, 1, 128, 32, dtype, seed=9)
+        q = torch.randn(4, 128, generator=torch.Generator().manual_seed(9)) * torch.tensor([1e-30, 1e-6, 1e6, 1.0])[:, None]
+        q[3, 1:] *= 1e-5
+        for s, scale in enumerate((1e29, 1e5, 1e-7, 1.0)):
+            out = _decode(b, 1, q.to(DEV), scale).cpu().view(4, 1, 128)
+            want, tol = M.attention(q[s].view(1, 1, 128), b.k[s], b.v[s], torch.ones(1, 90, dtype=torch.bool), scale, 2.0 ** -23, 0.0)
+            M.check(out[s][None], want, tol, f"{dtype} {scale}")
+
+
+def test_decode_is_reproducible_and_takes_a_stream():
+    _announce("decode twice")
+    b = M.Batch([3000, 10, 700], 4, 128, 16, "bf16", seed=10)
+    q = torch.randn(3, 16 * 128, generator=torch.Generator().manual_seed(10)).to(DEV)
+    t = b.on(DEV)
+    first = _decode(b, 16, q, 0.1, tensors=t)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        assert torch.equal(first, _decode(b, 16, q, 0.1, tensors=t, stream=side))
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Prompts
+# ---------------------------------------------------------------------------------------------------------------------
+def _prefill(b, H, q, new, scale, window=0, sinks=0, tensors=None):
+    k, v, table, lens = tensors or b.on(DEV)
+    start = torch.tensor([0] + new, dtype=torch.int32).cumsum(0).to(torch.int32).to(DEV)
+    out = torch.full_like(q, float("nan"))
+    B.bitnet_attn_prefill(q, start, k, v, table, lens, out, scale, window, sinks)
+    torch.cuda.synchronize()
+    return out
+
+
+def _check_prefill(b, H, new, io, seed, window=0, sinks=0):
+    scale = 1 / math.sqrt(b.dim)
+    q = torch.randn(sum(new), H * b.dim, generator=torch.Generator().manual_seed(seed)).to(M.DTYPES[io])
+    out = _prefill(b, H, q.to(DEV), new, scale, window, sinks).cpu().view(-1, H, b.dim)
+    at = 0
+    for s, n in enumerate(new):
+        if n == 0:
+            continue
+        L = b.lens[s]
+        pos = torch.arange(L - n, L)
+        seen = M.visible(pos, L, window, sinks)
+        there = b.table[s].repeat_interleave(b.page)[:L]
+        seen &= ((there >= 0) & (there < b.pages))[None]
+        qs, got = q[at:at + n].view(n, H, b.dim), out[at:at + n]
+        if L == 0:
+            assert not got.any()
+        else:
+            # a weight rounded once to the cache's type
+            weight = 0.0 if io == "f32" else {"bf16": 2.0 ** -8, "f16": 2.0 ** -10}[io]
+            want, tol = M.attention(qs, b.k[s], b.v[s], seen, scale, M.io_eps(io), weight)
+            M.check(got, want, tol, f"sequence {s}: {n} of {L}")
+        at += n
+
+
+@pytest.mark.parametrize("io", ["f32", "cache"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("H,Hkv,D,page", [(4, 1, 128, 16), (8, 2, 128, 32), (3, 3, 100, 64), (6, 2, 64, 128), (5, 1, 256, 256),
+                                          (16, 1, 80, 16), (17, 1, 20, 32), (3, 1, 132, 16), (4, 2, 4, 16)])
+def test_prefill_lengths(H, Hkv, D, page, dtype, io):
+    _announce("prefill", H, Hkv, D, page, dtype, io)
+    new = [1, 0, 2, 31, 33, 64, 65, 130, 7, 0, 20]
+    past = [0, 5, 0, 1, 0, 70, 3, 0, 200, 0, 64]
+    b = M.Batch([n + p for n, p in zip(new, past)], Hkv, D, page, dtype, seed=H + D)
+    _check_prefill(b, H, new, dtype if io == "cache" else io, seed=11)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 4), (31, 70), (64, 64), (100, 33), (1000, 5), (200, 10 ** 9), (10 ** 12, 3)])
+@pytest.mark.parametrize("H,Hkv,D,page,dtype,io", [(8, 2, 128, 16, "bf16", "f32"), (3, 3, 100, 64, "f16", "f32"), (4, 1, 64, 32, "bf16", "bf16"),
+                                                   (2, 2, 128, 256, "f16", "f16")])
+def test_prefill_window_and_sinks(H, Hkv, D, page, dtype, io, window, sinks):
+    _announce("prefill window", H, Hkv, D, page, dtype, io, window, sinks)
+    new, past = [300, 17, 1, 129], [0, 500, 333, 64]
+    b = M.Batch([n + p for n, p in zip(new, past)], Hkv, D, page, dtype, seed=D)
+    _check_prefill(b, H, new, io, seed=12, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype,io,D", [("bf16", "bf16", 128), ("bf16", "f32", 128), ("f16", "f32", 100)])
+def test_prefill_long(dtype, io, D):
+    _announce("prefill long", dtype, io, D)
+    b = M.Batch([1500, 700], 2, D, 64, dtype, seed=13)
+    _check_prefill(b, 4, [1500, 600], io, seed=13)
+
+
+def test_prefill_more_tokens_than_cached_and_missing_pages():
+    _announce("prefill short cache")
+    b = M.Batch([5, 40, 100], 1, 64, 16, "bf16", seed=14)
+    b.table[2, 1:3] = -1
+    q = torch.randn(90, 2 * 64, generator=torch.Generator().manual_seed(14))
+    out = _prefill(b, 2, q.to(DEV), [20, 40, 30], 0.125).cpu().view(90, 2, 64)
+    assert not out[:15].any(), "positions below 0 see nothing"
+    M.check(out[15:20], *M.attention(q[15:20].view(5, 2, 64), b.k[0], b.v[0], M.visible(torch.arange(5), 5, 0, 0), 0.125, 2.0 ** -23, 0.0))
+    there = (b.table[2].repeat_interleave(16)[:100] >= 0)[None]
+    seen = M.visible(torch.arange(70, 100), 100, 0, 0) & there
+    M.check(out[60:], *M.attention(q[60:].view(30, 2, 64), b.k[2], b.v[2], seen, 0.125, 2.0 ** -23, 0.0))
+
+
+def test_prefill_rows_of_no_sequence_stay():
+    _announce("prefill spans that do not fit")
+    b = M.Batch([30, 30], 1, 64, 16, "bf16", seed=15)
+    q = torch.randn(40, 64, generator=torch.Generator().manual_seed(15)).to(DEV)
+    k, v, table, lens = b.on(DEV)
+    out = torch.full_like(q, 7.0)
+    B.bitnet_attn_prefill(q, torch.tensor([0, 30, 90], dtype=torch.int32, device=DEV), k, v, table, lens, out, 0.125)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out).all() and (out[30:] == 7.0).all() and not (out[:30] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype,io", [("bf16", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f16", "f16")])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (40, 3)])
+def test_prefill_values_that_are_not_finite_reach_only_queries_that_see_them(dtype, io, window, sinks):
+    _announce("prefill not finite", dtype, io, window)
+    b = M.Batch([230], 1, 128, 16, dtype, seed=16)
+    b.v[0][100, 0, 3] = float("nan")
+    b.v[0][101, 0, 90] = float("inf")
+    b.v[0][150, 0, 90] = float("-inf")
+    b.v[0][229, 0, 127] = float("-inf")
+    b.v[0][0, 0, 0] = float("inf")
+    b.k[0][180, 0, 5] = float("nan")
+    b.write(0, 0, b.k[0], b.v[0])
+    q = torch.randn(230, 3 * 128, generator=torch.Generator().manual_seed(16)).to(M.DTYPES[io])
+    out = _prefill(b, 3, q.to(DEV), [230], 0.09, window, sinks).cpu().double().view(230, 3, 128)
+    seen = M.visible(torch.arange(230), 230, window, sinks)
+    clean = b.k[0].clone()
+    clean[180] = 0.0
+    weight = 0.0 if io == "f32" else {"bf16": 2.0 ** -8, "f16": 2.0 ** -10}[io]
+    want, tol = M.attention(q.view(230, 3, 128), clean, b.v[0], seen, 0.09, M.io_eps(io), weight)
+    nan_key = seen[:, 180]
+    assert torch.isnan(out[nan_key]).all(), "a score that is no number spoils its row"
+    fine = torch.isfinite(want[~nan_key])
+    assert torch.equal(torch.isfinite(out[~nan_key]), fine), "values that are not finite reach exactly the queries that see them"
+    M.check(torch.where(fine, out[~nan_key], 0.0), torch.where(fine, want[~nan_key], 0.0), tol[~nan_key])
+
+
+def test_prefill_ends_where_decode_does():
+    _announce("prefill against decode")
+    b = M.Batch([333], 2, 128, 32, "bf16", seed=17)
+    q = torch.randn(333, 8 * 128, generator=torch.Generator().manual_seed(17)).to(DEV)
+    whole = _prefill(b, 8, q, [333], 0.09, 64, 4)
+    one = _decode(b, 8, q[-1:].contiguous(), 0.09, 64, 4)
+    assert float((whole[-1:] - one).abs().max()) < 1e-5
+
+
+def test_cache_past_four_gib():
+    _announce("cache of 5 GiB")
+    H, D, page, dtype = 8, 128, 256, torch.bfloat16
+    pages = (5 << 30) // (H * D * page * 2)
+    k = torch.empty(pages, H, D // 8, page, 8, dtype=dtype, device=DEV)
+    v = torch.empty(pages, H, page // 8, D, 8, dtype=dtype, device=DEV)
+    b = M.Batch([600], H, D, page, "bf16", seed=18)
+    far = torch.tensor([pages - 1, 0, pages - 2], dtype=torch.int32)
+    for i, p in enumerate(far.tolist()):
+        k[p], v[p] = b.k_cache[b.table[0, i]].to(DEV), b.v_cache[b.table[0, i]].to(DEV)
+    table, lens = far.view(1, 3).to(DEV), b.kv_len.to(DEV)
+    q = torch.randn(20, 2 * H * D, generator=torch.Generator().manual_seed(18))
+    want, tol = M.attention(q.view(20, 2 * H, D), b.k[0], b.v[0], M.visible(torch.arange(580, 600), 600, 0, 0), 0.09, 2.0 ** -23, 0.0)
+    out = torch.empty_like(q, device=DEV)
+    B.bitnet_attn_prefill(q.to(DEV), torch.tensor([0, 20], dtype=torch.int32, device=DEV), k, v, table, lens, out, 0.09)
+    M.check(out.view(20, 2 * H, D), want, tol, "prefill")
+    out = torch.empty(1, 2 * H * D, device=DEV)
+    B.bitnet_attn_decode(q[19:].contiguous().to(DEV), k, v, table, lens, out, 0.09, ws=_ws(1, 2 * H, H, D, page, 3, 0, 0))
+    M.check(out.view(1, 2 * H, D), want[19:], tol[19:], "decode")
+    new = torch.randn(1, H * D, generator=torch.Generator().manual_seed(19)).to(DEV)
+    B.bitnet_kv_append(new, -new, None, k, v, table, lens)
+    torch.cuda.synchronize()
+    assert torch.equal(k[pages - 2, :, :, 599 - 512].reshape(-1), new[0].to(dtype))
+    assert torch.equal(v[pages - 2, :, (599 - 512) // 8, :, (599 - 512) % 8].reshape(-1), -new[0].to(dtype))
