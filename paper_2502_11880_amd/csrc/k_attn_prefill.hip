@@ -36,347 +36,552 @@ __device__ __forceinline__ int first_tile(const int32_t* q_start, int b, int gro
     return (int)((int64_t)q_start[b] * group / columns) + b;
 }
 
-template <int T, int DP, bool F32, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_prefill_kernel(PrefillArgs a) {
-    constexpr int kQParts = F32 ? Elem<T>::kExactParts : 1;
-    constexpr int kPParts = F32 ? Elem<T>::kExactParts : 1;
-    constexpr int kThreads = 64 * WAVES, kColumns = 32 * WAVES;
-    constexpr int kSteps = DP / 16, kBlocks = DP / 32;
-    constexpr int kWords = kTile * DP / 8;               // 16-byte words of a tile's keys (and at most of its values)
-    constexpr int kLoads = kWords / kThreads;
-    __shared__ uint4 kt[2][kWords];                       // [chunk][key]
-    __shared__ uint4 vt[2][kWords + 32];                  // [eight keys][channel]; reads of channels past D run on
-    __shared__ int odd_tile[2];                           // the last masked tile of the buffer with values that are not finite
-    const KvCache& c = a.c;
-    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, n = lane & 31;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int dim = c.dim, ps = 1 << c.shift;
-    const bool full = dim == DP;
+template <int T, int DP, bool F32, int WAVES, bool FULL>
+struct Prefill {
+    static constexpr int kQParts = F32 ? Elem<T>::kExactParts : 1;
+    static constexpr int kPParts = kQParts;
+    static constexpr int kThreads = 64 * WAVES, kColumns = 32 * WAVES;
+    static constexpr int kSteps = DP / 16, kBlocks = (DP + 31) / 32;
+    static constexpr int kWords = kTile * DP / 8;         // 16-byte words of a tile's keys (and at most of its values)
+    static constexpr int kLoads = (kWords + kThreads - 1) / kThreads;
+    static constexpr int kAhead = 4;                      // words of the keys on their way from LDS
+    static constexpr int kSchedMfma = 0x8, kSchedLds = 0x100;
 
-    // work groups of one kv head follow each other at a distance of kv_heads (with 8 of them: on one XCD, whose L2 keeps the
-    // head's keys), the last tiles, which have the most keys before them, first
-    const int kvh = blockIdx.x % c.kv_heads;
-    const int id = a.tiles - 1 - (int)(blockIdx.x / c.kv_heads);
-    const int b = find_last(c.n_seqs, id, [&](int i) { return first_tile(a.q_start, i, a.group, kColumns); });
-    const Span span = span_of(a.q_start, b, a.n_tokens);
-    const int col0 = (id - first_tile(a.q_start, b, a.group, kColumns)) * kColumns;
-    const int columns = span.count * a.group;
-    if (col0 >= columns) return;
-    const int len = seq_len(c, b);
-    const int p0 = len - span.count;                      // position of the first token (below 0: it sees nothing)
+    struct Lds {
+        uint4 k[2][kLoads * kThreads];                    // [chunk][key]
+        uint4 v[2][kWords + 32];                          // [eight keys][channel]; reads of channels past D run on
+        int odd;                                          // a masked tile has values that are not finite
+    };
 
-    const int col = col0 + wave * 32 + n;
-    const bool used = col < columns;
-    const int token = (used ? col : columns - 1) / a.group, in_group = (used ? col : columns - 1) - token * a.group;
-    const int pos = p0 + token;
-    const int64_t row = ((int64_t)(span.first + token) * a.heads + kvh * a.group + in_group) * dim;
+    const PrefillArgs& a;
+    Lds& lds;
+    int tid, half, n, dim, ps, dim_magic;
+    int kvh, b, len;
+    int pos, low;                                         // of this column; keys up to low are behind its window
+    int wave_first, wave_last, open_first, open_last;     // tiles that this wave sees, and those that all its columns see
+    int group_first, group_last;                          // tiles that all columns of the work group see
+    int sink_end;                                         // tiles with sinks end here
+    int sink_tiles, first, n_tiles;
+    const int32_t* table;
+    const uint16_t *kbase, *vbase;
+    int key_row;
 
-    // q as operands: chunk 2 s + half of this lane's column, in parts
-    v4u qf[kQParts][kSteps];
-    float gain = a.scale2;
-    {
-        float up = 1.0f;
+    v4u stage_k[kLoads], stage_v[kLoads];
+
+    static __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+    __device__ __forceinline__ Prefill(const PrefillArgs& args, Lds& l) : a(args), lds(l) {}
+
+    // Tiles are numbered by their first key / 64; the t-th that the work group looks at:
+    __device__ __forceinline__ int tile_of(int t) const { return t < sink_tiles ? t : t - sink_tiles + first; }
+    __device__ __forceinline__ int channels() const { return FULL ? DP : dim; }
+
+    // Pages of a tile's four quarters (pages of 64 and more: all the same, and only p0 is kept).
+    struct Pages {
+        int p0, p1, p2, p3;
+    };
+    __device__ __forceinline__ int page_at(int key) const {
+        const int at = key >> a.c.shift;
+        return at < a.c.max_pages ? table[at] : -1;
+    }
+    __device__ __forceinline__ Pages ask_pages(int tile) const {
+        const int key = tile * kTile;
+        Pages p{page_at(key), 0, 0, 0};
+        if (a.c.shift < 6) {
+            p.p1 = page_at(key + 16);
+            p.p2 = page_at(key + 32);
+            p.p3 = page_at(key + 48);
+        }
+        return p;
+    }
+    // A bit for each quarter that has a page; where there is none, page 0 is read and nothing of it used.
+    __device__ __forceinline__ uint32_t settle(Pages& p) const {
+        const int p0 = uniform(p.p0);
+        const bool a0 = page_ok(a.c, p0);
+        p.p0 = a0 ? p0 : 0;
+        if (a.c.shift >= 6) return a0 ? 15u : 0u;
+        const int p1 = uniform(p.p1), p2 = uniform(p.p2), p3 = uniform(p.p3);
+        const bool a1 = page_ok(a.c, p1), a2 = page_ok(a.c, p2), a3 = page_ok(a.c, p3);
+        p.p1 = a1 ? p1 : 0;
+        p.p2 = a2 ? p2 : 0;
+        p.p3 = a3 ? p3 : 0;
+        return (a0 ? 1u : 0u) | (a1 ? 2u : 0u) | (a2 ? 4u : 0u) | (a3 ? 8u : 0u);
+    }
+    static __device__ __forceinline__ int of_quarter(int quarter, int p0, int p1, int p2, int p3) {
+        return quarter & 2 ? (quarter & 1 ? p3 : p2) : (quarter & 1 ? p1 : p0);
+    }
+    // Which eight keys of a tile word w of its values belongs to: w / dim.
+    __device__ __forceinline__ int eight_of(int w) const {
+        if constexpr (FULL) return w / DP;
+        else return (w * dim_magic) >> 20;                // exact: w < 8 dim <= 2048
+    }
+
+    static __device__ __forceinline__ v4u load16(const void* base, uint32_t offset) {
+        return *reinterpret_cast<const v4u*>(static_cast<const uint8_t*>(base) + offset);
+    }
+    // A tile's words on their way to registers: word tid + i threads of the keys (chunk-major: a wave reads 64 keys of a chunk)
+    // and of the values.  In pages of 64 and more a tile is one run of either but for the keys' chunks, and a thread's place in
+    // it never changes.
+    static constexpr bool kEven = FULL && kWords % kThreads == 0;
+    __device__ __forceinline__ void load_keys(int tile, const Pages p) {
+        const KvCache& c = a.c;
+        const int key = tile * kTile, chunk0 = uniform(tid / kTile), at = tid & 63;
+        const uint16_t* kp = c.shift >= 6 ? kbase + (int64_t)p.p0 * c.k_page + (chunk0 * ps + (key & (ps - 1))) * 8 : nullptr;
+        if (c.shift >= 6) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                v4u x = {0u, 0u, 0u, 0u};
+                if (kEven || chunk0 + i * WAVES < c.chunks) x = load16(kp + i * WAVES * ps * 8, (uint32_t)at * 16);
+                stage_k[i] = x;
+            }
+        } else {
+            kp = kbase + (int64_t)of_quarter(at >> 4, p.p0, p.p1, p.p2, p.p3) * c.k_page + (chunk0 * ps + ((key + at) & (ps - 1))) * 8;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                v4u x = {0u, 0u, 0u, 0u};
+                if (kEven || chunk0 + i * WAVES < c.chunks) x = load16(kp + i * WAVES * ps * 8, 0);
+                stage_k[i] = x;
+            }
+        }
+    }
+    __device__ __forceinline__ void load_values(int tile, const Pages p) {
+        const KvCache& c = a.c;
+        const int key = tile * kTile;
+        if (c.shift >= 6) {
+            const uint16_t* vp = vbase + (int64_t)p.p0 * c.v_page + (key & (ps - 1)) * channels();
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                v4u x = {0u, 0u, 0u, 0u};
+                if (kEven || tid + i * kThreads < (kTile / 8) * channels()) x = load16(vp + i * kThreads * 8, (uint32_t)tid * 16);
+                stage_v[i] = x;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int w = tid + i * kThreads, eight = eight_of(w), d = w - eight * channels();
+                const int page = of_quarter((eight >> 1) & 3, p.p0, p.p1, p.p2, p.p3);
+                v4u x = {0u, 0u, 0u, 0u};
+                if (kEven || w < (kTile / 8) * channels())
+                    x = load16(vbase + (int64_t)page * c.v_page + ((key + 8 * eight) & (ps - 1)) * channels(), (uint32_t)d * 16);
+                stage_v[i] = x;
+            }
+        }
+    }
+    // Into LDS.  Values of keys that the cache does not hold become zeros: whatever lies there must not meet a weight of 0 in
+    // the product.
+    __device__ __forceinline__ void store_keys(int buf) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) lds.k[buf][tid + i * kThreads] = __builtin_bit_cast(uint4, stage_k[i]);
+    }
+    __device__ __forceinline__ void store_values(int buf, int tile, uint32_t there) {
+        if (there != 15 || tile < group_first || tile > group_last) {
+            uint32_t odd = 0;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int eight = eight_of(tid + i * kThreads);
+                int held = len - (tile * kTile + 8 * eight);
+                held = (there >> ((eight >> 1) & 3)) & 1 ? held : 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    stage_v[i][e] &= (held > 2 * e ? 0x0000FFFFu : 0u) | (held > 2 * e + 1 ? 0xFFFF0000u : 0u);
+                    odd |= not_finite<T>(stage_v[i][e]);
+                }
+            }
+            if (odd) lds.odd = 1;
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int w = tid + i * kThreads;
+            if (kEven || w < (kTile / 8) * channels()) lds.v[buf][w] = __builtin_bit_cast(uint4, stage_v[i]);
+        }
+    }
+
+    // Does this wave see anything of the tile?  And every column all of it?
+    __device__ __forceinline__ bool sees(int tile) const {
+        return (tile >= wave_first || tile < sink_end) && tile <= wave_last;
+    }
+    __device__ __forceinline__ bool sees_all(int tile, uint32_t there) const {
+        return there == 15 && tile >= open_first && tile <= open_last;
+    }
+    // Which of the eight keys from `base` on this column sees, a bit each.
+    static __device__ __forceinline__ uint32_t first_bits(int n) { return (1u << (n < 0 ? 0 : n > 8 ? 8 : n)) - 1u; }
+    __device__ __forceinline__ uint32_t visible(int base, int p, int low, uint32_t there, int quarter) const {
+        const uint32_t seen = first_bits(p + 1 - base) & (~first_bits(low + 1 - base) | first_bits(a.n_sink - base));
+        return (there >> quarter) & 1 ? seen : 0u;
+    }
+
+    // Scores of 64 keys: s[block][i] is key 32 block + 16 (i / 8) + 8 half + i % 8 against this lane's column.
+    __device__ __forceinline__ void scores(int buf, const v4u (&qf)[kQParts][kSteps], v16f (&s)[2]) const {
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[blk][i] = 0.0f;
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) {
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk) {
+                const v4u kf = __builtin_bit_cast(v4u, lds.k[buf][(2 * st + half) * kTile + 32 * blk + key_row]);
+#pragma unroll
+                for (int p = 0; p < kQParts; ++p) s[blk] = Elem<T>::mfma32(kf, qf[p][st], s[blk]);
+            }
+        }
+    }
+    // The order of the scores' instructions: kAhead words of the keys on their way (by itself the compiler keeps two).
+    static __device__ __forceinline__ void order_scores() {
+        __builtin_amdgcn_sched_group_barrier(kSchedLds, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * kSteps; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, kQParts, 0);
+            if (i < 2 * kSteps - kAhead) __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
+        }
+    }
+
+    __device__ __forceinline__ void mask(int key, uint32_t there, v16f (&s)[2]) const {
+#pragma unroll
+        for (int quarter = 0; quarter < 4; ++quarter) {
+            const int seen = (int)visible(key + 16 * quarter + 8 * half, pos, low, there, quarter);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int keep = (seen << (31 - e)) >> 31, i = 8 * (quarter & 1) + e;
+                const float x = s[quarter >> 1][i];
+                s[quarter >> 1][i] = __int_as_float((__float_as_int(x) & keep) | (__float_as_int(kNegInf) & ~keep));
+            }
+        }
+    }
+
+    // The reference m of the weights (of the scaled scores) and the running sum; s becomes the weights exp2(s - m).  m moves
+    // only where the maximum has grown by more than kSlack: what is there then needs no factor in most tiles, and a weight of
+    // up to 2^kSlack loses nothing.  Returns the factor.
+    static constexpr float kSlack = 8.0f;
+    static constexpr float kLiftLow = T == kF16 ? 6.0f : 0.0f;   // 2^(kSlack + lift) stays in the type's range
+    __device__ __forceinline__ float softmax(v16f (&s)[2], float gain, float& m, float& l) const {
+        float top = kNegInf;
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(top, s[blk][i]), s[blk][i + 1]);
+        top = max_xor32(top) * gain;
+        float alpha = 1.0f;
+        if (__any(top > m + kSlack)) {
+            const float m_new = top > m + kSlack ? top : m;
+            alpha = m_new == m ? 1.0f : exp2_fast(m - m_new);
+            m = m_new;
+            l *= alpha;
+        }
+        const float base = kLiftLow - (m == kNegInf ? 0.0f : m);
+        float sum = 0.0f;
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[blk][i] = exp2_fast(__builtin_fmaf(s[blk][i], gain, base));
+                if constexpr (kPParts > 1) sum += s[blk][i];
+            }
+        if constexpr (kPParts > 1) l += sum;
+        return alpha;
+    }
+
+    // Operands of the second product: the weights of 16 keys (quarter) in parts.  Rounded weights are summed as rounded: the
+    // sum then belongs to the product it divides, and takes half the instructions.
+    __device__ __forceinline__ void weights(const v16f (&s)[2], int quarter, v4u (&pf)[kPParts], float& l) const {
+        const int blk = quarter >> 1, i0 = 8 * (quarter & 1);
+        if constexpr (kPParts == 1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                pf[0][e] = Elem<T>::pack(s[blk][i0 + 2 * e], s[blk][i0 + 2 * e + 1]);
+                l = Elem<T>::add2(pf[0][e], l);
+            }
+        } else {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = s[blk][i0 + e];
+#pragma unroll
+            for (int p = 0; p < kPParts; ++p)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pf[p][e] = Elem<T>::part(x[2 * e], x[2 * e + 1]);
+        }
+    }
+
+    // Scores, softmax and product of every tile, the next tile's words on their way.
+    __device__ __forceinline__ void all_tiles(const v4u (&qf)[kQParts][kSteps], float gain, float& m, float& l, v16f (&o)[kBlocks]) {
+        Pages pages{};                                    // of the tile after the one being loaded
+        uint32_t there = 0;
+        if (n_tiles > 0) {
+            pages = ask_pages(tile_of(0));
+            there = settle(pages);
+            load_keys(tile_of(0), pages);
+            load_values(tile_of(0), pages);
+            if (n_tiles > 1) pages = ask_pages(tile_of(1));
+        }
+        __syncthreads();
+        if (n_tiles > 0) {
+            store_keys(0);
+            store_values(0, tile_of(0), there);
+        }
+        __syncthreads();
+        for (int t = 0; t < n_tiles; ++t) {
+            const int tile = tile_of(t), buf = t & 1;
+            const uint32_t now = there;
+            if (t + 1 < n_tiles) {
+                there = settle(pages);
+                load_keys(tile_of(t + 1), pages);
+                load_values(tile_of(t + 1), pages);
+                if (t + 2 < n_tiles) pages = ask_pages(tile_of(t + 2));
+            }
+            if (sees(tile)) {
+                v16f s[2];
+                scores(buf, qf, s);
+                order_scores();
+                if (!sees_all(tile, now)) mask(tile * kTile, now, s);
+                const float alpha = softmax(s, gain, m, l);
+                if (__any(alpha != 1.0f)) {
+#pragma unroll
+                    for (int d = 0; d < kBlocks; ++d) o[d] *= alpha;
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    v4u pf[kPParts];
+                    weights(s, q, pf, l);
+#pragma unroll
+                    for (int d = 0; d < kBlocks; ++d) {
+                        const v4u vf = __builtin_bit_cast(v4u, lds.v[buf][(2 * q + half) * channels() + 32 * d + n]);
+#pragma unroll
+                        for (int p = 0; p < kPParts; ++p) o[d] = Elem<T>::mfma32(vf, pf[p], o[d]);
+                    }
+                }
+            }
+            if (t + 1 < n_tiles) {
+                store_keys(buf ^ 1);
+                store_values(buf ^ 1, tile_of(t + 1), there);
+            }
+            __syncthreads();
+        }
+    }
+
+    // All tiles once more, twice for every block of 32 channels: first the values that are not finite, counted as the marks of
+    // each kind that a column sees (see mark_half), then the product without them.
+    __device__ __forceinline__ void careful(const v4u (&qf)[kQParts][kSteps], float gain, bool used, int64_t row) {
+        constexpr uint32_t one = T == kBf16 ? 0x3F80u : 0x3C00u;
+        for (int d = 0; 32 * d < channels(); ++d) {
+            float m = kNegInf, l = 0.0f;
+            v16f o, odd;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = odd[i] = 0.0f;
+            for (int turn = 0; turn < 2 * n_tiles; ++turn) {
+                const int t = turn < n_tiles ? turn : turn - n_tiles, tile = tile_of(t), key = tile * kTile;
+                __syncthreads();
+                Pages p = ask_pages(tile);
+                const uint32_t there = settle(p);
+                load_keys(tile, p);
+                load_values(tile, p);
+                store_keys(0);
+                store_values(0, tile, there);
+                __syncthreads();
+                if (!sees(tile)) continue;
+                if (turn < n_tiles) {
+                    v16f marks;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) marks[i] = 0.0f;
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t bits = visible(key + 16 * q + 8 * half, pos, low, there, q);
+                        const v4u vf = __builtin_bit_cast(v4u, lds.v[0][(2 * q + half) * channels() + 32 * d + n]);
+                        v4u mark, seen;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            mark[e] = mark_half<T>(vf[e] & 0xFFFFu) | mark_half<T>(vf[e] >> 16) << 16;
+                            seen[e] = ((bits >> (2 * e)) & 1 ? one : 0u) | ((bits >> (2 * e)) & 2 ? one << 16 : 0u);
+                        }
+                        marks = Elem<T>::mfma32(mark, seen, marks);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) odd[i] += unmark(marks[i]);
+                } else {
+                    v16f s[2];
+                    scores(0, qf, s);
+                    if (!sees_all(tile, there)) mask(key, there, s);
+                    o *= softmax(s, gain, m, l);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        v4u pf[kPParts];
+                        weights(s, q, pf, l);
+                        v4u vf = __builtin_bit_cast(v4u, lds.v[0][(2 * q + half) * channels() + 32 * d + n]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) vf[e] &= ~not_finite<T>(vf[e]);
+#pragma unroll
+                        for (int p = 0; p < kPParts; ++p) o = Elem<T>::mfma32(vf, pf[p], o);
+                        __builtin_amdgcn_sched_barrier(0);   // one quarter's registers at a time
+                    }
+                }
+            }
+            l = sum_xor32(l);
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            if (!used) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = 32 * d + 8 * i + 4 * half;
+                if (FULL || at < dim)
+                    store4<T, F32>(a.out, row + at, o[4 * i] * inv + odd[4 * i], o[4 * i + 1] * inv + odd[4 * i + 1],
+                                   o[4 * i + 2] * inv + odd[4 * i + 2], o[4 * i + 3] * inv + odd[4 * i + 3]);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void run() {
+        const KvCache& c = a.c;
+        tid = threadIdx.x;
+        const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        half = lane >> 5;
+        n = lane & 31;
+        dim = c.dim;
+        ps = 1 << c.shift;
+        dim_magic = ((1 << 20) + dim - 1) / dim;
+        // key of a row of a 32-key block: the order in which a lane's 16 scores are its operand words of the second product
+        key_row = (n & 16) | ((n & 4) << 1) | ((n & 8) >> 1) | (n & 3);
+
+        // work groups of one kv head follow each other at a distance of kv_heads (with 8 of them: on one XCD, whose L2 keeps
+        // the head's keys), the last tiles, which have the most keys before them, first
+        kvh = blockIdx.x % c.kv_heads;
+        const int id = a.tiles - 1 - (int)(blockIdx.x / c.kv_heads);
+        b = find_last(c.n_seqs, id, [&](int i) { return first_tile(a.q_start, i, a.group, kColumns); });
+        b = uniform(b);
+        Span span = span_of(a.q_start, b, a.n_tokens);
+        span = {uniform(span.first), uniform(span.count)};
+        const int col0 = (id - uniform(first_tile(a.q_start, b, a.group, kColumns))) * kColumns;
+        const int columns = span.count * a.group;
+        if (col0 >= columns) return;
+        len = uniform(seq_len(c, b));
+        const int p0 = len - span.count;                  // position of the first token (below 0: it sees nothing)
+        table = c.table + (int64_t)b * c.max_pages;
+        kbase = c.k + (int64_t)kvh * c.chunks * ps * 8;
+        vbase = c.v + (int64_t)kvh * dim * ps;
+
+        const int col = col0 + wave * 32 + n;
+        const bool used = col < columns;
+        const int token = (used ? col : columns - 1) / a.group, in_group = (used ? col : columns - 1) - token * a.group;
+        pos = p0 + token;
+        low = a.window > 0 ? pos - a.window : -1;
+        const int64_t row = ((int64_t)(span.first + token) * a.heads + kvh * a.group + in_group) * dim;
+
+        // The tiles of the work group: those of the sinks, then from the window's first to the last position's.  Positions of
+        // its and of this wave's columns (an unused wave sees nothing):
+        const int last_col = (col0 + kColumns < columns ? col0 + kColumns : columns) - 1;
+        const int pos_lo = p0 + col0 / a.group, pos_hi = p0 + last_col / a.group;
+        const int wcol0 = col0 + wave * 32, wcol1 = wcol0 + 31 < columns ? wcol0 + 31 : columns - 1;
+        const int wpos_lo = p0 + wcol0 / a.group, wpos_hi = wcol0 < columns ? p0 + wcol1 / a.group : -1;
+        auto behind = [&](int p) { return a.window > 0 && p >= a.window ? p - a.window + 1 : 0; };   // first key in the window
+        const int lo = behind(pos_lo), sinks = a.n_sink < lo ? a.n_sink : lo;
+        first = lo / kTile;
+        sink_tiles = (sinks + kTile - 1) / kTile;
+        sink_tiles = sink_tiles < first ? sink_tiles : first;
+        n_tiles = pos_hi < 0 ? 0 : sink_tiles + pos_hi / kTile + 1 - first;
+        sink_end = (a.n_sink + kTile - 1) / kTile;
+        wave_first = uniform(behind(wpos_lo) / kTile);
+        wave_last = uniform(wpos_hi < 0 ? -1 : wpos_hi / kTile);
+        open_first = uniform((behind(wpos_hi) + kTile - 1) / kTile);
+        open_last = uniform((wpos_lo + 1) / kTile - 1);
+        group_first = (behind(pos_hi) + kTile - 1) / kTile;
+        group_last = (pos_lo + 1) / kTile - 1;
+
+        if (tid == 0) lds.odd = 0;
+        // q as operands: chunk 2 s + half of this lane's column, in parts.  The factor of the scores is positive (a negative
+        // scale changes q's sign, a scale of 0 makes q 0), so that it can be applied after the maximum.
+        v4u qf[kQParts][kSteps];
+        float gain = fabsf(a.scale2), up = a.scale2 < 0.0f ? -1.0f : a.scale2 == 0.0f ? 0.0f : 1.0f;
         if constexpr (F32 && T == kF16) {
             float top = 0.0f;
             for (int d = 4 * half; d < dim; d += 8) {
                 const float4 x = load4<T, F32>(a.q, row + d);
                 top = fmaxf(top, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(x.z), fabsf(x.w))));
             }
-            up = row_gain(max_xor32(top));
-            gain = a.scale2 / up;
+            const float g = row_gain(max_xor32(top));
+            up *= g;
+            gain /= g;
         }
+        if (a.scale2 == 0.0f) gain = 1.0f;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             const int d = 8 * (2 * s + half);
             float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f), y = x;
-            if (full || d < dim) x = load4<T, F32>(a.q, row + d);
-            if (full || d + 4 < dim) y = load4<T, F32>(a.q, row + d + 4);
+            if (FULL || d < dim) x = load4<T, F32>(a.q, row + d);
+            if (FULL || d + 4 < dim) y = load4<T, F32>(a.q, row + d + 4);
+            x.x *= up; x.y *= up; x.z *= up; x.w *= up;
+            y.x *= up; y.y *= up; y.z *= up; y.w *= up;
             if constexpr (kQParts == 1) {
                 qf[0][s] = v4u{Elem<T>::pack(x.x, x.y), Elem<T>::pack(x.z, x.w), Elem<T>::pack(y.x, y.y),
                                Elem<T>::pack(y.z, y.w)};
             } else {
-                if constexpr (T == kF16) {
-                    x.x *= up; x.y *= up; x.z *= up; x.w *= up;
-                    y.x *= up; y.y *= up; y.z *= up; y.w *= up;
-                }
 #pragma unroll
                 for (int p = 0; p < kQParts; ++p)
                     qf[p][s] = v4u{Elem<T>::part(x.x, x.y), Elem<T>::part(x.z, x.w), Elem<T>::part(y.x, y.y),
                                    Elem<T>::part(y.z, y.w)};
             }
         }
-    }
 
-    // Positions of the work group's and of this wave's columns, and the tiles they see: those of the sinks, then from the
-    // window's first to the last position's.
-    const int last_col = (col0 + kColumns < columns ? col0 + kColumns : columns) - 1;
-    const int pos_lo = p0 + col0 / a.group, pos_hi = p0 + last_col / a.group;
-    const int wcol0 = col0 + wave * 32, wcol1 = wcol0 + 31 < columns ? wcol0 + 31 : columns - 1;
-    const bool wave_used = wcol0 < columns;
-    const int wpos_lo = p0 + (wave_used ? wcol0 : columns - 1) / a.group, wpos_hi = p0 + (wave_used ? wcol1 : columns - 1) / a.group;
-    const int lo = a.window > 0 && pos_lo >= a.window ? pos_lo - a.window + 1 : 0;
-    const int sinks = a.n_sink < lo ? a.n_sink : lo;
-    const int first = lo / kTile;
-    int sink_tiles = (sinks + kTile - 1) / kTile;
-    sink_tiles = sink_tiles < first ? sink_tiles : first;
-    const int n_tiles = pos_hi < 0 ? 0 : sink_tiles + pos_hi / kTile + 1 - first;
-    auto tile_key = [&](int t) { return (t < sink_tiles ? t : t - sink_tiles + first) * kTile; };
-
-    const int32_t* table = c.table + (int64_t)b * c.max_pages;
-    const int chunks = c.chunks;
-    const int k_words = chunks * kTile, v_words = dim * (kTile / 8);
-    const int64_t k_head = (int64_t)kvh * chunks * ps * 8, v_head = (int64_t)kvh * dim * ps;
-    const int steps = (chunks + 1) / 2;
-
-    // pages of the four quarters of a tile (-1 where there is none)
-    int pages[4];
-    auto load_pages = [&](int key) {
+        float m = kNegInf, l = 0.0f;
+        v16f o[kBlocks];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = (key + 16 * i) >> c.shift;
-            const int page = at < c.max_pages ? table[at] : -1;
-            pages[i] = page_ok(c, page) ? page : -1;
+        for (int t = 0; t < kBlocks; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+
+        all_tiles(qf, gain, m, l, o);
+        if (uniform(lds.odd)) {
+            careful(qf, gain, used, row);
+            return;
         }
-    };
-    auto page_of = [&](int quarter) {
-        const int x = quarter == 0 ? pages[0] : quarter == 1 ? pages[1] : quarter == 2 ? pages[2] : pages[3];
-        return x < 0 ? 0 : x;
-    };
-    v4u stage_k[kLoads], stage_v[kLoads];
-    auto load_tile = [&](int key) {
+        l = sum_xor32(l);
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;    // l is 0 where nothing was visible
+        if (!used) return;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int w = tid + i * kThreads;
-            const int at = w & (kTile - 1), chunk = w / kTile;
-            v4u x = {0u, 0u, 0u, 0u};
-            if (full || w < k_words)
-                x = *reinterpret_cast<const v4u*>(c.k + (int64_t)page_of(at >> 4) * c.k_page + k_head +
-                                                  (int64_t)(chunk * ps + ((key + at) & (ps - 1))) * 8);
-            stage_k[i] = x;
-        }
+        for (int d = 0; d < kBlocks; ++d) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int w = tid + i * kThreads;
-            const int eight = full ? w / DP : w / dim, d = w - eight * dim;
-            v4u x = {0u, 0u, 0u, 0u};
-            if (full || w < v_words)
-                x = *reinterpret_cast<const v4u*>(c.v + (int64_t)page_of((eight >> 1) & 3) * c.v_page + v_head +
-                                                  (int64_t)((key + 8 * eight) & (ps - 1)) * dim + d * 8);
-            stage_v[i] = x;
-        }
-    };
-    // there: whether the four quarters have pages.  Values of keys that the cache does not hold become zeros: whatever lies
-    // there must not meet a weight of 0 in the product.
-    auto store_tile = [&](int buf, int t, uint32_t there) {
-        const int key = tile_key(t);
-        // does every query of the work group see every key?
-        const bool open = there == 15 && key + kTile - 1 <= pos_lo &&
-                          (a.window <= 0 || key > pos_hi - a.window || key + kTile <= a.n_sink);
-        uint32_t odd = 0;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) kt[buf][tid + i * kThreads] = __builtin_bit_cast(uint4, stage_k[i]);
-        const bool whole = there == 15 && key + kTile <= len;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int w = tid + i * kThreads;
-            v4u x = stage_v[i];
-            if (!whole) {
-                const int eight = full ? w / DP : w / dim;
-                int held = len - (key + 8 * eight);
-                held = (there >> ((eight >> 1) & 3)) & 1 ? held : 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    x[e] &= (held > 2 * e ? 0x0000FFFFu : 0u) | (held > 2 * e + 1 ? 0xFFFF0000u : 0u);
+            for (int i = 0; i < 4; ++i) {
+                const int at = 32 * d + 8 * i + 4 * half;
+                if (FULL || at < dim)
+                    store4<T, F32>(a.out, row + at, o[d][4 * i] * inv, o[d][4 * i + 1] * inv, o[d][4 * i + 2] * inv,
+                                   o[d][4 * i + 3] * inv);
             }
-            if (!open) odd |= not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
-            if (full || w < v_words) vt[buf][w] = __builtin_bit_cast(uint4, x);
-        }
-        if (odd) odd_tile[buf] = t;
-    };
-    auto there_of = [&]() {
-        return (pages[0] >= 0 ? 1u : 0u) | (pages[1] >= 0 ? 2u : 0u) | (pages[2] >= 0 ? 4u : 0u) | (pages[3] >= 0 ? 8u : 0u);
-    };
-
-    float m = kNegInf, l = 0.0f;
-    v16f o[kBlocks];
-#pragma unroll
-    for (int t = 0; t < kBlocks; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
-
-    // key of a row of a 32-key block: the order in which a lane's 16 scores are its operand words of the second product
-    const int key_row = (n & 16) | ((n & 4) << 1) | ((n & 8) >> 1) | (n & 3);
-
-    uint32_t there = 0;
-    if (tid < 2) odd_tile[tid] = -1;
-    __syncthreads();
-    if (n_tiles > 0) {
-        load_pages(tile_key(0));
-        there = there_of();
-        load_tile(tile_key(0));
-        store_tile(0, 0, there);
-    }
-    __syncthreads();
-    for (int t = 0; t < n_tiles; ++t) {
-        const int key = tile_key(t), buf = t & 1;
-        const uint32_t now = there;
-        if (t + 1 < n_tiles) {
-            load_pages(tile_key(t + 1));
-            there = there_of();
-            load_tile(tile_key(t + 1));
-        }
-        // does this wave see anything of the tile, and all of it?
-        const bool near = key <= wpos_hi && (a.window <= 0 || key + kTile - 1 > wpos_lo - a.window);
-        const bool sink = a.window > 0 && key < a.n_sink && key <= wpos_hi;
-        if (wave_used && (near || sink)) {
-            v16f s[2];
-#pragma unroll
-            for (int blk = 0; blk < 2; ++blk) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[blk][i] = 0.0f;
-            }
-#pragma unroll
-            for (int st = 0; st < kSteps; ++st) {
-                if (!full && st >= steps) continue;
-#pragma unroll
-                for (int blk = 0; blk < 2; ++blk) {
-                    const v4u kf = __builtin_bit_cast(v4u, kt[buf][(2 * st + half) * kTile + 32 * blk + key_row]);
-#pragma unroll
-                    for (int p = 0; p < kQParts; ++p) s[blk] = Elem<T>::mfma32(kf, qf[p][st], s[blk]);
-                }
-            }
-            const bool whole = now == 15 && key + kTile - 1 <= wpos_lo &&
-                               (a.window <= 0 || key > wpos_hi - a.window || key + kTile <= a.n_sink);
-            float top = kNegInf;
-#pragma unroll
-            for (int blk = 0; blk < 2; ++blk) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float x = s[blk][i] * gain;
-                    if (!whole) {
-                        const int quarter = 2 * blk + (i >> 3);
-                        const int j = key + 16 * quarter + 8 * half + (i & 7);
-                        const bool in = ((now >> quarter) & 1) && j <= pos && (a.window <= 0 || j > pos - a.window || j < a.n_sink);
-                        x = in ? x : kNegInf;
-                    }
-                    s[blk][i] = x;
-                    top = fmaxf(top, x);
-                }
-            }
-            top = max_xor32(top);
-            const float m_new = fmaxf(m, top);
-            if (__any(m_new > m)) {
-                const float alpha = m_new == kNegInf ? 1.0f : exp2_fast(m - m_new);
-                l *= alpha;
-#pragma unroll
-                for (int d = 0; d < kBlocks; ++d) o[d] *= alpha;
-                m = m_new;
-            }
-            const float base = (m == kNegInf ? 0.0f : m) - kLift<T>;
-            float sum = 0.0f;
-#pragma unroll
-            for (int blk = 0; blk < 2; ++blk) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[blk][i] = exp2_fast(s[blk][i] - base);
-                    sum += s[blk][i];
-                }
-            }
-            l += sum;
-            const bool odd = !whole && odd_tile[buf] == t;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {                 // 16 keys
-                const int blk = q >> 1, i0 = 8 * (q & 1);
-                v4u pf[kPParts];
-                if constexpr (kPParts == 1) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) pf[0][e] = Elem<T>::pack(s[blk][i0 + 2 * e], s[blk][i0 + 2 * e + 1]);
-                } else {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = s[blk][i0 + e];
-#pragma unroll
-                    for (int p = 0; p < kPParts; ++p)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) pf[p][e] = Elem<T>::part(x[2 * e], x[2 * e + 1]);
-                }
-#pragma unroll
-                for (int d = 0; d < kBlocks; ++d) {
-                    if (!full && 32 * d >= dim) continue;
-                    v4u vf = __builtin_bit_cast(v4u, vt[buf][(2 * q + half) * dim + 32 * d + n]);
-                    if (odd) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) vf[e] &= ~not_finite<T>(vf[e]);
-                    }
-#pragma unroll
-                    for (int p = 0; p < kPParts; ++p) o[d] = Elem<T>::mfma32(vf, pf[p], o[d]);
-                }
-            }
-            if (odd) {
-                constexpr uint32_t one = T == kBf16 ? 0x3F80u : 0x3C00u;
-                for (int d = 0; d < kBlocks; ++d) {
-                    if (!full && 32 * d >= dim) continue;
-                    v16f count;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) count[i] = 0.0f;
-                    for (int q = 0; q < 4; ++q) {
-                        const uint4 w = vt[buf][(2 * q + half) * dim + 32 * d + n];
-                        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-                        v4u mark, seen;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            mark[e] = mark_half<T>(x[e] & 0xFFFFu) | mark_half<T>(x[e] >> 16) << 16;
-                            seen[e] = 0;
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const int j = key + 16 * q + 8 * half + 2 * e + h;
-                                const bool in = ((now >> q) & 1) && j <= pos && (a.window <= 0 || j > pos - a.window || j < a.n_sink);
-                                seen[e] |= in ? one << (16 * h) : 0u;
-                            }
-                        }
-                        count = Elem<T>::mfma32(mark, seen, count);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float x = unmark(count[i]);
-#pragma unroll
-                        for (int k = 0; k < kBlocks; ++k) o[k][i] += k == d ? x : 0.0f;
-                    }
-                }
-            }
-        }
-        if (t + 1 < n_tiles) store_tile(buf ^ 1, t + 1, there);
-        __syncthreads();
-    }
-
-    l = sum_xor32(l);
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;        // l is 0 where nothing was visible
-    if (!used) return;
-#pragma unroll
-    for (int d = 0; d < kBlocks; ++d) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = 32 * d + 8 * i + 4 * half;
-            if (full || at < dim)
-                store4<T, F32>(a.out, row + at, o[d][4 * i] * inv, o[d][4 * i + 1] * inv, o[d][4 * i + 2] * inv,
-                               o[d][4 * i + 3] * inv);
         }
     }
+};
+
+template <int T, int DP, bool F32, int WAVES, int PER_SIMD, bool FULL>
+__global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attn_prefill_kernel(PrefillArgs a) {
+    using P = Prefill<T, DP, F32, WAVES, FULL>;
+    __shared__ typename P::Lds lds;
+    P(a, lds).run();
 }
 
-template <int T, int DP, bool F32, int WAVES>
+template <int T, int DP, bool F32, int WAVES, int PER_SIMD>
 hipError_t launch(PrefillArgs a, hipStream_t s) {
     a.tiles = (int)((int64_t)a.n_tokens * a.group / (32 * WAVES)) + a.c.n_seqs;
-    hipLaunchKernelGGL((attn_prefill_kernel<T, DP, F32, WAVES>), dim3((unsigned)a.tiles * (unsigned)a.c.kv_heads),
-                       dim3(64 * WAVES), 0, s, a);
+    const dim3 grid((unsigned)a.tiles * (unsigned)a.c.kv_heads), block(64 * WAVES);
+    if (DP != 112 && a.c.dim == DP)
+        hipLaunchKernelGGL((attn_prefill_kernel<T, DP, F32, WAVES, PER_SIMD, DP != 112>), grid, block, 0, s, a);
+    else
+        hipLaunchKernelGGL((attn_prefill_kernel<T, DP, F32, WAVES, PER_SIMD, false>), grid, block, 0, s, a);
     return hipGetLastError();
+}
+
+// Two waves a SIMD (256 registers each) cover each other's waits and softmax: work groups of 8 waves, whose tiles are read once
+// for 256 columns, where those fill the CUs, else of 4.  Three parts of q need more registers: one wave a SIMD.
+template <int T, bool F32, int DP>
+hipError_t launch_waves(const PrefillArgs& a, hipStream_t s) {
+    if constexpr (F32 && T == kBf16) {
+        return launch<T, DP, F32, 4, 1>(a, s);
+    } else {
+        const int64_t groups = ((int64_t)a.n_tokens * a.group / 256 + a.c.n_seqs) * a.c.kv_heads;
+        if (groups >= device_cus()) return launch<T, DP, F32, 8, 2>(a, s);
+        return launch<T, DP, F32, 4, F32 ? 1 : 2>(a, s);
+    }
 }
 
 template <int T, bool F32>
 hipError_t launch_dim(const PrefillArgs& a, hipStream_t s) {
-    if (a.c.dim <= 64) return launch<T, 64, F32, 4>(a, s);
-    if (a.c.dim <= 128) return launch<T, 128, F32, 4>(a, s);
-    return launch<T, 256, F32, 4>(a, s);
+    if (a.c.dim <= 64) return launch<T, 64, F32, 4, 2>(a, s);
+    if (a.c.dim <= 96) return launch_waves<T, F32, 96>(a, s);
+    if (a.c.dim <= 112) return launch_waves<T, F32, 112>(a, s);
+    if (a.c.dim <= 128) return launch_waves<T, F32, 128>(a, s);
+    return launch<T, 256, F32, 4, 1>(a, s);
 }
 
 }  // namespace

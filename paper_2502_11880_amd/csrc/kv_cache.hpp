@@ -15,6 +15,9 @@ namespace bitnet {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -108,7 +111,11 @@ struct Elem<kBf16> {
     }
     static __device__ __forceinline__ float to(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
     static __device__ __forceinline__ uint32_t pack(float a, float b) {   // rounded to nearest even
-        return (uint32_t)from(a) | (uint32_t)from(b) << 16;
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{a, b}), bf16x2));
+    }
+    // sum + both values of a word
+    static __device__ __forceinline__ float add2(uint32_t w, float sum) {
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
     }
     // the leading part of two values, which lose it
     static __device__ __forceinline__ uint32_t part(float& a, float& b) {
@@ -135,6 +142,9 @@ struct Elem<kF16> {
     static __device__ __forceinline__ float to(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
     static __device__ __forceinline__ uint32_t pack(float a, float b) {
         return (uint32_t)from(a) | (uint32_t)from(b) << 16;
+    }
+    static __device__ __forceinline__ float add2(uint32_t w, float sum) {
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), __builtin_bit_cast(f16x2, 0x3C003C00u), sum, false);
     }
     static __device__ __forceinline__ uint32_t part(float& a, float& b) {
         const uint16_t x = from(a), y = from(b);
