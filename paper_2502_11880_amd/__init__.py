@@ -8,6 +8,7 @@ kernels of ``libbitnet_mi355x.so``; if that library has not been built, every ca
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 
@@ -102,6 +103,8 @@ class BitnetError(RuntimeError):
 def lib():
     """The loaded C library (loads it on first use; raises if it is not built)."""
     global _handle
+    if _handle is not None:
+        return _handle
     with _lock:
         if _handle is None:
             if not os.path.exists(LIB_PATH):
@@ -140,10 +143,20 @@ def _ptr(t, name, dtype=None, device=True):
     return t.data_ptr()
 
 
+@functools.lru_cache(maxsize=None)
+def _current_stream():
+    """A call that returns the current stream's handle (building a torch.cuda.Stream for it takes 2.7 us, a third of a call)."""
+    import torch
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is None or device is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    torch.cuda.init()
+    return lambda: raw(device())
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -304,43 +317,46 @@ class _KvTables(ctypes.Structure):         # bitnet_kv_tables
                 ("n_seqs", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("n_pages", ctypes.c_int64)]
 
 
-def _dtype(t, name) -> int:
+@functools.lru_cache(maxsize=None)
+def _types():
+    """(int32, the value of bitnet_dtype of every type it has)."""
     import torch
-    if t.dtype == torch.float32:
-        return BITNET_DTYPE_F32
-    if t.dtype == torch.bfloat16:
-        return BITNET_DTYPE_BF16
-    if t.dtype == torch.float16:
-        return BITNET_DTYPE_F16
-    raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return torch.int32, {torch.float32: BITNET_DTYPE_F32, torch.bfloat16: BITNET_DTYPE_BF16, torch.float16: BITNET_DTYPE_F16}
+
+
+def _dtype(t, name) -> int:
+    d = _types()[1].get(t.dtype)
+    if d is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return d
 
 
 def _cache(k_cache, v_cache, table, kv_len):
     """The C description of one layer's cache, from tensors k_cache [n_pages, Hkv, ceil(D / 8), page_size, 8] and
     v_cache [n_pages, Hkv, page_size / 8, D, 8] (bfloat16 or float16), table int32 [n_seqs, max_pages] and kv_len int32
     [n_seqs]."""
-    import torch
-    if k_cache.dim() != 5 or v_cache.dim() != 5 or table.dim() != 2:
+    ks, vs, ts = k_cache.shape, v_cache.shape, table.shape
+    if len(ks) != 5 or len(vs) != 5 or len(ts) != 2:
         raise ValueError("k_cache and v_cache must have 5 dimensions and table 2")
-    pages, heads, chunks, ps, eight = k_cache.shape
-    dim = v_cache.shape[3]
-    if eight != 8 or chunks != -(-dim // 8) or v_cache.shape != (pages, heads, ps // 8, dim, 8):
-        raise ValueError(f"k_cache {tuple(k_cache.shape)} and v_cache {tuple(v_cache.shape)} are not "
+    pages, heads, chunks, ps, eight = ks
+    dim = vs[3]
+    if eight != 8 or chunks != -(-dim // 8) or vs != (pages, heads, ps // 8, dim, 8):
+        raise ValueError(f"k_cache {tuple(ks)} and v_cache {tuple(vs)} are not "
                          "[pages, heads, ceil(dim / 8), page_size, 8] and [pages, heads, page_size / 8, dim, 8]")
-    if v_cache.dtype != k_cache.dtype:
+    if v_cache.dtype is not k_cache.dtype:
         raise TypeError(f"v_cache must be {k_cache.dtype}, got {v_cache.dtype}")
-    seqs, width = table.shape
+    seqs, width = ts
     if kv_len.numel() != seqs:
         raise ValueError(f"kv_len must have one entry for each of the {seqs} rows of table, got {kv_len.numel()}")
-    return _KvCache(_ptr(k_cache, "k_cache"), _ptr(v_cache, "v_cache"), _ptr(table, "table", torch.int32),
-                    _ptr(kv_len, "kv_len", torch.int32), pages, seqs, width, ps, heads, dim, _dtype(k_cache, "k_cache"))
+    i32 = _types()[0]
+    return _KvCache(_ptr(k_cache, "k_cache"), _ptr(v_cache, "v_cache"), _ptr(table, "table", i32),
+                    _ptr(kv_len, "kv_len", i32), pages, seqs, width, ps, heads, dim, _dtype(k_cache, "k_cache"))
 
 
 def _q_start(q_start, seqs):
-    import torch
     if q_start.numel() != seqs + 1:
         raise ValueError(f"q_start must have {seqs + 1} entries, got {q_start.numel()}")
-    return _ptr(q_start, "q_start", torch.int32)
+    return _ptr(q_start, "q_start", _types()[0])
 
 
 def _rows(t, name, heads_dim):
@@ -421,18 +437,16 @@ def _pool(k_pool, v_pool):
 
 
 def _tables(table, kv_len, refs):
-    import torch
+    i32 = _types()[0]
     if table.dim() != 2 or (kv_len is not None and kv_len.numel() != table.shape[0]):
         raise ValueError("table must be [n_seqs, max_pages] and kv_len [n_seqs]")
-    return _KvTables(_ptr(table, "table", torch.int32), _ptr(kv_len, "kv_len", torch.int32),
-                     _ptr(refs, "refs", torch.int32), table.shape[0], table.shape[1], refs.numel())
+    return _KvTables(_ptr(table, "table", i32), _ptr(kv_len, "kv_len", i32), _ptr(refs, "refs", i32), table.shape[0], table.shape[1], refs.numel())
 
 
 def _list(t, name, n=None):
-    import torch
     if n is not None and t.numel() != n:
         raise ValueError(f"{name} must have {n} entries, got {t.numel()}")
-    return _ptr(t, name, torch.int32)
+    return _ptr(t, name, _types()[0])
 
 
 def bitnet_kv_workspace_bytes(n_pages: int, n_seqs: int) -> int:

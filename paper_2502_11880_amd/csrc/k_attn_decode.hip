@@ -14,6 +14,8 @@
 // sum, unnormalised output) in the workspace, and a second launch joins them.
 #include "kv_cache.hpp"
 
+#include <type_traits>
+
 namespace bitnet {
 namespace {
 
@@ -23,7 +25,10 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kMaxGroups = 1024;     // work groups of a split launch
 constexpr int kMaxSeqs = 1024;       // sequences of a split launch (more go in several)
 constexpr int kMinShare = 4;         // units of a share, at least: one for each wave
-constexpr int kWholeUnits = 8;       // rows of up to so many units are never split
+constexpr int kWholeUnits = 8;       // rows of up to so many units are never split,
+constexpr int kManyUnits = 64;       // nor rows of up to so many where there are
+constexpr int kManyRows = 512;       // so many of them
+constexpr int kIds = 512;            // units whose pages a work group looks up at a time
 
 // The keys that the last position of a sequence of length L sees: [0, sinks) and [lo, L).
 struct Sight {
@@ -69,7 +74,7 @@ struct Row {
     v4f o[DP / 16];
 };
 
-template <int T, int DP, bool F32>
+template <int T, int DP, bool F32, bool FULL, bool PAGE16>
 struct Decode {
     static constexpr int kQParts = F32 ? Elem<T>::kExactParts : 1;
     static constexpr int kPParts = F32 ? Elem<T>::kExactParts : 2;
@@ -129,101 +134,117 @@ struct Decode {
         }
     }
 
-    // Units u0 .. u1 - 1 of a row, this wave's every fourth, into its state.
-    static __device__ __forceinline__ void run(const DecodeArgs& a, int b, int kvh, const Sight& sight, int u0, int u1,
-                                               const uint4* qs, float gain, Row<DP>& row) {
+    // The pages of units u0 .. u1 - 1 (at most kIds), and, pages of 16, those of their upper halves.  In LDS, so that waiting for a
+    // page number does not wait for the keys and values that are on their way.
+    static __device__ __forceinline__ void stage_ids(const KvCache& c, int b, const Sight& sight, int u0, int u1, int (&ids)[2][kIds]) {
+        const int32_t* table = c.table + (int64_t)b * c.max_pages;
+        for (int i = threadIdx.x; i < u1 - u0; i += kThreads) {
+            const int at = unit_key(sight, u0 + i) >> c.shift;
+            ids[0][i] = table[at];
+            if (PAGE16) ids[1][i] = at + 1 < c.max_pages ? table[at + 1] : -1;
+        }
+    }
+
+    // Units u0 .. u1 - 1 of a row (their pages in ids), this wave's every fourth, into its state.
+    static __device__ __forceinline__ void run(const DecodeArgs& a, int kvh, const Sight& sight, int u0, int u1,
+                                               const int (&ids)[2][kIds], const uint4* qs, float gain, Row<DP>& row) {
         const KvCache& c = a.c;
         const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int ps = 1 << c.shift;
-        const bool full = DP == c.dim;
-        const int32_t* table = c.table + (int64_t)b * c.max_pages;
+        const int ps = PAGE16 ? 16 : 1 << c.shift;
+        const int dim = FULL ? DP : c.dim, chunks = FULL ? DP / 8 : c.chunks;
         const int first = u0 + wave;
         const int count = first < u1 ? (u1 - first + kWaves - 1) / kWaves : 0;
         if (count == 0) return;
-        const uint16_t* kbase = c.k + (int64_t)kvh * c.chunks * ps * 8;
-        const uint16_t* vbase = c.v + (int64_t)kvh * c.dim * ps;
-
-        int id0 = -1, id1 = -1;           // the pages of 64 of this wave's units, one a lane (and of their upper halves)
-        auto fetch_ids = [&](int it) {
-            const int u = first + kWaves * (it + lane);
-            id0 = id1 = -1;
-            if (u < u1) {
-                const int key = unit_key(sight, u), at = key >> c.shift;
-                id0 = table[at];
-                const int next = (key + 16) >> c.shift;
-                id1 = next == at ? id0 : next < c.max_pages ? table[next] : -1;
-            }
+        const uint16_t* kbase = c.k + (int64_t)kvh * chunks * ps * 8;
+        const uint16_t* vbase = c.v + (int64_t)kvh * dim * ps;
+        // places of this lane's words in a unit: of the keys, key 8 (m / 4) + m % 4 (+ 4 in the second tile) of chunk g (+ 4 j);
+        // of the values, channel m (+ 16 t) of the eight keys g.  Read once: past the caches' memory.
+        const uint32_t k_lane = (uint32_t)(g * ps + 8 * (m >> 2) + (m & 3)) * 16, v_lane = (uint32_t)(g * dim + m) * 16;
+        auto load = [](const uint16_t* base, uint32_t offset) {
+            return __builtin_nontemporal_load(reinterpret_cast<const v4u*>(reinterpret_cast<const uint8_t*>(base) + offset));
         };
+
+        auto page_of = [&](int half, int it) { return __builtin_amdgcn_readfirstlane(ids[half][wave + kWaves * it]); };
         v4u kf[2][DP / 32], vf[DP / 16];
         auto issue_k = [&](int it) {
             const int key = unit_key(sight, first + kWaves * it);
-            const int p0 = __builtin_amdgcn_readlane(id0, it & 63), p1 = __builtin_amdgcn_readlane(id1, it & 63);
-            int page = m < 8 ? p0 : p1;
-            page = page_ok(c, page) ? page : 0;
-            const uint16_t* kp = kbase + (int64_t)page * c.k_page;
+            int p0 = page_of(0, it);
+            p0 = page_ok(c, p0) ? p0 : 0;
+            const uint16_t* kp = kbase + (int64_t)p0 * c.k_page + (PAGE16 ? 0 : (key & (ps - 1)) * 8);
+            uint32_t at = k_lane;
+            if (PAGE16 && m >= 8) {     // keys 16 to 31 of the unit: the second page's first 16
+                int p1 = page_of(1, it);
+                p1 = page_ok(c, p1) ? p1 : 0;
+                kp = kbase + (int64_t)p1 * c.k_page;
+                at -= 256;
+            }
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int in_page = (key + 8 * (m >> 2) + 4 * t + (m & 3)) & (ps - 1);
+            for (int j = 0; j < DP / 32; ++j) {
 #pragma unroll
-                for (int j = 0; j < DP / 32; ++j) {
-                    const int chunk = 4 * j + g;
+                for (int t = 0; t < 2; ++t) {
                     v4u w = {0u, 0u, 0u, 0u};
-                    if (full || chunk < c.chunks) w = *reinterpret_cast<const v4u*>(kp + (chunk * ps + in_page) * 8);
+                    if (FULL || 4 * j + g < chunks) w = load(kp + j * 4 * ps * 8, at + 64 * t);
                     kf[t][j] = w;
                 }
             }
         };
         auto issue_v = [&](int it) {
             const int key = unit_key(sight, first + kWaves * it);
-            const int p0 = __builtin_amdgcn_readlane(id0, it & 63), p1 = __builtin_amdgcn_readlane(id1, it & 63);
-            int page = g < 2 ? p0 : p1;
-            page = page_ok(c, page) ? page : 0;
-            const uint16_t* vp = vbase + (int64_t)page * c.v_page + ((key + 8 * g) & (ps - 1)) * c.dim;
+            int p0 = page_of(0, it);
+            p0 = page_ok(c, p0) ? p0 : 0;
+            const uint16_t* vp = vbase + (int64_t)p0 * c.v_page + (PAGE16 ? 0 : (key & (ps - 1)) * dim);
+            uint32_t at = v_lane;
+            if (PAGE16 && g >= 2) {
+                int p1 = page_of(1, it);
+                p1 = page_ok(c, p1) ? p1 : 0;
+                vp = vbase + (int64_t)p1 * c.v_page;
+                at -= (uint32_t)dim * 32;
+            }
 #pragma unroll
             for (int t = 0; t < DP / 16; ++t) {
-                const int d = 16 * t + m;
                 v4u w = {0u, 0u, 0u, 0u};
-                if (full || d < c.dim) w = *reinterpret_cast<const v4u*>(vp + d * 8);
+                if (FULL || 16 * t + m < dim) w = load(vp, at + 256 * t);
                 vf[t] = w;
             }
         };
 
-        fetch_ids(0);
         issue_k(0);
         issue_v(0);
-        for (int it = 0; it < count; ++it) {
+        // one unit; MORE: the next one's keys are asked for as soon as the scores are formed, its values after the product (known
+        // when compiled: where a load may or may not be on its way, every wait is for all of them)
+        auto step = [&](int it, auto more_) {
+            constexpr bool MORE = decltype(more_)::value;
             const int key = unit_key(sight, first + kWaves * it);
-            const bool ok0 = page_ok(c, __builtin_amdgcn_readlane(id0, it & 63));
-            const bool ok1 = page_ok(c, __builtin_amdgcn_readlane(id1, it & 63));
+            const bool ok0 = page_ok(c, page_of(0, it)), ok1 = PAGE16 ? page_ok(c, page_of(1, it)) : ok0;
             v4f s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+            int q_at = g * 16 + m;
+            asm volatile("" : "+v"(q_at));                // q stays in LDS: in registers it would halve the waves
 #pragma unroll
             for (int p = 0; p < kQParts; ++p) {
 #pragma unroll
                 for (int j = 0; j < DP / 32; ++j) {
-                    const uint4 qw = qs[(p * kChunks + 4 * j + g) * 16 + m];
+                    const uint4 qw = qs[(p * kChunks + 4 * j) * 16 + q_at];
                     const v4u qf = {qw.x, qw.y, qw.z, qw.w};
                     s[0] = Elem<T>::mfma16(kf[0][j], qf, s[0]);
                     s[1] = Elem<T>::mfma16(kf[1][j], qf, s[1]);
                 }
             }
-            const bool more = it + 1 < count;
-            if (more) {
-                if (((it + 1) & 63) == 0) fetch_ids(it + 1);
+            if constexpr (MORE) {
                 issue_k(it + 1);
             }
             // scores of the keys key + 8 g + e, e = 4 t + i
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * gain;
-            const bool whole = ok0 && ok1 && key + kUnit <= sight.len && (key >= sight.lo || key + kUnit <= sight.sinks);
+            const bool whole = (ok0 & ok1 & (key + kUnit <= sight.len) & ((key >= sight.lo) | (key + kUnit <= sight.sinks))) != 0;
             if (!whole) {
                 const bool there = g < 2 ? ok0 : ok1;
                 uint32_t seen = 0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int j = key + 8 * g + e;
-                    const bool in = there && j < sight.len && (j >= sight.lo || j < sight.sinks);
+                    const bool in = there & (j < sight.len) & ((j >= sight.lo) | (j < sight.sinks));
                     seen |= in ? 1u << e : 0u;
                     x[e] = in ? x[e] : kNegInf;
                 }
@@ -260,19 +281,22 @@ struct Decode {
 #pragma unroll
                 for (int t = 0; t < DP / 16; ++t) row.o[t] = Elem<T>::mfma16(vf[t], pf, row.o[t]);
             }
-            if (more) issue_v(it + 1);
-        }
+            if constexpr (MORE) issue_v(it + 1);
+        };
+        for (int it = 0; it + 1 < count; ++it) step(it, std::true_type{});
+        step(count - 1, std::false_type{});
     }
 };
 
-template <int T, int DP, bool F32>
-__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_decode_kernel(DecodeArgs a) {
-    using D = Decode<T, DP, F32>;
+template <int T, int DP, bool F32, bool FULL, bool PAGE16>
+__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_decode_kernel(DecodeArgs a) {
+    using D = Decode<T, DP, F32, FULL, PAGE16>;
     __shared__ uint4 qs[D::kQBytes / 16];
     __shared__ float gain[16];
     __shared__ float wave_m[kWaves][16], wave_l[kWaves][16];
     __shared__ int prefix[kMaxSeqs + 1];
     __shared__ int wave_total[kWaves];
+    __shared__ int ids[2][kIds];
     extern __shared__ float wave_o[];                     // [wave][head][channel]
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -351,7 +375,9 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_decode_kernel
         const int kvh = row / a.tiles, tile = row - kvh * a.tiles;
         const int head0 = kvh * a.group + tile * 16;
         const int count = a.group - tile * 16 < 16 ? a.group - tile * 16 : 16;
+        const int stop = u1 < sight.units ? u1 : sight.units;
         D::stage_q(a, b, head0, count, qs, gain);
+        D::stage_ids(a.c, b, sight, u0, stop < u0 + kIds ? stop : u0 + kIds, ids);
         __syncthreads();
 
         Row<DP> r;
@@ -359,7 +385,14 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_decode_kernel
         r.l = 0.0f;
 #pragma unroll
         for (int t = 0; t < DP / 16; ++t) r.o[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-        D::run(a, b, kvh, sight, u0, u1 < sight.units ? u1 : sight.units, qs, gain[n], r);
+        for (int v0 = u0; v0 < stop; v0 += kIds) {
+            if (v0 > u0) {
+                __syncthreads();
+                D::stage_ids(a.c, b, sight, v0, stop < v0 + kIds ? stop : v0 + kIds, ids);
+                __syncthreads();
+            }
+            D::run(a, kvh, sight, v0, stop < v0 + kIds ? stop : v0 + kIds, ids, qs, gain[n], r);
+        }
 
         // the four waves' states become one
         r.l = sum_xor32(sum_xor16(r.l));
@@ -478,36 +511,47 @@ __global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
                    none ? 0.0f : o[3] / l);
 }
 
-template <int T, int DP, bool F32>
-hipError_t launch(DecodeArgs a, bool split, hipStream_t s) {
+template <int T, int DP, bool F32, bool FULL, bool PAGE16>
+hipError_t launch_page(DecodeArgs a, bool split, hipStream_t s) {
     const size_t lds = (size_t)kWaves * a.rows * DP * 4;
     const int rows = a.c.kv_heads * a.tiles;
     const int total = a.n_seqs, first = a.first_seq;
+    const auto kern = attn_decode_kernel<T, DP, F32, FULL, PAGE16>;
     if (!split) {
         a.ws = nullptr;
         const int64_t most = (1 << 23) / rows;            // a grid has fewer than 2^32 threads
         for (int64_t at = 0; at < total; at += most) {
             a.first_seq = first + (int)at;
             a.n_seqs = (int)(total - at < most ? total - at : most);
-            hipLaunchKernelGGL((attn_decode_kernel<T, DP, F32>), dim3((unsigned)(a.n_seqs * rows)), dim3(kThreads), lds, s, a);
+            hipLaunchKernelGGL(kern, dim3((unsigned)(a.n_seqs * rows)), dim3(kThreads), lds, s, a);
         }
         return hipGetLastError();
     }
+    // One round of work groups, each with keys and values of 16 DP KiB on their way: two a CU (DP <= 64: four) keep the memory
+    // busy, and a third only starts and joins more parts (131071 keys of 8 heads 95 us against 98, 32 sequences 81 against 83).
+    const int resident = resident_groups(reinterpret_cast<const void*>(kern), kThreads, lds), most = DP <= 64 ? 4 : 2;
+    const int groups = (resident < most ? resident : most) * device_cus() < kMaxGroups ? (resident < most ? resident : most) * device_cus()
+                                                                                      : kMaxGroups;
     for (int at = 0; at < total; at += kMaxSeqs) {
         a.first_seq = first + at;
         a.n_seqs = total - at < kMaxSeqs ? total - at : kMaxSeqs;
-        hipLaunchKernelGGL((attn_decode_kernel<T, DP, F32>), dim3(kMaxGroups), dim3(kThreads), lds, s, a);
+        hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kThreads), lds, s, a);
         hipLaunchKernelGGL((attn_join_kernel<T, F32>), dim3((unsigned)(a.n_seqs * rows), (unsigned)((a.rows * a.c.dim / 4 + 63) / 64)),
                            dim3(256), 0, s, a);
     }
     return hipGetLastError();
 }
 
+template <int T, int DP, bool F32, bool FULL>
+hipError_t launch(const DecodeArgs& a, bool split, hipStream_t s) {
+    return a.c.shift == 4 ? launch_page<T, DP, F32, FULL, true>(a, split, s) : launch_page<T, DP, F32, FULL, false>(a, split, s);
+}
+
 template <int T, bool F32>
 hipError_t launch_dim(const DecodeArgs& a, bool split, hipStream_t s) {
-    if (a.c.dim <= 64) return launch<T, 64, F32>(a, split, s);
-    if (a.c.dim <= 128) return launch<T, 128, F32>(a, split, s);
-    return launch<T, 256, F32>(a, split, s);
+    if (a.c.dim <= 64) return a.c.dim == 64 ? launch<T, 64, F32, true>(a, split, s) : launch<T, 64, F32, false>(a, split, s);
+    if (a.c.dim <= 128) return a.c.dim == 128 ? launch<T, 128, F32, true>(a, split, s) : launch<T, 128, F32, false>(a, split, s);
+    return launch<T, 256, F32, false>(a, split, s);
 }
 
 int most_units(int64_t max_pages, int page_size, int window, int n_sink) {
@@ -520,11 +564,19 @@ int most_units(int64_t max_pages, int page_size, int window, int n_sink) {
     return (int)units;
 }
 
+// Whether rows are split: not where the longest takes little longer than starting and joining parts would, nor where they are
+// many and a window or a short table keeps them about alike (then the work groups are enough and the second launch is saved).
+bool rows_split(int64_t n_seqs, int heads, int kv_heads, int page_size, int64_t max_pages, int window, int n_sink) {
+    const int units = most_units(max_pages, page_size, window, n_sink);
+    const int64_t rows = n_seqs * kv_heads * ((heads / kv_heads + 15) / 16);
+    return units > kWholeUnits && (units > kManyUnits || rows < kManyRows);
+}
+
 }  // namespace
 
-size_t attn_decode_workspace_bytes(int64_t, int heads, int kv_heads, int dim, int page_size, int64_t max_pages, int window,
-                                   int n_sink) {
-    if (most_units(max_pages, page_size, window, n_sink) <= kWholeUnits) return 0;
+size_t attn_decode_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim, int page_size, int64_t max_pages,
+                                   int window, int n_sink) {
+    if (!rows_split(n_seqs, heads, kv_heads, page_size, max_pages, window, n_sink)) return 0;
     const int group = heads / kv_heads;
     return (size_t)kPrefixBytes + (size_t)(2 * kMaxGroups * slot_floats(group < 16 ? group : 16, dim)) * 4;
 }
@@ -543,7 +595,7 @@ hipError_t launch_attn_decode(const KvCache& c, int dtype, const AttnArgs& args,
     a.n_sink = args.n_sink;
     a.n_seqs = c.n_seqs;
     a.ws = static_cast<int32_t*>(ws);
-    const bool split = most_units(c.max_pages, 1 << c.shift, args.window, args.n_sink) > kWholeUnits;
+    const bool split = rows_split(c.n_seqs, args.heads, c.kv_heads, 1 << c.shift, c.max_pages, args.window, args.n_sink);
     if (dtype == kBf16) return args.f32 ? launch_dim<kBf16, true>(a, split, s) : launch_dim<kBf16, false>(a, split, s);
     return args.f32 ? launch_dim<kF16, true>(a, split, s) : launch_dim<kF16, false>(a, split, s);
 }
