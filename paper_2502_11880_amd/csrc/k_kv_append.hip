@@ -10,6 +10,7 @@ namespace bitnet {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWantGroups = 4096;    // sixteen work groups a CU (five prompts of 7400 tokens: 74 us against 78 with eight)
 
 // Units of sequence b start at floor(q_start[b] / 8) + 2 b: its tokens touch at most ceil(n / 8) + 1 of them, which never
 // reach the next sequence's, so no prefix sum is needed (a few units stay empty).
@@ -17,7 +18,7 @@ __device__ __forceinline__ int first_unit(const int32_t* q_start, int b) { retur
 
 template <int T, bool F32>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvCache c, const void* k, const void* v, const int32_t* q_start,
-                                                             int n_tokens) {
+                                                             int n_tokens, int heads) {
     const int id = blockIdx.x;
     const int b = q_start ? find_last(c.n_seqs, id, [&](int i) { return first_unit(q_start, i); }) : id;
     const Span span = span_of(q_start, b, n_tokens);
@@ -31,42 +32,56 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvCache c, const vo
     const int page = c.table[(int64_t)b * c.max_pages + at];
     if (!page_ok(c, page)) return;
     const int ps = 1 << c.shift, slot = base & (ps - 1);
-    const int h = blockIdx.y;
+    const int h0 = blockIdx.y * heads, h1 = h0 + heads < c.kv_heads ? h0 + heads : c.kv_heads;
     const int64_t row0 = (int64_t)span.first - p0;        // row of position p: row0 + p
-    uint16_t* kp = c.k + (int64_t)page * c.k_page + (int64_t)h * c.chunks * ps * 8;
-    uint16_t* vp = c.v + (int64_t)page * c.v_page + (int64_t)h * c.dim * ps + (int64_t)slot * c.dim;
-    const int k_items = c.chunks * 8;
-    for (int i = threadIdx.x; i < k_items + c.dim; i += kThreads) {
-        if (i < k_items) {
-            const int p = base + (i & 7), chunk = i >> 3;
-            if (p < low || p >= len) continue;
-            const int64_t src = ((row0 + p) * c.kv_heads + h) * c.dim + 8 * chunk;
+    const int64_t row_step = (int64_t)c.kv_heads * c.dim;
+    uint16_t* kp = c.k + (int64_t)page * c.k_page + (int64_t)slot * 8;
+    uint16_t* vp = c.v + (int64_t)page * c.v_page + (int64_t)slot * c.dim;
+
+    // keys: eight threads a chunk, one for each token
+    const int p = base + (threadIdx.x & 7);
+    const int64_t k_row = (row0 + p) * row_step;
+    const int first_chunk = h0 * c.chunks, last_chunk = h1 * c.chunks;
+    if (p >= low && p < len) {
+#pragma unroll 2
+        for (int i = first_chunk + (threadIdx.x >> 3); i < last_chunk; i += kThreads / 8) {
+            const int h = i / c.chunks, chunk = i - h * c.chunks;
+            const int64_t src = k_row + h * c.dim + 8 * chunk;
             const float4 x = load4<T, F32>(k, src);
             float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (8 * chunk + 4 < c.dim) y = load4<T, F32>(k, src + 4);
-            *reinterpret_cast<uint4*>(kp + ((int64_t)chunk * ps + slot + (i & 7)) * 8) =
+            *reinterpret_cast<uint4*>(kp + ((int64_t)i * ps + (threadIdx.x & 7)) * 8) =
                 make_uint4(Elem<T>::pack(x.x, x.y), Elem<T>::pack(x.z, x.w), Elem<T>::pack(y.x, y.y), Elem<T>::pack(y.z, y.w));
-        } else {
-            const int d = i - k_items;
-            uint16_t e[8];
+        }
+    }
+    // values: a thread a channel of the eight tokens
+    const bool whole = base >= low && base + 8 <= len;
+    const int64_t v_row = (row0 + base) * row_step;
+    for (int i = h0 * c.dim + threadIdx.x; i < h1 * c.dim; i += kThreads) {
+        const int h = i / c.dim, d = i - h * c.dim;
+        uint16_t* dst = vp + ((int64_t)h * ps * c.dim + d * 8);
+        if (whole) {
+            uint32_t e[8];
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
-                const int p = base + t;
-                e[t] = 0;
-                if (p < low || p >= len) continue;
-                const int64_t src = ((row0 + p) * c.kv_heads + h) * c.dim + d;
-                if constexpr (F32) e[t] = Elem<T>::from(static_cast<const float*>(v)[src]);
+                const int64_t src = v_row + t * row_step + i;
+                if constexpr (F32) e[t] = __float_as_uint(static_cast<const float*>(v)[src]);
                 else e[t] = static_cast<const uint16_t*>(v)[src];
             }
-            uint16_t* dst = vp + (int64_t)d * 8;
-            if (base >= low && base + 8 <= len) {
-                *reinterpret_cast<uint4*>(dst) =
-                    make_uint4((uint32_t)e[0] | (uint32_t)e[1] << 16, (uint32_t)e[2] | (uint32_t)e[3] << 16,
-                               (uint32_t)e[4] | (uint32_t)e[5] << 16, (uint32_t)e[6] | (uint32_t)e[7] << 16);
-            } else {
+            uint4 w;
+            if constexpr (F32)
+                w = make_uint4(Elem<T>::pack(__uint_as_float(e[0]), __uint_as_float(e[1])), Elem<T>::pack(__uint_as_float(e[2]), __uint_as_float(e[3])),
+                               Elem<T>::pack(__uint_as_float(e[4]), __uint_as_float(e[5])), Elem<T>::pack(__uint_as_float(e[6]), __uint_as_float(e[7])));
+            else
+                w = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+            *reinterpret_cast<uint4*>(dst) = w;
+        } else {
 #pragma unroll
-                for (int t = 0; t < 8; ++t)
-                    if (base + t >= low && base + t < len) dst[t] = e[t];
+            for (int t = 0; t < 8; ++t) {
+                if (base + t < low || base + t >= len) continue;
+                const int64_t src = v_row + t * row_step + i;
+                if constexpr (F32) dst[t] = Elem<T>::from(static_cast<const float*>(v)[src]);
+                else dst[t] = static_cast<const uint16_t*>(v)[src];
             }
         }
     }
@@ -77,13 +92,17 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvCache c, const vo
 hipError_t launch_kv_append(const KvCache& c, int dtype, const void* k, const void* v, bool f32, const int32_t* q_start,
                             int n_tokens, hipStream_t s) {
     const int64_t units = q_start ? (int64_t)n_tokens / 8 + 2 * (int64_t)c.n_seqs : c.n_seqs;
-    const dim3 grid((unsigned)units, (unsigned)c.kv_heads);
+    // A prompt's units keep the device busy by themselves and one work group takes all heads of a unit (fewer, longer groups:
+    // what a group looks up before its first row, four dependent reads, then costs little); few units are split by heads.
+    const int64_t want = (kWantGroups + units - 1) / units;
+    const int splits = (int)(want < c.kv_heads ? want : c.kv_heads), heads = (c.kv_heads + splits - 1) / splits;
+    const dim3 grid((unsigned)units, (unsigned)((c.kv_heads + heads - 1) / heads));
     if (dtype == kBf16) {
-        if (f32) hipLaunchKernelGGL((kv_append_kernel<kBf16, true>), grid, dim3(kThreads), 0, s, c, k, v, q_start, n_tokens);
-        else hipLaunchKernelGGL((kv_append_kernel<kBf16, false>), grid, dim3(kThreads), 0, s, c, k, v, q_start, n_tokens);
+        if (f32) hipLaunchKernelGGL((kv_append_kernel<kBf16, true>), grid, dim3(kThreads), 0, s, c, k, v, q_start, n_tokens, heads);
+        else hipLaunchKernelGGL((kv_append_kernel<kBf16, false>), grid, dim3(kThreads), 0, s, c, k, v, q_start, n_tokens, heads);
     } else {
-        if (f32) hipLaunchKernelGGL((kv_append_kernel<kF16, true>), grid, dim3(kThreads), 0, s, c, k, v, q_start, n_tokens);
-        else hipLaunchKernelGGL((kv_append_kernel<kF16, false>), grid, dim3(kThreads), 0, s, c, k, v, q_start, n_tokens);
+        if (f32) hipLaunchKernelGGL((kv_append_kernel<kF16, true>), grid, dim3(kThreads), 0, s, c, k, v, q_start, n_tokens, heads);
+        else hipLaunchKernelGGL((kv_append_kernel<kF16, false>), grid, dim3(kThreads), 0, s, c, k, v, q_start, n_tokens, heads);
     }
     return hipGetLastError();
 }

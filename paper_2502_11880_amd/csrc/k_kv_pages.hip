@@ -13,7 +13,7 @@ constexpr int kPlanThreads = 1024;
 constexpr int kCopyThreads = 256;
 constexpr int kCopyWords = 4;                              // 16-byte words a thread holds at a time
 constexpr int kPiece = kCopyThreads * kCopyWords * 16;     // bytes of a piece
-constexpr int kCountIds = 2048;                            // page ids of one group of the compaction's counts
+constexpr int kCountIds = 8192;                            // page ids of one group of the compaction's counts
 
 // Workspace: a header, three ints for every sequence of a call, three for every page, and the counts.
 constexpr int kHeader = 64;                                // [0] pages to copy, [1] live pages
@@ -175,58 +175,18 @@ __global__ __launch_bounds__(kPlanThreads) void kv_fork_plan_kernel(KvTables t, 
     if (threadIdx.x == 0) *n_short = total;
 }
 
-// Forking, second half: the children's rows and the reference counts (the last page's bytes: copy_pages_kernel).
-__global__ __launch_bounds__(256) void kv_fork_rows_kernel(KvTables t, const int32_t* parents, const int32_t* children,
-                                                           int shift, const int32_t* ws) {
-    const int i = blockIdx.x, c = children[i], p = parents[i];
-    const int state = ws[ws_seq(t.n_seqs, 0) + i];
-    if (state == -3) return;
-    const bool ok = state != -2;
-    const int len = ok ? t.kv_len[p] : 0, full = len >> shift;
-    const int col = blockIdx.y * 256 + threadIdx.x;
-    if (col == 0) t.kv_len[c] = len;
-    if (col >= t.max_pages) return;
-    int page = -1;
-    if (ok && col < full) {
-        page = t.table[(int64_t)p * t.max_pages + col];
-        if ((unsigned)page < (unsigned)t.n_pages) atomicAdd(&t.refs[page], 1);
-    } else if (ok && col == full && state >= 0) {
-        page = ws[ws_seq(t.n_seqs, 2) + i];
-        t.refs[page] = 1;
-    }
-    t.table[(int64_t)c * t.max_pages + col] = page;
-}
-
-// Freeing: every entry is taken by exactly one thread, so a sequence that is named twice is freed once.  With keep_window the
-// sequence stays and loses the pages that no later token sees.
-__global__ __launch_bounds__(256) void kv_free_kernel(KvTables t, const int32_t* seqs, int shift, bool keep_window, int window,
-                                                      int n_sink) {
-    const int s = seqs[blockIdx.x];
-    if ((unsigned)s >= (unsigned)t.n_seqs) return;
-    const int col = blockIdx.y * 256 + threadIdx.x;
-    if (!keep_window && col == 0) t.kv_len[s] = 0;
-    if (col >= t.max_pages) return;
-    if (keep_window) {
-        const int64_t from = (int64_t)col << shift, to = from + (1 << shift);
-        if (from < n_sink || to > (int64_t)t.kv_len[s] + 1 - window) return;
-    }
-    const int page = atomicExch(&t.table[(int64_t)s * t.max_pages + col], -1);
-    if ((unsigned)page < (unsigned)t.n_pages) atomicSub(&t.refs[page], 1);
-}
-
-// Bytes of the pairs (src[i], dst[i]) in every plane; count: on the device or given.  Pairs out of range are skipped.
-__global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(KvPool p, const int32_t* src, const int32_t* dst,
-                                                                  const int32_t* n_dev, int n_host) {
-    const int n = n_dev ? *n_dev : n_host;
+// Bytes of the pairs (src[i], dst[i]), i < n, in every plane: this work group's share, as number `group` of `groups`.  Pairs out
+// of range are skipped.
+__device__ void copy_pages(const KvPool& p, const int32_t* src, const int32_t* dst, int n, int group, int groups) {
     const int k_pieces = (int)((p.k_bytes + kPiece - 1) / kPiece), v_pieces = (int)((p.v_bytes + kPiece - 1) / kPiece);
     const int per_layer = k_pieces + v_pieces;
     const int64_t per_pair = (int64_t)per_layer * p.n_layers;
     const int64_t all = per_pair * n;
-    for (int64_t w = blockIdx.x; w < all; w += gridDim.x) {
+    for (int64_t w = group; w < all; w += groups) {
         const int pair = (int)(w / per_pair);
-        const int rest = (int)(w - pair * per_pair);
-        const int layer = rest / per_layer;
-        int piece = rest - layer * per_layer;
+        const int64_t rest = w - pair * per_pair;
+        const int layer = (int)(rest / per_layer);
+        int piece = (int)(rest - (int64_t)layer * per_layer);
         const int from = src[pair], to = dst[pair];
         if ((unsigned)from >= (unsigned)p.n_pages || (unsigned)to >= (unsigned)p.n_pages || from == to) continue;
         const bool value = piece >= k_pieces;
@@ -250,12 +210,63 @@ __global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(KvPool p, cons
     }
 }
 
+__global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(KvPool p, const int32_t* src, const int32_t* dst, int n) {
+    copy_pages(p, src, dst, n, blockIdx.x, gridDim.x);
+}
+
+// Forking, second half: the children's rows and the reference counts by the first row_groups work groups, the last pages' bytes
+// by the others.
+__global__ __launch_bounds__(kCopyThreads) void kv_fork_kernel(KvPool pool, KvTables t, const int32_t* parents,
+                                                               const int32_t* children, int n, int shift, const int32_t* ws,
+                                                               int row_groups) {
+    if ((int)blockIdx.x >= row_groups) {
+        copy_pages(pool, ws + ws_seq(t.n_seqs, 1), ws + ws_seq(t.n_seqs, 2), n, blockIdx.x - row_groups, gridDim.x - row_groups);
+        return;
+    }
+    const int64_t entries = (int64_t)n * t.max_pages;
+    for (int64_t e = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; e < entries; e += (int64_t)row_groups * kCopyThreads) {
+        const int i = (int)(e / t.max_pages), col = (int)(e - (int64_t)i * t.max_pages);
+        const int state = ws[ws_seq(t.n_seqs, 0) + i];
+        if (state == -3) continue;
+        const int c = children[i], p = parents[i];
+        const bool ok = state != -2;
+        const int len = ok ? t.kv_len[p] : 0, full = len >> shift;
+        if (col == 0) t.kv_len[c] = len;
+        int page = -1;
+        if (ok && col < full) {
+            page = t.table[(int64_t)p * t.max_pages + col];
+            if ((unsigned)page < (unsigned)t.n_pages) atomicAdd(&t.refs[page], 1);
+        } else if (ok && col == full && state >= 0) {
+            page = ws[ws_seq(t.n_seqs, 2) + i];
+            t.refs[page] = 1;
+        }
+        t.table[(int64_t)c * t.max_pages + col] = page;
+    }
+}
+
+// Freeing: every entry is taken by exactly one thread, so a sequence that is named twice is freed once.  With keep_window the
+// sequence stays and loses the pages that no later token sees.
+__global__ __launch_bounds__(256) void kv_free_kernel(KvTables t, const int32_t* seqs, int shift, bool keep_window, int window,
+                                                      int n_sink) {
+    const int s = seqs[blockIdx.x];
+    if ((unsigned)s >= (unsigned)t.n_seqs) return;
+    const int col = blockIdx.y * 256 + threadIdx.x;
+    if (!keep_window && col == 0) t.kv_len[s] = 0;
+    if (col >= t.max_pages) return;
+    if (keep_window) {
+        const int64_t from = (int64_t)col << shift, to = from + (1 << shift);
+        if (from < n_sink || to > (int64_t)t.kv_len[s] + 1 - window) return;
+    }
+    const int page = atomicExch(&t.table[(int64_t)s * t.max_pages + col], -1);
+    if ((unsigned)page < (unsigned)t.n_pages) atomicSub(&t.refs[page], 1);
+}
+
 // Compaction: the k-th lowest hole below the number of live pages takes the k-th highest live page above it.
-// Live pages of every kCountIds ids.
+// Live pages of every kCountIds ids (only where there are more than so many).
 __global__ __launch_bounds__(256) void kv_count_kernel(const int32_t* refs, int n_pages, int32_t* counts) {
     __shared__ int part[4];
     int mine = 0;
-#pragma unroll
+#pragma unroll 8
     for (int i = 0; i < kCountIds / 256; ++i) {
         const int id = blockIdx.x * kCountIds + i * 256 + threadIdx.x;
         mine += id < n_pages && refs[id] > 0;
@@ -266,37 +277,42 @@ __global__ __launch_bounds__(256) void kv_count_kernel(const int32_t* refs, int 
 }
 
 // Pairs, and every page's place among the moved ones (-1: it stays).
-__global__ __launch_bounds__(256) void kv_pairs_kernel(const int32_t* refs, int n_pages, int n_seqs, int groups,
-                                                       int32_t* n_live_out, int32_t* ws) {
-    __shared__ int part[4];
+__global__ __launch_bounds__(kPlanThreads) void kv_pairs_kernel(const int32_t* refs, int n_pages, int n_seqs, int groups,
+                                                                int32_t* n_live_out, int32_t* ws) {
+    __shared__ int part[kPlanThreads / 64];
+    constexpr int kIds = kCountIds / kPlanThreads;
     const int32_t* counts = ws + ws_page(n_seqs, n_pages, 3);
     int32_t* src = ws + ws_page(n_seqs, n_pages, 0);
     int32_t* dst = ws + ws_page(n_seqs, n_pages, 1);
     int32_t* rank = ws + ws_page(n_seqs, n_pages, 2);
-    int lower = 0, all = 0;
-    for (int g = threadIdx.x; g < groups; g += 256) {
-        const int c = counts[g];
-        lower += g < (int)blockIdx.x ? c : 0;
-        all += c;
+    const int id0 = blockIdx.x * kCountIds + threadIdx.x * kIds;
+    int on[kIds], mine = 0;
+#pragma unroll
+    for (int i = 0; i < kIds; ++i) {
+        on[i] = id0 + i < n_pages && refs[id0 + i] > 0;
+        mine += on[i];
     }
-    int before, live;
-    block_scan(lower, part, before);
-    block_scan(all, part, live);
+    int before = 0, live, total;
+    int k = block_scan(mine, part, total);                 // live pages below the id
+    if (groups == 1) {
+        live = total;
+    } else {
+        int lower = 0, all = 0;
+        for (int g = threadIdx.x; g < groups; g += kPlanThreads) {
+            const int c = counts[g];
+            lower += g < (int)blockIdx.x ? c : 0;
+            all += c;
+        }
+        block_scan(lower, part, before);
+        block_scan(all, part, live);
+    }
+    k += before;
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         *n_live_out = live;
         if (live == 0) ws[0] = 0;
     }
-    const int id0 = blockIdx.x * kCountIds + threadIdx.x * (kCountIds / 256);
-    int on[kCountIds / 256], mine = 0;
 #pragma unroll
-    for (int i = 0; i < kCountIds / 256; ++i) {
-        on[i] = id0 + i < n_pages && refs[id0 + i] > 0;
-        mine += on[i];
-    }
-    int total;
-    int k = before + block_scan(mine, part, total);        // live pages below the id
-#pragma unroll
-    for (int i = 0; i < kCountIds / 256; ++i) {
+    for (int i = 0; i < kIds; ++i) {
         const int id = id0 + i;
         if (id < n_pages) {
             int r = -1;
@@ -313,26 +329,35 @@ __global__ __launch_bounds__(256) void kv_pairs_kernel(const int32_t* refs, int 
     }
 }
 
-// Tables and reference counts after the moves.
-__global__ __launch_bounds__(256) void kv_remap_kernel(KvTables t, const int32_t* ws) {
+// The moves: tables and reference counts by the first row_groups work groups, the pages' bytes by the others.
+__global__ __launch_bounds__(kCopyThreads) void kv_compact_kernel(KvPool pool, KvTables t, const int32_t* ws, int row_groups) {
     const int32_t* src = ws + ws_page(t.n_seqs, t.n_pages, 0);
     const int32_t* dst = ws + ws_page(t.n_seqs, t.n_pages, 1);
     const int32_t* rank = ws + ws_page(t.n_seqs, t.n_pages, 2);
     const int moves = ws[0];
-    const int64_t entries = (int64_t)t.n_seqs * t.max_pages, step = (int64_t)gridDim.x * 256;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < entries; i += step) {
+    if ((int)blockIdx.x >= row_groups) {
+        copy_pages(pool, src, dst, moves, blockIdx.x - row_groups, gridDim.x - row_groups);
+        return;
+    }
+    const int64_t entries = (int64_t)t.n_seqs * t.max_pages, step = (int64_t)row_groups * kCopyThreads;
+    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < entries; i += step) {
         const int page = t.table[i];
         if ((unsigned)page >= (unsigned)t.n_pages) continue;
         const int r = rank[page];
         if (r >= 0) t.table[i] = dst[r];
     }
-    for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < moves; r += step) {
+    for (int64_t r = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; r < moves; r += step) {
         t.refs[dst[r]] = t.refs[src[r]];
         t.refs[src[r]] = 0;
     }
 }
 
 int copy_groups() { return device_cus() * 8; }
+// Work groups for the entries of tables, up to 512.
+int row_groups(int64_t entries) {
+    const int64_t groups = (entries + kCopyThreads - 1) / kCopyThreads;
+    return (int)(groups < 512 ? groups : 512);
+}
 
 int64_t pieces_of(const KvPool& p) {
     return ((p.k_bytes + kPiece - 1) / kPiece + (p.v_bytes + kPiece - 1) / kPiece) * p.n_layers;
@@ -346,8 +371,7 @@ size_t kv_workspace_bytes(int64_t n_pages, int64_t n_seqs) {
 
 hipError_t launch_kv_copy(const KvPool& p, const int32_t* src, const int32_t* dst, int n, hipStream_t s) {
     const int64_t all = pieces_of(p) * n, most = copy_groups();
-    hipLaunchKernelGGL(copy_pages_kernel, dim3((unsigned)(all < most ? all : most)), dim3(kCopyThreads), 0, s, p, src, dst,
-                       (const int32_t*)nullptr, n);
+    hipLaunchKernelGGL(copy_pages_kernel, dim3((unsigned)(all < most ? all : most)), dim3(kCopyThreads), 0, s, p, src, dst, n);
     return hipGetLastError();
 }
 
@@ -375,26 +399,26 @@ hipError_t launch_kv_fork(const KvPool& p, const KvTables& t, const int32_t* par
     int32_t* w = static_cast<int32_t*>(ws);
     hipLaunchKernelGGL(kv_fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, t, parents, children, n, shift, n_short, w);
     if (n == 0) return hipGetLastError();
-    hipLaunchKernelGGL(kv_fork_rows_kernel, dim3((unsigned)n, (unsigned)((t.max_pages + 255) / 256)), dim3(256), 0, s, t,
-                       parents, children, shift, w);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    return launch_kv_copy(p, w + ws_seq(t.n_seqs, 1), w + ws_seq(t.n_seqs, 2), n, s);
+    const int64_t most = copy_groups(), all = pieces_of(p) * n;
+    const int rows = row_groups((int64_t)n * t.max_pages);
+    hipLaunchKernelGGL(kv_fork_kernel, dim3((unsigned)(rows + (all < most ? all : most))), dim3(kCopyThreads), 0, s, p, t, parents,
+                       children, n, shift, w, rows);
+    return hipGetLastError();
 }
 
 hipError_t launch_kv_compact(const KvPool& p, const KvTables& t, int32_t* n_live, void* ws, hipStream_t s) {
     int32_t* w = static_cast<int32_t*>(ws);
     const int groups = (t.n_pages + kCountIds - 1) / kCountIds;
-    hipLaunchKernelGGL(kv_count_kernel, dim3((unsigned)groups), dim3(256), 0, s, t.refs, t.n_pages,
-                       w + ws_page(t.n_seqs, t.n_pages, 3));
-    hipLaunchKernelGGL(kv_pairs_kernel, dim3((unsigned)groups), dim3(256), 0, s, t.refs, t.n_pages, t.n_seqs, groups, n_live,
-                       w);
+    if (groups > 1)
+        hipLaunchKernelGGL(kv_count_kernel, dim3((unsigned)groups), dim3(256), 0, s, t.refs, t.n_pages,
+                           w + ws_page(t.n_seqs, t.n_pages, 3));
+    hipLaunchKernelGGL(kv_pairs_kernel, dim3((unsigned)groups), dim3(kPlanThreads), 0, s, t.refs, t.n_pages, t.n_seqs, groups,
+                       n_live, w);
     const int64_t entries = (int64_t)t.n_seqs * t.max_pages > t.n_pages ? (int64_t)t.n_seqs * t.max_pages : t.n_pages;
-    const int64_t remap = (entries + 255) / 256, most = copy_groups();
-    hipLaunchKernelGGL(kv_remap_kernel, dim3((unsigned)(remap < most ? remap : most)), dim3(256), 0, s, t, w);
-    const int64_t all = pieces_of(p) * (t.n_pages / 2 + 1);
-    hipLaunchKernelGGL(copy_pages_kernel, dim3((unsigned)(all < most ? all : most)), dim3(kCopyThreads), 0, s, p,
-                       w + ws_page(t.n_seqs, t.n_pages, 0), w + ws_page(t.n_seqs, t.n_pages, 1), w, 0);
+    const int rows = row_groups(entries);
+    const int64_t all = pieces_of(p) * (t.n_pages / 2 + 1), most = copy_groups();
+    hipLaunchKernelGGL(kv_compact_kernel, dim3((unsigned)(rows + (all < most ? all : most))), dim3(kCopyThreads), 0, s, p, t, w,
+                       rows);
     return hipGetLastError();
 }
 
