@@ -314,6 +314,12 @@ size_t bitnet_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64
 bitnet_status bitnet_attn_decode(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads, float scale,
                                  int64_t window, int64_t n_sink, void* out, void* ws, size_t ws_bytes, void* stream);
 
+/* Workspace bytes with which bitnet_attn_prefill splits the keys of few queries (0 is a valid answer; 0 also for unsupported
+ * sizes).  dtype is that of q and out. */
+size_t bitnet_attn_prefill_workspace_bytes(int cache_dtype, int dtype, int64_t n_seqs, int64_t n_tokens, int64_t n_heads,
+                                           int64_t n_kv_heads, int64_t head_dim, int64_t page_size, int64_t max_pages,
+                                           int64_t window, int64_t n_sink);
+
 /*
  * bitnet_attn_prefill -- attention of a ragged batch of new tokens over the cache that already holds them (and what came
  * before): the n tokens of sequence s are at positions p = kv_len[s] - n + i and see j <= p, with window > 0 only
@@ -321,12 +327,15 @@ bitnet_status bitnet_attn_decode(const bitnet_kv_cache* cache, const void* q, in
  *   q, out    device [n_tokens, n_heads, head_dim]; q_start device int32 [n_seqs + 1] as in bitnet_kv_append (not NULL).
  *   dtype     BITNET_DTYPE_F32: 32-bit precision throughout (about a third of the speed: products in parts);
  *             the cache's type: the weights are rounded to it once before the second product, their sum is not.
- *   Rows of out that no sequence owns are not written.  Other arguments as bitnet_attn_decode; no workspace.
+ *   ws        optional (NULL): bitnet_attn_prefill_workspace_bytes(...) bytes, any contents, nothing kept.  With it a call of
+ *             few queries (a chunk of a prompt behind a long cache, a short prompt) splits their keys over the device and
+ *             joins the parts in a second launch; without, or with less, it does not split.
+ *   Rows of out that no sequence owns are not written.  Other arguments as bitnet_attn_decode.
  *   n_tokens <= 2^24, n_tokens * n_heads <= 2^30, n_seqs * n_kv_heads <= 2^22.
  */
 bitnet_status bitnet_attn_prefill(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads,
                                   const int32_t* q_start, int64_t n_tokens, float scale, int64_t window, int64_t n_sink,
-                                  void* out, void* stream);
+                                  void* out, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Pages.  bitnet_kv_pool: the caches of n_layers layers that share one table, k [n_layers, n_pages, k_page_bytes] and v

@@ -69,9 +69,10 @@ _SIGNATURES = [
     ("bitnet_attn_decode", ctypes.c_int,
      [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_int64, ctypes.c_int64,
       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    ("bitnet_attn_prefill_workspace_bytes", ctypes.c_size_t, [ctypes.c_int] * 2 + [ctypes.c_int64] * 9),
     ("bitnet_attn_prefill", ctypes.c_int,
      [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_float,
-      ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]),
+      ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     ("bitnet_kv_workspace_bytes", ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int64]),
     ("bitnet_kv_copy_pages", ctypes.c_int,
      [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
@@ -414,15 +415,31 @@ def bitnet_attn_decode(q, k_cache, v_cache, table, kv_len, out, scale: float, wi
     _check("bitnet_attn_decode", st)
 
 
+def bitnet_attn_prefill_workspace_bytes(cache_dtype: int, dtype: int, n_seqs: int, n_tokens: int, n_heads: int,
+                                        n_kv_heads: int, head_dim: int, page_size: int, max_pages: int, window: int = 0,
+                                        n_sink: int = 0) -> int:
+    return int(lib().bitnet_attn_prefill_workspace_bytes(cache_dtype, dtype, n_seqs, n_tokens, n_heads, n_kv_heads, head_dim,
+                                                         page_size, max_pages, window, n_sink))
+
+
 def bitnet_attn_prefill(q, q_start, k_cache, v_cache, table, kv_len, out, scale: float, window: int = 0, n_sink: int = 0,
-                        stream=None) -> None:
+                        ws=None, stream=None) -> None:
     """Causal attention of the new tokens q ([tokens, H * D], float32 or the cache's type), which the cache already holds:
-    rows q_start[s] .. q_start[s + 1] - 1 are the last tokens of sequence s."""
+    rows q_start[s] .. q_start[s + 1] - 1 are the last tokens of sequence s.  ws (optional): a workspace of
+    bitnet_attn_prefill_workspace_bytes, with which few queries split their keys; where there is none and the call goes to
+    the current stream, one is taken from torch's allocator."""
     c = _cache(k_cache, v_cache, table, kv_len)
     n = q.shape[0]
-    st = lib().bitnet_attn_prefill(ctypes.byref(c), _ptr(q, "q"), _dtype(q, "q"), _heads(q, out, c, n),
-                                   _q_start(q_start, c.n_seqs), n, scale, window, n_sink, _ptr(out, "out"),
-                                   _stream(stream))
+    heads, dtype = _heads(q, out, c, n), _dtype(q, "q")
+    if ws is None and stream is None:
+        need = lib().bitnet_attn_prefill_workspace_bytes(c.dtype, dtype, c.n_seqs, n, heads, c.n_kv_heads, c.head_dim,
+                                                         c.page_size, c.max_pages, window, n_sink)
+        if need:
+            import torch
+            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    st = lib().bitnet_attn_prefill(ctypes.byref(c), _ptr(q, "q"), dtype, heads, _q_start(q_start, c.n_seqs), n, scale, window,
+                                   n_sink, _ptr(out, "out"), _ptr(ws, "ws"),
+                                   0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
     _check("bitnet_attn_prefill", st)
 
 

@@ -29,7 +29,12 @@ struct PrefillArgs {
     float scale2;                    // scale * log2 e
     int window, n_sink;
     int tiles;                       // work groups of a kv head
+    int splits;                      // parts that the keys of each are divided into
+    float* ws;                       // their results, where there are several
 };
+
+// What a work group of `columns` columns leaves for joining: reference and sum of every column, then its output.
+__host__ __device__ __forceinline__ int64_t part_floats(int columns, int dim) { return (int64_t)columns * (2 + dim); }
 
 // Work groups of sequence b start at floor(q_start[b] group / columns) + b.
 __device__ __forceinline__ int first_tile(const int32_t* q_start, int b, int group, int columns) {
@@ -44,6 +49,7 @@ struct Prefill {
     static constexpr int kSteps = DP / 16, kBlocks = (DP + 31) / 32;
     static constexpr int kWords = kTile * DP / 8;         // 16-byte words of a tile's keys (and at most of its values)
     static constexpr int kLoads = (kWords + kThreads - 1) / kThreads;
+    static constexpr bool kSplit = WAVES == 4;            // work groups of 8 waves are only taken where they are enough
     static constexpr int kAhead = 4;                      // words of the keys on their way from LDS
     static constexpr int kSchedMfma = 0x8, kSchedLds = 0x100;
 
@@ -61,7 +67,7 @@ struct Prefill {
     int wave_first, wave_last, open_first, open_last;     // tiles that this wave sees, and those that all its columns see
     int group_first, group_last;                          // tiles that all columns of the work group see
     int sink_end;                                         // tiles with sinks end here
-    int sink_tiles, first, n_tiles;
+    int sink_tiles, first, n_tiles, part_first;           // (n_tiles from part_first on are this work group's)
     const int32_t* table;
     const uint16_t *kbase, *vbase;
     int key_row;
@@ -72,7 +78,10 @@ struct Prefill {
     __device__ __forceinline__ Prefill(const PrefillArgs& args, Lds& l) : a(args), lds(l) {}
 
     // Tiles are numbered by their first key / 64; the t-th that the work group looks at:
-    __device__ __forceinline__ int tile_of(int t) const { return t < sink_tiles ? t : t - sink_tiles + first; }
+    __device__ __forceinline__ int tile_of(int t) const {
+        if constexpr (kSplit) t += part_first;
+        return t < sink_tiles ? t : t - sink_tiles + first;
+    }
     __device__ __forceinline__ int channels() const { return FULL ? DP : dim; }
 
     // Pages of a tile's four quarters (pages of 64 and more: all the same, and only p0 is kept).
@@ -413,15 +422,35 @@ struct Prefill {
                 }
             }
             l = sum_xor32(l);
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            if (!used) continue;
+            if (used) store_block(d, o, odd, m, l, row);
+        }
+    }
+
+    // Channels 32 d .. of this lane's column: divided by the sum, or, where the keys are split, as they are, with m and l.
+    __device__ __forceinline__ void store_block(int d, const v16f& o, const v16f& more, float m, float l, int64_t row) const {
+        if (kSplit && a.splits > 1) {
+            float* part = a.ws + ((int64_t)blockIdx.x * a.splits + blockIdx.y) * part_floats(kColumns, dim);
+            const int col = (tid >> 6) * 32 + n;
+            if (d == 0 && half == 0) {
+                part[col] = m;
+                part[kColumns + col] = l;
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int at = 32 * d + 8 * i + 4 * half;
                 if (FULL || at < dim)
-                    store4<T, F32>(a.out, row + at, o[4 * i] * inv + odd[4 * i], o[4 * i + 1] * inv + odd[4 * i + 1],
-                                   o[4 * i + 2] * inv + odd[4 * i + 2], o[4 * i + 3] * inv + odd[4 * i + 3]);
+                    *reinterpret_cast<v4f*>(part + 2 * kColumns + (int64_t)col * dim + at) =
+                        v4f{o[4 * i] + more[4 * i], o[4 * i + 1] + more[4 * i + 1], o[4 * i + 2] + more[4 * i + 2], o[4 * i + 3] + more[4 * i + 3]};
             }
+            return;
+        }
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;    // l is 0 where nothing was visible
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = 32 * d + 8 * i + 4 * half;
+            if (FULL || at < dim)
+                store4<T, F32>(a.out, row + at, o[4 * i] * inv + more[4 * i], o[4 * i + 1] * inv + more[4 * i + 1],
+                               o[4 * i + 2] * inv + more[4 * i + 2], o[4 * i + 3] * inv + more[4 * i + 3]);
         }
     }
 
@@ -474,6 +503,10 @@ struct Prefill {
         sink_tiles = sink_tiles < first ? sink_tiles : first;
         n_tiles = pos_hi < 0 ? 0 : sink_tiles + pos_hi / kTile + 1 - first;
         sink_end = (a.n_sink + kTile - 1) / kTile;
+        if constexpr (kSplit) {
+            part_first = (int)((int64_t)n_tiles * blockIdx.y / a.splits);
+            n_tiles = (int)((int64_t)n_tiles * (blockIdx.y + 1) / a.splits) - part_first;
+        }
         wave_first = uniform(behind(wpos_lo) / kTile);
         wave_last = uniform(wpos_hi < 0 ? -1 : wpos_hi / kTile);
         open_first = uniform((behind(wpos_hi) + kTile - 1) / kTile);
@@ -529,18 +562,12 @@ struct Prefill {
             return;
         }
         l = sum_xor32(l);
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;    // l is 0 where nothing was visible
         if (!used) return;
+        v16f none;
 #pragma unroll
-        for (int d = 0; d < kBlocks; ++d) {
+        for (int i = 0; i < 16; ++i) none[i] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = 32 * d + 8 * i + 4 * half;
-                if (FULL || at < dim)
-                    store4<T, F32>(a.out, row + at, o[d][4 * i] * inv, o[d][4 * i + 1] * inv, o[d][4 * i + 2] * inv,
-                                   o[d][4 * i + 3] * inv);
-            }
-        }
+        for (int d = 0; d < kBlocks; ++d) store_block(d, o[d], none, m, l, row);
     }
 };
 
@@ -551,42 +578,118 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attn_prefill_kernel(Pref
     P(a, lds).run();
 }
 
+// The parts of every column in the order of the keys.  A thread four channels; blockIdx.y: slices of a work group's columns.
+template <int T, bool F32>
+__global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, int group_columns) {
+    const KvCache& c = a.c;
+    const int kvh = blockIdx.x % c.kv_heads, id = a.tiles - 1 - (int)(blockIdx.x / c.kv_heads);
+    const int b = find_last(c.n_seqs, id, [&](int i) { return first_tile(a.q_start, i, a.group, group_columns); });
+    const Span span = span_of(a.q_start, b, a.n_tokens);
+    const int col0 = (id - first_tile(a.q_start, b, a.group, group_columns)) * group_columns;
+    const int columns = span.count * a.group;
+    const int quads = c.dim >> 2, slice = group_columns / gridDim.y;
+    const float* parts = a.ws + (int64_t)blockIdx.x * a.splits * part_floats(group_columns, c.dim);
+    for (int i = threadIdx.x; i < slice * quads; i += 256) {
+        const int in_slice = i / quads, d = 4 * (i - in_slice * quads), local = blockIdx.y * slice + in_slice, col = col0 + local;
+        if (col >= columns) continue;
+        float m = kNegInf, l = 0.0f;
+        v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int z = 0; z < a.splits; ++z) {
+            const float* part = parts + (int64_t)z * part_floats(group_columns, c.dim);
+            const float pm = part[local], pl = part[group_columns + local];
+            const v4f po = *reinterpret_cast<const v4f*>(part + 2 * group_columns + (int64_t)local * c.dim + d);
+            const float top = fmaxf(m, pm);
+            const float fa = m == kNegInf ? 0.0f : exp2_fast(m - top), fb = pm == kNegInf ? 0.0f : exp2_fast(pm - top);
+            o = o * fa + po * fb;
+            l = l * fa + pl * fb;
+            m = top;
+        }
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const int token = col / a.group, head = kvh * a.group + col - token * a.group;
+        store4<T, F32>(a.out, ((int64_t)(span.first + token) * a.heads + head) * c.dim + d, o[0] * inv, o[1] * inv, o[2] * inv,
+                       o[3] * inv);
+    }
+}
+
+// How a call is laid out.  Two waves a SIMD (256 registers each) cover each other's waits and softmax: work groups of 8 waves,
+// whose tiles are read once for 256 columns, where those fill the CUs, else of 4; three parts of q need more registers: one wave
+// a SIMD.  Where even groups of 4 waves leave half of their places empty (a chunk of a prompt behind a long cache, a short
+// prompt), each one's keys are split into parts of four tiles and more, and a second launch joins them.
+constexpr int kCus = 256;
+struct Plan {
+    int waves, splits, tiles;        // tiles: work groups of a kv head
+};
+Plan plan_of(int64_t n_seqs, int64_t n_tokens, int heads, int kv_heads, int dim, int page_size, int64_t max_pages, int window,
+             int n_sink, bool three_parts, bool f32) {
+    const int64_t group = heads / kv_heads, rows = n_tokens * group;
+    const bool one_a_simd = three_parts ? dim > 64 : dim > 128 || (f32 && dim > 64);
+    Plan p{4, 1, 0};
+    if (!three_parts && dim > 64 && dim <= 128 && (rows / 256 + n_seqs) * kv_heads >= kCus) p.waves = 8;
+    const int columns = 32 * p.waves;
+    p.tiles = (int)(rows / columns + n_seqs);
+    if (p.waves == 4) {
+        const int64_t busy = ((rows + columns - 1) / columns) * kv_heads, places = one_a_simd ? kCus : 2 * kCus;
+        int64_t tiles = (max_pages * page_size + kTile - 1) / kTile;
+        if (window > 0) {
+            const int64_t near = ((int64_t)window + columns / group + kTile - 1) / kTile + 2 + ((int64_t)n_sink + kTile - 1) / kTile;
+            tiles = near < tiles ? near : tiles;
+        }
+        int64_t splits = places / busy;
+        splits = splits < tiles / 4 ? splits : tiles / 4;
+        p.splits = (int)(splits < 1 ? 1 : splits > 32 ? 32 : splits);
+    }
+    return p;
+}
+
 template <int T, int DP, bool F32, int WAVES, int PER_SIMD>
-hipError_t launch(PrefillArgs a, hipStream_t s) {
-    a.tiles = (int)((int64_t)a.n_tokens * a.group / (32 * WAVES)) + a.c.n_seqs;
-    const dim3 grid((unsigned)a.tiles * (unsigned)a.c.kv_heads), block(64 * WAVES);
+hipError_t launch(const PrefillArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)a.tiles * (unsigned)a.c.kv_heads, (unsigned)a.splits), block(64 * WAVES);
     if (DP != 112 && a.c.dim == DP)
         hipLaunchKernelGGL((attn_prefill_kernel<T, DP, F32, WAVES, PER_SIMD, DP != 112>), grid, block, 0, s, a);
     else
         hipLaunchKernelGGL((attn_prefill_kernel<T, DP, F32, WAVES, PER_SIMD, false>), grid, block, 0, s, a);
+    if (a.splits > 1)
+        hipLaunchKernelGGL((attn_prefill_join_kernel<T, F32>), dim3(grid.x, 16), dim3(256), 0, s, a, 32 * WAVES);
     return hipGetLastError();
 }
 
-// Two waves a SIMD (256 registers each) cover each other's waits and softmax: work groups of 8 waves, whose tiles are read once
-// for 256 columns, where those fill the CUs, else of 4.  Three parts of q need more registers: one wave a SIMD.
 template <int T, bool F32, int DP>
-hipError_t launch_waves(const PrefillArgs& a, hipStream_t s) {
+hipError_t launch_waves(const PrefillArgs& a, int waves, hipStream_t s) {
     if constexpr (F32 && T == kBf16) {
         return launch<T, DP, F32, 4, 1>(a, s);
     } else {
-        const int64_t groups = ((int64_t)a.n_tokens * a.group / 256 + a.c.n_seqs) * a.c.kv_heads;
-        if (groups >= device_cus()) return launch<T, DP, F32, 8, 2>(a, s);
+        if (waves == 8) return launch<T, DP, F32, 8, 2>(a, s);
         return launch<T, DP, F32, 4, F32 ? 1 : 2>(a, s);
     }
 }
 
 template <int T, bool F32>
-hipError_t launch_dim(const PrefillArgs& a, hipStream_t s) {
+hipError_t launch_dim(const PrefillArgs& a, int waves, hipStream_t s) {
     if (a.c.dim <= 64) return launch<T, 64, F32, 4, 2>(a, s);
-    if (a.c.dim <= 96) return launch_waves<T, F32, 96>(a, s);
-    if (a.c.dim <= 112) return launch_waves<T, F32, 112>(a, s);
-    if (a.c.dim <= 128) return launch_waves<T, F32, 128>(a, s);
+    if (a.c.dim <= 96) return launch_waves<T, F32, 96>(a, waves, s);
+    if (a.c.dim <= 112) return launch_waves<T, F32, 112>(a, waves, s);
+    if (a.c.dim <= 128) return launch_waves<T, F32, 128>(a, waves, s);
+    if (a.c.dim <= 192) return launch<T, 192, F32, 4, 1>(a, s);
     return launch<T, 256, F32, 4, 1>(a, s);
+}
+
+size_t parts_bytes(const Plan& p, int kv_heads, int dim) {
+    return p.splits > 1 ? (size_t)p.tiles * kv_heads * p.splits * (size_t)part_floats(32 * p.waves, dim) * 4 : 0;
 }
 
 }  // namespace
 
-hipError_t launch_attn_prefill(const KvCache& c, int dtype, const AttnArgs& args, hipStream_t s) {
+size_t attn_prefill_workspace_bytes(int64_t n_seqs, int64_t n_tokens, int heads, int kv_heads, int dim, int page_size,
+                                    int64_t max_pages, int window, int n_sink, bool three_parts, bool f32) {
+    return parts_bytes(plan_of(n_seqs, n_tokens, heads, kv_heads, dim, page_size, max_pages, window, n_sink, three_parts, f32),
+                       kv_heads, dim);
+}
+
+hipError_t launch_attn_prefill(const KvCache& c, int dtype, const AttnArgs& args, void* ws, size_t ws_bytes, hipStream_t s) {
+    Plan p = plan_of(c.n_seqs, args.n_tokens, args.heads, c.kv_heads, c.dim, 1 << c.shift, c.max_pages, args.window, args.n_sink,
+                     args.f32 && dtype == kBf16, args.f32);
+    if (!ws || ws_bytes < parts_bytes(p, c.kv_heads, c.dim)) p.splits = 1;
     PrefillArgs a{};
     a.c = c;
     a.q = args.q;
@@ -598,8 +701,11 @@ hipError_t launch_attn_prefill(const KvCache& c, int dtype, const AttnArgs& args
     a.scale2 = args.scale * kLog2e;
     a.window = args.window;
     a.n_sink = args.n_sink;
-    if (dtype == kBf16) return args.f32 ? launch_dim<kBf16, true>(a, s) : launch_dim<kBf16, false>(a, s);
-    return args.f32 ? launch_dim<kF16, true>(a, s) : launch_dim<kF16, false>(a, s);
+    a.tiles = p.tiles;
+    a.splits = p.splits;
+    a.ws = static_cast<float*>(ws);
+    if (dtype == kBf16) return args.f32 ? launch_dim<kBf16, true>(a, p.waves, s) : launch_dim<kBf16, false>(a, p.waves, s);
+    return args.f32 ? launch_dim<kF16, true>(a, p.waves, s) : launch_dim<kF16, false>(a, p.waves, s);
 }
 
 }  // namespace bitnet

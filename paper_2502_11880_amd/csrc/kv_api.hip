@@ -20,7 +20,7 @@ int shift_of(int64_t page_size) {
         if (page_size == (int64_t)1 << s) return s;
     return -1;
 }
-bool cache_dtype(int dtype) { return dtype == BITNET_DTYPE_BF16 || dtype == BITNET_DTYPE_F16; }
+bool cache_dtype_ok(int dtype) { return dtype == BITNET_DTYPE_BF16 || dtype == BITNET_DTYPE_F16; }
 bool heads_ok(int64_t kv_heads, int64_t dim) {
     return kv_heads >= 1 && kv_heads <= kMaxHeads && dim >= 4 && dim <= 256 && dim % 4 == 0;
 }
@@ -35,7 +35,7 @@ size_t page_bytes(int64_t page_size, int64_t kv_heads, int64_t dim, bool values)
 // Sizes and types of a cache, then (where anything is to be done) its pointers.
 int check_cache(const bitnet_kv_cache* c, bool pointers) {
     if (!c) return fail(BITNET_E_INVALID, "null cache");
-    if (!cache_dtype(c->dtype)) return fail(BITNET_E_INVALID, "cache dtype %d: bf16 (1) or f16 (2) is needed", c->dtype);
+    if (!cache_dtype_ok(c->dtype)) return fail(BITNET_E_INVALID, "cache dtype %d: bf16 (1) or f16 (2) is needed", c->dtype);
     if (shift_of(c->page_size) < 0) return fail(BITNET_E_SHAPE, "page_size %d: 16, 32, 64, 128 or 256 is needed", c->page_size);
     if (!heads_ok(c->n_kv_heads, c->head_dim))
         return fail(BITNET_E_SHAPE, "need 1 <= n_kv_heads <= 1024 and head_dim %% 4 == 0, 4 <= head_dim <= 256; got %d heads of %d",
@@ -135,7 +135,7 @@ bitnet_status st(int code) { return (bitnet_status)code; }
 extern "C" {
 
 size_t bitnet_kv_page_bytes(int dtype, int64_t page_size, int64_t n_kv_heads, int64_t head_dim, int values) {
-    if (!cache_dtype(dtype) || shift_of(page_size) < 0 || !heads_ok(n_kv_heads, head_dim)) return 0;
+    if (!cache_dtype_ok(dtype) || shift_of(page_size) < 0 || !heads_ok(n_kv_heads, head_dim)) return 0;
     return page_bytes(page_size, n_kv_heads, head_dim, values != 0);
 }
 
@@ -184,9 +184,23 @@ bitnet_status bitnet_attn_decode(const bitnet_kv_cache* cache, const void* q, in
                          "bitnet_attn_decode launch"));
 }
 
+size_t bitnet_attn_prefill_workspace_bytes(int cache_dtype, int dtype, int64_t n_seqs, int64_t n_tokens, int64_t n_heads,
+                                           int64_t n_kv_heads, int64_t head_dim, int64_t page_size, int64_t max_pages,
+                                           int64_t window, int64_t n_sink) {
+    if (!cache_dtype_ok(cache_dtype) || (dtype != BITNET_DTYPE_F32 && dtype != cache_dtype) || shift_of(page_size) < 0 ||
+        !heads_ok(n_kv_heads, head_dim) || !rows_ok(n_seqs, max_pages, page_size) || n_seqs < 1 || n_heads < 1 ||
+        n_heads > kMaxHeads || n_heads % n_kv_heads || n_tokens < 1 || n_tokens > kMaxTokens ||
+        n_tokens * n_heads > (int64_t)1 << 30 || n_seqs * n_kv_heads > (int64_t)1 << 22 || window < 0 || n_sink < 0)
+        return 0;
+    return bitnet::attn_prefill_workspace_bytes(n_seqs, n_tokens, (int)n_heads, (int)n_kv_heads, (int)head_dim, (int)page_size,
+                                                max_pages, clip(window), clip(n_sink),
+                                                dtype == BITNET_DTYPE_F32 && cache_dtype == BITNET_DTYPE_BF16,
+                                                dtype == BITNET_DTYPE_F32);
+}
+
 bitnet_status bitnet_attn_prefill(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads,
                                   const int32_t* q_start, int64_t n_tokens, float scale, int64_t window, int64_t n_sink,
-                                  void* out, void* stream) {
+                                  void* out, void* ws, size_t ws_bytes, void* stream) {
     const bool work = n_tokens > 0 && cache && cache->n_seqs > 0;
     if (const int e = check_cache(cache, work)) return st(e);
     if (const int e = check_attn(cache, dtype, n_heads, window, n_sink)) return st(e);
@@ -198,9 +212,10 @@ bitnet_status bitnet_attn_prefill(const bitnet_kv_cache* cache, const void* q, i
     if (!q || !out || !q_start) return st(fail(BITNET_E_INVALID, "null pointer argument"));
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(q_start, 4))
         return st(fail(BITNET_E_ALIGN, "q and out need 16-byte alignment, q_start 4-byte"));
+    if (!aligned(ws, 16)) return st(fail(BITNET_E_ALIGN, "ws needs 16-byte alignment"));
     const bitnet::AttnArgs a{q, out, q_start, (int)n_tokens, (int)n_heads, scale, clip(window), clip(n_sink),
                              dtype == BITNET_DTYPE_F32};
-    return st(hip_status(bitnet::launch_attn_prefill(view_of(cache), cache->dtype, a, (hipStream_t)stream),
+    return st(hip_status(bitnet::launch_attn_prefill(view_of(cache), cache->dtype, a, ws, ws_bytes, (hipStream_t)stream),
                          "bitnet_attn_prefill launch"));
 }
 

@@ -141,7 +141,7 @@ struct Elem<kF16> {
     }
     static __device__ __forceinline__ float to(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
     static __device__ __forceinline__ uint32_t pack(float a, float b) {
-        return (uint32_t)from(a) | (uint32_t)from(b) << 16;
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{a, b}), f16x2));
     }
     static __device__ __forceinline__ float add2(uint32_t w, float sum) {
         return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), __builtin_bit_cast(f16x2, 0x3C003C00u), sum, false);
@@ -233,7 +233,10 @@ struct AttnArgs {
 size_t attn_decode_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim, int page_size, int64_t max_pages,
                                    int window, int n_sink);
 hipError_t launch_attn_decode(const KvCache& c, int dtype, const AttnArgs& a, void* ws, hipStream_t s);
-hipError_t launch_attn_prefill(const KvCache& c, int dtype, const AttnArgs& a, hipStream_t s);
+// Prefill: ws null or smaller than this: nothing is split.
+size_t attn_prefill_workspace_bytes(int64_t n_seqs, int64_t n_tokens, int heads, int kv_heads, int dim, int page_size,
+                                    int64_t max_pages, int window, int n_sink, bool three_parts, bool f32);
+hipError_t launch_attn_prefill(const KvCache& c, int dtype, const AttnArgs& a, void* ws, size_t ws_bytes, hipStream_t s);
 
 // A pool: n_layers planes of keys and of values, each n_pages pages of k_bytes / v_bytes.
 struct KvPool {

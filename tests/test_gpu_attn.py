@@ -213,6 +213,44 @@ def test_prefill_long(dtype, io, D):
     _check_prefill(b, 4, [1500, 600], io, seed=13)
 
 
+@pytest.mark.parametrize("H,Hkv,D,page,dtype,io", [(8, 2, 128, 16, "bf16", "f32"), (4, 4, 100, 64, "f16", "f32"), (8, 1, 64, 32, "bf16", "bf16"),
+                                                   (16, 1, 256, 128, "f16", "f16"), (3, 1, 192, 64, "bf16", "bf16"), (5, 1, 80, 256, "f16", "f16")])
+@pytest.mark.parametrize("new,past,window,sinks", [([40], [2600], 0, 0), ([3, 0, 70], [1999, 5, 700], 0, 0), ([17, 1], [2500, 0], 1500, 70)])
+def test_prefill_chunks_whose_keys_are_split(H, Hkv, D, page, dtype, io, new, past, window, sinks):
+    _announce("prefill split", H, Hkv, D, page, dtype, io, new, window)
+    b = M.Batch([n + p for n, p in zip(new, past)], Hkv, D, page, dtype, seed=D + 3)
+    b.table[0, 300 // page] = -1
+    kinds = {"f32": 0, "bf16": 1, "f16": 2}
+    assert B.bitnet_attn_prefill_workspace_bytes(kinds[dtype], kinds[io], len(new), sum(new), H, Hkv, D, page, b.width, window, sinks) > 0
+    _check_prefill(b, H, new, io, seed=21, window=window, sinks=sinks)
+
+
+def test_prefill_split_and_whole_agree_and_take_a_stream():
+    _announce("prefill split on a stream")
+    b = M.Batch([3000], 2, 128, 64, "bf16", seed=22)
+    b.v[0][2990, 1, 5] = float("inf")            # seen by the last queries only
+    b.write(0, 0, b.k[0], b.v[0])
+    k, v, table, lens = b.on(DEV)
+    q = torch.randn(50, 8 * 128, generator=torch.Generator().manual_seed(22)).to(DEV)
+    start = torch.tensor([0, 50], dtype=torch.int32, device=DEV)
+    need = B.bitnet_attn_prefill_workspace_bytes(1, 0, 1, 50, 8, 2, 128, 64, table.shape[1])
+    side, outs = torch.cuda.Stream(), []
+    torch.cuda.synchronize()
+    for ws in (None, torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV), torch.zeros(need, dtype=torch.uint8, device=DEV),
+               torch.zeros(need - 16, dtype=torch.uint8, device=DEV)):
+        out = torch.full_like(q, 7.0)
+        torch.cuda.synchronize()
+        B.bitnet_attn_prefill(q, start, k, v, table, lens, out, 0.09, ws=ws, stream=side)
+        torch.cuda.synchronize()
+        outs.append(out)
+    assert torch.equal(outs[1].isfinite(), outs[0].isfinite()) and not outs[0][40:].isfinite().all() and outs[0][:40].isfinite().all()
+    for o in outs:
+        o.nan_to_num_(0.0, 0.0, 0.0)
+    assert torch.equal(outs[1], outs[2]), "the workspace's contents do not matter"
+    assert torch.equal(outs[0], outs[3]), "too small a workspace: not split"
+    assert float((outs[0] - outs[1]).abs().max()) < 1e-5
+
+
 def test_prefill_more_tokens_than_cached_and_missing_pages():
     _announce("prefill short cache")
     b = M.Batch([5, 40, 100], 1, 64, 16, "bf16", seed=14)

@@ -54,6 +54,15 @@ def test_workspace_bytes():
     for bad in ((1, 33, 8, 128, 16, 4096), (1, 32, 8, 130, 16, 4096), (1, 32, 8, 128, 24, 4096), (1, 0, 8, 128, 16, 4096),
                 (1, 2048, 8, 128, 16, 4096), (1, 32, 8, 128, 16, 0), (1, 32, 8, 128, 16, 1 << 21), (1, 32, 8, 128, 16, 4096, -1, 0)):
         assert f(*bad) == 0
+    g = B.bitnet_attn_prefill_workspace_bytes
+    assert g(1, 1, 1, 64, 32, 8, 128, 64, 130) > 0             # few queries, many keys: split
+    assert g(1, 1, 1, 64, 32, 8, 128, 64, 2) == 0              # few keys
+    assert g(1, 1, 1, 4096, 32, 8, 128, 64, 130) == 0          # queries enough
+    assert g(1, 0, 2, 64, 32, 8, 128, 64, 130, 64, 4) == 0     # a short window
+    for bad in ((0, 0, 1, 64, 32, 8, 128, 64, 130), (1, 2, 1, 64, 32, 8, 128, 64, 130), (1, 1, 0, 64, 32, 8, 128, 64, 130),
+                (1, 1, 1, 0, 32, 8, 128, 64, 130), (1, 1, 1, 64, 31, 8, 128, 64, 130), (1, 1, 1, 64, 32, 8, 126, 64, 130),
+                (1, 1, 1, 64, 32, 8, 128, 60, 130), (1, 1, 1, 64, 32, 8, 128, 64, 0), (1, 1, 1, 64, 32, 8, 128, 64, 130, -1, 0)):
+        assert g(*bad) == 0
     assert B.bitnet_kv_workspace_bytes(0, 1) == 0 and B.bitnet_kv_workspace_bytes(100, -1) == 0
     assert B.bitnet_kv_workspace_bytes(100, 0) >= 1200 and B.bitnet_kv_workspace_bytes(1 << 20, 64) >= 12 << 20
 
@@ -73,8 +82,8 @@ def _decode(cache, q=FAKE, dtype=0, heads=32, window=0, sinks=0, out=FAKE, ws=FA
     return B.lib().bitnet_attn_decode(_ref(cache), q, dtype, heads, 1.0, window, sinks, out, ws, ws_bytes, None)
 
 
-def _prefill(cache, q=FAKE, dtype=0, heads=32, start=FAKE, n=3, window=0, sinks=0, out=FAKE):
-    return B.lib().bitnet_attn_prefill(_ref(cache), q, dtype, heads, start, n, 1.0, window, sinks, out, None)
+def _prefill(cache, q=FAKE, dtype=0, heads=32, start=FAKE, n=3, window=0, sinks=0, out=FAKE, ws=None):
+    return B.lib().bitnet_attn_prefill(_ref(cache), q, dtype, heads, start, n, 1.0, window, sinks, out, ws, 0, None)
 
 
 @pytest.mark.parametrize("fault,status", CACHE_FAULTS)
@@ -111,6 +120,7 @@ def test_attention_refusals():
     assert _prefill(c, n=-1) == SHAPE and _prefill(c, n=(1 << 24) + 1) == SHAPE and _prefill(c, heads=1024, n=(1 << 20) + 1) == SHAPE
     assert _prefill(_cache(n_seqs=1 << 20), n=3) == SHAPE
     assert _prefill(c, n=0, q=None, out=None) == OK
+    assert _prefill(c, ws=FAKE + 4) == ALIGN
 
 
 def test_page_call_refusals():
