@@ -295,7 +295,8 @@ size_t bitnet_kv_page_bytes(int dtype, int64_t page_size, int64_t n_kv_heads, in
 bitnet_status bitnet_kv_append(const bitnet_kv_cache* cache, const void* k, const void* v, int src_dtype,
                                const int32_t* q_start, int64_t n_tokens, void* stream);
 
-/* Workspace bytes bitnet_attn_decode needs (0 is a valid answer; 0 also for unsupported sizes). */
+/* Workspace bytes with which bitnet_attn_decode serves n_seqs sequences and fewer (0 is a valid answer; 0 also for unsupported
+ * sizes). */
 size_t bitnet_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,
                                           int64_t page_size, int64_t max_pages, int64_t window, int64_t n_sink);
 
@@ -307,7 +308,8 @@ size_t bitnet_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64
  *   q, out    device [n_seqs, n_heads, head_dim] of dtype BITNET_DTYPE_F32 or the cache's.  With F32 the products and the
  *             softmax keep 32-bit precision whatever the cache's type; softmax statistics and sums are 32 bits always.
  *   ws        bitnet_attn_decode_workspace_bytes(...) bytes (partial results of long sequences, which are split and joined),
- *             any contents on entry, nothing kept between calls; NULL where that is 0.
+ *             any contents on entry, nothing kept between calls; may be NULL where that is 0, or where n_seqs * n_kv_heads
+ *             is 512 and more and a row has at most 2048 visible keys (then no row is split).
  *   n_heads % n_kv_heads == 0, n_heads <= 1024.  Reductions run in a fixed order: the same call gives the same bits.
  *   Values that are not finite reach only the outputs of heads whose query sees them.
  */

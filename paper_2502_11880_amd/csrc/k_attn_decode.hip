@@ -574,11 +574,14 @@ bool rows_split(int64_t n_seqs, int heads, int kv_heads, int page_size, int64_t 
 
 }  // namespace
 
-size_t attn_decode_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim, int page_size, int64_t max_pages,
-                                   int window, int n_sink) {
-    if (!rows_split(n_seqs, heads, kv_heads, page_size, max_pages, window, n_sink)) return 0;
+size_t attn_decode_workspace_bytes(int heads, int kv_heads, int dim, int page_size, int64_t max_pages, int window, int n_sink) {
+    if (most_units(max_pages, page_size, window, n_sink) <= kWholeUnits) return 0;
     const int group = heads / kv_heads;
     return (size_t)kPrefixBytes + (size_t)(2 * kMaxGroups * slot_floats(group < 16 ? group : 16, dim)) * 4;
+}
+
+bool attn_decode_splits(int64_t n_seqs, int heads, int kv_heads, int page_size, int64_t max_pages, int window, int n_sink) {
+    return rows_split(n_seqs, heads, kv_heads, page_size, max_pages, window, n_sink);
 }
 
 hipError_t launch_attn_decode(const KvCache& c, int dtype, const AttnArgs& args, void* ws, hipStream_t s) {

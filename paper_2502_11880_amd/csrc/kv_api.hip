@@ -163,7 +163,7 @@ size_t bitnet_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64
     if (shift_of(page_size) < 0 || !heads_ok(n_kv_heads, head_dim) || !rows_ok(n_seqs, max_pages, page_size) || n_heads < 1 ||
         n_heads > kMaxHeads || n_heads % n_kv_heads || window < 0 || n_sink < 0)
         return 0;
-    return bitnet::attn_decode_workspace_bytes(n_seqs, (int)n_heads, (int)n_kv_heads, (int)head_dim, (int)page_size, max_pages,
+    return bitnet::attn_decode_workspace_bytes((int)n_heads, (int)n_kv_heads, (int)head_dim, (int)page_size, max_pages,
                                                clip(window), clip(n_sink));
 }
 
@@ -175,8 +175,12 @@ bitnet_status bitnet_attn_decode(const bitnet_kv_cache* cache, const void* q, in
     if (!work) return st(hip_status(hipSuccess, ""));
     if (!q || !out) return st(fail(BITNET_E_INVALID, "null pointer argument"));
     if (!aligned(q, 16) || !aligned(out, 16)) return st(fail(BITNET_E_ALIGN, "q and out need 16-byte alignment"));
-    const size_t need = bitnet_attn_decode_workspace_bytes(cache->n_seqs, n_heads, cache->n_kv_heads, cache->head_dim,
-                                                           cache->page_size, cache->max_pages, window, n_sink);
+    // a call whose rows stay whole needs none
+    const bool splits = bitnet::attn_decode_splits(cache->n_seqs, (int)n_heads, cache->n_kv_heads, cache->page_size,
+                                                   cache->max_pages, clip(window), clip(n_sink));
+    const size_t need = splits ? bitnet_attn_decode_workspace_bytes(cache->n_seqs, n_heads, cache->n_kv_heads, cache->head_dim,
+                                                                    cache->page_size, cache->max_pages, window, n_sink)
+                               : 0;
     if (const int e = check_workspace(ws, ws_bytes, need)) return st(e);
     const bitnet::AttnArgs a{q, out, nullptr, (int)cache->n_seqs, (int)n_heads, scale, clip(window), clip(n_sink),
                              dtype == BITNET_DTYPE_F32};

@@ -229,9 +229,10 @@ struct AttnArgs {
     int window, n_sink;       // window 0: none
     bool f32;                 // q and out in 32 bits, else in the cache's type
 };
-// Decode: bytes for the partial results of rows that are split (0 where none can be).
-size_t attn_decode_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim, int page_size, int64_t max_pages,
-                                   int window, int n_sink);
+// Decode: bytes for the partial results of rows that are split (0 where none can be, whatever the number of sequences), and
+// whether a call splits any.
+size_t attn_decode_workspace_bytes(int heads, int kv_heads, int dim, int page_size, int64_t max_pages, int window, int n_sink);
+bool attn_decode_splits(int64_t n_seqs, int heads, int kv_heads, int page_size, int64_t max_pages, int window, int n_sink);
 hipError_t launch_attn_decode(const KvCache& c, int dtype, const AttnArgs& a, void* ws, hipStream_t s);
 // Prefill: ws null or smaller than this: nothing is split.
 size_t attn_prefill_workspace_bytes(int64_t n_seqs, int64_t n_tokens, int heads, int kv_heads, int dim, int page_size,
