@@ -3,6 +3,7 @@
 // between host and device or synchronises.
 #include "bitnet_mi355x.h"
 #include "bitnet_internal.hpp"
+#include "status.hpp"
 
 #include <cstdarg>
 #include <cstdio>

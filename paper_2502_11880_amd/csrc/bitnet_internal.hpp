@@ -10,10 +10,6 @@ namespace bitnet {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef unsigned int v4u __attribute__((ext_vector_type(4)));
 
-// The C entry points' status and detail text (bitnet_api.hip).
-int fail(int status, const char* fmt, ...);
-int hip_status(hipError_t e, const char* what);
-
 constexpr int kRowsPerGroup = 16;     // weight rows per MFMA tile (both layouts)
 constexpr int kSubK = 64;             // k per 16x16x64 int8 MFMA
 constexpr int kI2sBlockK = 256;       // I2_S block: up to four 64-k sub-tiles, 1 KiB per row group

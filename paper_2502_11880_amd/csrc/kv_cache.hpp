@@ -10,6 +10,7 @@
 #pragma once
 
 #include "bitnet_internal.hpp"
+#include "status.hpp"
 
 namespace bitnet {
 
