@@ -334,3 +334,51 @@ def test_cache_past_four_gib():
     torch.cuda.synchronize()
     assert torch.equal(k[pages - 2, :, :, 599 - 512].reshape(-1), new[0].to(dtype))
     assert torch.equal(v[pages - 2, :, (599 - 512) // 8, :, (599 - 512) % 8].reshape(-1), -new[0].to(dtype))
+
+
+@pytest.mark.parametrize("dtype,io", [("bf16", "f32"), ("f16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("H,Hkv", [(16, 1), (40, 2), (33, 1)])
+def test_decode_widest_heads_with_full_tiles(H, Hkv, dtype, io):
+    _announce("decode 256 channels", H, Hkv, dtype, io)
+    _check_decode(M.Batch([1300, 9, 200, 0], Hkv, 256, 32, dtype, seed=23), H, io, seed=23)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.11])
+def test_scales_of_zero_and_below(scale):
+    _announce("scale", scale)
+    b = M.Batch([700, 90], 2, 64, 16, "bf16", seed=24)
+    _check_decode(b, 8, "f32", seed=24, scale=scale)
+    q = torch.randn(150, 8 * 64, generator=torch.Generator().manual_seed(25))
+    out = _prefill(b, 8, q.to(DEV), [100, 50], scale).cpu().view(150, 8, 64)
+    for rows, s in ((slice(0, 100), 0), (slice(100, 150), 1)):
+        L, n = b.lens[s], rows.stop - rows.start
+        want, tol = M.attention(q[rows].view(n, 8, 64), b.k[s], b.v[s], M.visible(torch.arange(L - n, L), L, 0, 0), scale, 2.0 ** -23, 0.0)
+        M.check(out[rows], want, tol, f"sequence {s}")
+
+
+def test_prefill_of_a_chunk_in_a_graph():
+    _announce("prefill in a graph")
+    b = M.Batch([3000, 1200], 2, 128, 64, "bf16", seed=26)
+    k, v, table, lens = b.on(DEV)
+    q = torch.randn(30, 8 * 128, generator=torch.Generator().manual_seed(26)).to(DEV)
+    start = torch.tensor([0, 20, 30], dtype=torch.int32, device=DEV)
+    out = torch.empty_like(q)
+    need = B.bitnet_attn_prefill_workspace_bytes(1, 0, 2, 30, 8, 2, 128, 64, table.shape[1])
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    call = lambda: B.bitnet_attn_prefill(q, start, k, v, table, lens, out, 0.09, ws=ws)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for step in range(4):                    # other queries, another length: what the graph reads is on the device
+        q.copy_(torch.randn(30, 8 * 128, generator=torch.Generator().manual_seed(30 + step)))
+        lens[0] = 3000 - 7 * step
+        call()
+        torch.cuda.synchronize()
+        want = out.clone()
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), f"replay {step}"
