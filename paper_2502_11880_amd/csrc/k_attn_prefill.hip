@@ -130,26 +130,29 @@ struct Prefill {
     // A tile's words on their way to registers: word tid + i threads of the keys (chunk-major: a wave reads 64 keys of a chunk)
     // and of the values.  In pages of 64 and more a tile is one run of either but for the keys' chunks, and a thread's place in
     // it never changes.
+    // Words past the last chunk or channel are read again from the last one and not stored: a load that may or may not
+    // be on its way would make every wait one for all of them (heads of 96 with 8 waves: 142 us against 102).
     static constexpr bool kEven = FULL && kWords % kThreads == 0;
+    __device__ __forceinline__ int chunk_of(int i) const { return uniform(tid / kTile) + i * WAVES; }
+    __device__ __forceinline__ int held_chunk(int i) const {
+        const int chunk = chunk_of(i);
+        return kEven || chunk < a.c.chunks ? chunk : a.c.chunks - 1;
+    }
+    __device__ __forceinline__ int held_word(int i) const {
+        const int w = tid + i * kThreads, last = (kTile / 8) * channels() - 1;
+        return kEven || w < last ? w : last;
+    }
     __device__ __forceinline__ void load_keys(int tile, const Pages p) {
         const KvCache& c = a.c;
-        const int key = tile * kTile, chunk0 = uniform(tid / kTile), at = tid & 63;
-        const uint16_t* kp = c.shift >= 6 ? kbase + (int64_t)p.p0 * c.k_page + (chunk0 * ps + (key & (ps - 1))) * 8 : nullptr;
+        const int key = tile * kTile, at = tid & 63;
         if (c.shift >= 6) {
+            const uint16_t* kp = kbase + (int64_t)p.p0 * c.k_page + (key & (ps - 1)) * 8;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                v4u x = {0u, 0u, 0u, 0u};
-                if (kEven || chunk0 + i * WAVES < c.chunks) x = load16(kp + i * WAVES * ps * 8, (uint32_t)at * 16);
-                stage_k[i] = x;
-            }
+            for (int i = 0; i < kLoads; ++i) stage_k[i] = load16(kp + held_chunk(i) * ps * 8, (uint32_t)at * 16);
         } else {
-            kp = kbase + (int64_t)of_quarter(at >> 4, p.p0, p.p1, p.p2, p.p3) * c.k_page + (chunk0 * ps + ((key + at) & (ps - 1))) * 8;
+            const uint16_t* kp = kbase + (int64_t)of_quarter(at >> 4, p.p0, p.p1, p.p2, p.p3) * c.k_page + ((key + at) & (ps - 1)) * 8;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                v4u x = {0u, 0u, 0u, 0u};
-                if (kEven || chunk0 + i * WAVES < c.chunks) x = load16(kp + i * WAVES * ps * 8, 0);
-                stage_k[i] = x;
-            }
+            for (int i = 0; i < kLoads; ++i) stage_k[i] = load16(kp + held_chunk(i) * ps * 8, 0);
         }
     }
     __device__ __forceinline__ void load_values(int tile, const Pages p) {
@@ -159,19 +162,15 @@ struct Prefill {
             const uint16_t* vp = vbase + (int64_t)p.p0 * c.v_page + (key & (ps - 1)) * channels();
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                v4u x = {0u, 0u, 0u, 0u};
-                if (kEven || tid + i * kThreads < (kTile / 8) * channels()) x = load16(vp + i * kThreads * 8, (uint32_t)tid * 16);
-                stage_v[i] = x;
+                if constexpr (kEven) stage_v[i] = load16(vp + i * kThreads * 8, (uint32_t)tid * 16);
+                else stage_v[i] = load16(vp, (uint32_t)held_word(i) * 16);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int w = tid + i * kThreads, eight = eight_of(w), d = w - eight * channels();
+                const int w = held_word(i), eight = eight_of(w), d = w - eight * channels();
                 const int page = of_quarter((eight >> 1) & 3, p.p0, p.p1, p.p2, p.p3);
-                v4u x = {0u, 0u, 0u, 0u};
-                if (kEven || w < (kTile / 8) * channels())
-                    x = load16(vbase + (int64_t)page * c.v_page + ((key + 8 * eight) & (ps - 1)) * channels(), (uint32_t)d * 16);
-                stage_v[i] = x;
+                stage_v[i] = load16(vbase + (int64_t)page * c.v_page + ((key + 8 * eight) & (ps - 1)) * channels(), (uint32_t)d * 16);
             }
         }
     }
@@ -179,14 +178,15 @@ struct Prefill {
     // the product.
     __device__ __forceinline__ void store_keys(int buf) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) lds.k[buf][tid + i * kThreads] = __builtin_bit_cast(uint4, stage_k[i]);
+        for (int i = 0; i < kLoads; ++i)
+            if (kEven || chunk_of(i) < a.c.chunks) lds.k[buf][tid + i * kThreads] = __builtin_bit_cast(uint4, stage_k[i]);
     }
     __device__ __forceinline__ void store_values(int buf, int tile, uint32_t there) {
         if (there != 15 || tile < group_first || tile > group_last) {
             uint32_t odd = 0;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int eight = eight_of(tid + i * kThreads);
+                const int eight = eight_of(held_word(i));
                 int held = len - (tile * kTile + 8 * eight);
                 held = (there >> ((eight >> 1) & 3)) & 1 ? held : 0;
 #pragma unroll
@@ -310,17 +310,19 @@ struct Prefill {
         }
     }
 
-    // Scores, softmax and product of every tile, the next tile's words on their way.
-    __device__ __forceinline__ void all_tiles(const v4u (&qf)[kQParts][kSteps], float gain, float& m, float& l, v16f (&o)[kBlocks]) {
-        Pages pages{};                                    // of the tile after the one being loaded
-        uint32_t there = 0;
-        if (n_tiles > 0) {
-            pages = ask_pages(tile_of(0));
-            there = settle(pages);
-            load_keys(tile_of(0), pages);
-            load_values(tile_of(0), pages);
-            if (n_tiles > 1) pages = ask_pages(tile_of(1));
-        }
+    // The first tile's words on their way, and the pages of the second asked for.
+    __device__ __forceinline__ void begin(Pages& pages, uint32_t& there) {
+        if (n_tiles <= 0) return;
+        there = settle(pages);
+        load_keys(tile_of(0), pages);
+        load_values(tile_of(0), pages);
+        if (n_tiles > 1) pages = ask_pages(tile_of(1));
+    }
+
+    // Scores, softmax and product of every tile, the next tile's words on their way.  pages: of the tile after the one being
+    // loaded; there: quarters of the latter that have one.
+    __device__ __forceinline__ void all_tiles(Pages pages, uint32_t there, const v4u (&qf)[kQParts][kSteps], float gain, float& m,
+                                              float& l, v16f (&o)[kBlocks]) {
         __syncthreads();
         if (n_tiles > 0) {
             store_keys(0);
@@ -515,16 +517,33 @@ struct Prefill {
         group_last = (pos_lo + 1) / kTile - 1;
 
         if (tid == 0) lds.odd = 0;
+        if constexpr (!FULL) {                            // chunks past D: q has zeros there, and 0 times them has to be 0
+            for (int w = c.chunks * kTile + tid; w < DP / 8 * kTile; w += kThreads) lds.k[0][w] = lds.k[1][w] = make_uint4(0, 0, 0, 0);
+        }
+        // A work group starts with three loads that follow each other (pages, then keys and values); q comes beside them.
+        Pages pages{};
+        uint32_t there = 0;
+        if (n_tiles > 0) pages = ask_pages(tile_of(0));
+        float4 x[kSteps][2];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int d = 8 * (2 * s + half);
+            x[s][0] = x[s][1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (FULL || d < dim) x[s][0] = load4<T, F32>(a.q, row + d);
+            if (FULL || d + 4 < dim) x[s][1] = load4<T, F32>(a.q, row + d + 4);
+        }
+        if constexpr (kQParts < 3) begin(pages, there);
         // q as operands: chunk 2 s + half of this lane's column, in parts.  The factor of the scores is positive (a negative
         // scale changes q's sign, a scale of 0 makes q 0), so that it can be applied after the maximum.
         v4u qf[kQParts][kSteps];
         float gain = fabsf(a.scale2), up = a.scale2 < 0.0f ? -1.0f : a.scale2 == 0.0f ? 0.0f : 1.0f;
         if constexpr (F32 && T == kF16) {
             float top = 0.0f;
-            for (int d = 4 * half; d < dim; d += 8) {
-                const float4 x = load4<T, F32>(a.q, row + d);
-                top = fmaxf(top, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(x.z), fabsf(x.w))));
-            }
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    top = fmaxf(top, fmaxf(fmaxf(fabsf(x[s][i].x), fabsf(x[s][i].y)), fmaxf(fabsf(x[s][i].z), fabsf(x[s][i].w))));
             const float g = row_gain(max_xor32(top));
             up *= g;
             gain /= g;
@@ -532,23 +551,19 @@ struct Prefill {
         if (a.scale2 == 0.0f) gain = 1.0f;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            const int d = 8 * (2 * s + half);
-            float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f), y = x;
-            if (FULL || d < dim) x = load4<T, F32>(a.q, row + d);
-            if (FULL || d + 4 < dim) y = load4<T, F32>(a.q, row + d + 4);
-            x.x *= up; x.y *= up; x.z *= up; x.w *= up;
-            y.x *= up; y.y *= up; y.z *= up; y.w *= up;
-            if constexpr (kQParts == 1) {
-                qf[0][s] = v4u{Elem<T>::pack(x.x, x.y), Elem<T>::pack(x.z, x.w), Elem<T>::pack(y.x, y.y),
-                               Elem<T>::pack(y.z, y.w)};
-            } else {
+            float4 u = x[s][0], w = x[s][1];
+            u.x *= up; u.y *= up; u.z *= up; u.w *= up;
+            w.x *= up; w.y *= up; w.z *= up; w.w *= up;
 #pragma unroll
-                for (int p = 0; p < kQParts; ++p)
-                    qf[p][s] = v4u{Elem<T>::part(x.x, x.y), Elem<T>::part(x.z, x.w), Elem<T>::part(y.x, y.y),
-                                   Elem<T>::part(y.z, y.w)};
+            for (int p = 0; p < kQParts; ++p) {
+                if constexpr (kQParts == 1)
+                    qf[p][s] = v4u{Elem<T>::pack(u.x, u.y), Elem<T>::pack(u.z, u.w), Elem<T>::pack(w.x, w.y), Elem<T>::pack(w.z, w.w)};
+                else
+                    qf[p][s] = v4u{Elem<T>::part(u.x, u.y), Elem<T>::part(u.z, u.w), Elem<T>::part(w.x, w.y), Elem<T>::part(w.z, w.w)};
             }
         }
 
+        if constexpr (kQParts == 3) begin(pages, there);
         float m = kNegInf, l = 0.0f;
         v16f o[kBlocks];
 #pragma unroll
@@ -556,7 +571,7 @@ struct Prefill {
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
 
-        all_tiles(qf, gain, m, l, o);
+        all_tiles(pages, there, qf, gain, m, l, o);
         if (uniform(lds.odd)) {
             careful(qf, gain, used, row);
             return;
@@ -612,10 +627,17 @@ __global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, i
     }
 }
 
-// How a call is laid out.  Two waves a SIMD (256 registers each) cover each other's waits and softmax: work groups of 8 waves,
-// whose tiles are read once for 256 columns, where those fill the CUs, else of 4; three parts of q need more registers: one wave
-// a SIMD.  Where even groups of 4 waves leave half of their places empty (a chunk of a prompt behind a long cache, a short
-// prompt), each one's keys are split into parts of four tiles and more, and a second launch joins them.
+// How a call is laid out.  Two waves a SIMD (256 registers each) cover each other's waits and softmax: one work group of 8 waves
+// a CU, whose tiles are read once for 256 columns, or two of 4, of which one starts, ends or waits at a barrier while the
+// other computes.  The large ones win where work groups go through many keys, the small ones where they are short (us, 8 waves /
+// 4, bf16, 32 heads of 128: 4096 tokens 151 / 160, three prompts of 2048 155 / 144, eight of 1024 120 / 117, sixteen of 512
+// 89 / 83; 8192 tokens behind a window of 4096 447 / 455, 2048 309 / 290, 1024 190 / 182; heads of 100, 512: 134 / 129) or
+// where 8 waves do not divide a tile evenly (heads of 96: 124 / 102; of 100 without a window the large ones stay ahead, 170 / 176).
+// Two parts of q fit 256 registers only in the large ones (f16 heads of 100 behind a window 174 / 220), three in neither: one
+// wave a SIMD (8192 tokens, window 1024: 465; 8 waves with what does not fit in memory 525).
+// Where even groups of 4 waves leave half of their places empty (a chunk of a prompt behind a long cache, a short prompt),
+// each one's keys are split into parts of four tiles and more, and a second launch joins them (64 tokens behind 8000: 184 us
+// whole, 30 split).
 constexpr int kCus = 256;
 struct Plan {
     int waves, splits, tiles;        // tiles: work groups of a kv head
@@ -625,7 +647,10 @@ Plan plan_of(int64_t n_seqs, int64_t n_tokens, int heads, int kv_heads, int dim,
     const int64_t group = heads / kv_heads, rows = n_tokens * group;
     const bool one_a_simd = three_parts ? dim > 64 : dim > 128 || (f32 && dim > 64);
     Plan p{4, 1, 0};
-    if (!three_parts && dim > 64 && dim <= 128 && (rows / 256 + n_seqs) * kv_heads >= kCus) p.waves = 8;
+    constexpr int kLongKeys = 2048;
+    const bool brief = (window > 0 && window <= kLongKeys) || (dim == 128 && n_tokens <= kLongKeys * n_seqs);
+    const bool wide = !three_parts && dim > 64 && dim <= 128 && (f32 || (dim > 96 && !brief));
+    if (wide && (rows / 256 + n_seqs) * kv_heads >= kCus) p.waves = 8;
     const int columns = 32 * p.waves;
     p.tiles = (int)(rows / columns + n_seqs);
     if (p.waves == 4) {
@@ -658,6 +683,8 @@ template <int T, bool F32, int DP>
 hipError_t launch_waves(const PrefillArgs& a, int waves, hipStream_t s) {
     if constexpr (F32 && T == kBf16) {
         return launch<T, DP, F32, 4, 1>(a, s);
+    } else if constexpr (!F32 && DP == 96) {
+        return launch<T, DP, F32, 4, 2>(a, s);
     } else {
         if (waves == 8) return launch<T, DP, F32, 8, 2>(a, s);
         return launch<T, DP, F32, 4, F32 ? 1 : 2>(a, s);

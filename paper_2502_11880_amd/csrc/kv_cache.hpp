@@ -148,10 +148,12 @@ struct Elem<kF16> {
         return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), __builtin_bit_cast(f16x2, 0x3C003C00u), sum, false);
     }
     static __device__ __forceinline__ uint32_t part(float& a, float& b) {
-        const uint16_t x = from(a), y = from(b);
-        a -= to(x);
-        b -= to(y);
-        return (uint32_t)x | (uint32_t)y << 16;
+        const f16x2 x = __builtin_convertvector((v2f{a, b}), f16x2);
+        const uint32_t w = __builtin_bit_cast(uint32_t, x);
+        // a - x[0] and b - x[1], exact, from the 16 bits in place (the compiler would convert them first)
+        asm("v_fma_mix_f32 %0, -%1, 1.0, %2 op_sel_hi:[1,0,0]" : "=v"(a) : "v"(w), "v"(a));
+        asm("v_fma_mix_f32 %0, -%1, 1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(b) : "v"(w), "v"(b));
+        return w;
     }
     static __device__ __forceinline__ v4f mfma16(v4u a, v4u b, v4f c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
