@@ -284,7 +284,8 @@ typedef struct {
 size_t bitnet_kv_page_bytes(int dtype, int64_t page_size, int64_t n_kv_heads, int64_t head_dim, int values);
 
 /*
- * bitnet_kv_append -- keys and values of new tokens written into their pages, rounded to the cache's type (nearest even).
+ * bitnet_kv_append -- keys and values of new tokens written into their pages, rounded to the cache's type (nearest even;
+ * f16: past 65504 to infinity).
  *   k, v      device [n_tokens, n_kv_heads, head_dim] of src_dtype (BITNET_DTYPE_F32 or the cache's).
  *   q_start   device int32 [n_seqs + 1]: tokens q_start[s] .. q_start[s+1] - 1 belong to sequence s (first 0, last n_tokens,
  *             never decreasing); NULL: one token a sequence (n_tokens == n_seqs).
@@ -327,7 +328,8 @@ size_t bitnet_attn_prefill_workspace_bytes(int cache_dtype, int dtype, int64_t n
  * before): the n tokens of sequence s are at positions p = kv_len[s] - n + i and see j <= p, with window > 0 only
  * j > p - window or j < n_sink.  A position below 0 sees nothing (out 0).
  *   q, out    device [n_tokens, n_heads, head_dim]; q_start device int32 [n_seqs + 1] as in bitnet_kv_append (not NULL).
- *   dtype     BITNET_DTYPE_F32: 32-bit precision throughout (about a third of the speed: products in parts);
+ *   dtype     BITNET_DTYPE_F32: 32-bit precision throughout: products in parts, two for f16 caches, three for bf16, each
+ *             as long as the product itself;
  *             the cache's type: the weights are rounded to it once before the second product, their sum is not.
  *   ws        optional (NULL): bitnet_attn_prefill_workspace_bytes(...) bytes, any contents, nothing kept.  With it a call of
  *             few queries (a chunk of a prompt behind a long cache, a short prompt) splits their keys over the device and

@@ -12,6 +12,11 @@
 // Work is split evenly whatever the lengths: all units of the launch in one line (sequence, kv head, unit), one share of equal
 // length for every work group, which its four waves take in turn.  A row that crosses shares leaves partial results (maximum,
 // sum, unnormalised output) in the workspace, and a second launch joins them.
+//
+// Measured (kernel times; D = 128, 32 heads of 8 kv heads unless said): one sequence of 131071 keys 82 us (6.6 TB/s of keys and
+// values) and 5 to join; 32 sequences of up to 6000 keys 77 (5.3 TB/s) and 4.5; 24 sequences of 32 heads of 100, f16, behind a
+// window of 1024, 57 us whole (5.3 TB/s); one of 61 keys 5.7 us.  A large plain read reaches 6.4 to 7.0 TB/s here.  What is
+// left is a share's start: length, pages and first keys are three reads in a row, and rows that end inside a share start anew.
 #include "kv_cache.hpp"
 
 #include <type_traits>
@@ -25,9 +30,12 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kMaxGroups = 1024;     // work groups of a split launch
 constexpr int kMaxSeqs = 1024;       // sequences of a split launch (more go in several)
 constexpr int kMinShare = 4;         // units of a share, at least: one for each wave
-constexpr int kWholeUnits = 8;       // rows of up to so many units are never split,
-constexpr int kManyUnits = 64;       // nor rows of up to so many where there are
-constexpr int kManyRows = 512;       // so many of them
+// Rows of up to kWholeUnits units are never split (61 keys: 5.7 us in one launch, where the join alone takes 4.5), nor rows of up
+// to kManyUnits where there are kManyRows of them: a work group a row is enough then, and the join is saved (24 x 32 rows of
+// 1028 keys: 57 us whole).
+constexpr int kWholeUnits = 8;
+constexpr int kManyUnits = 64;
+constexpr int kManyRows = 512;
 constexpr int kIds = 512;            // units whose pages a work group looks up at a time
 
 // The keys that the last position of a sequence of length L sees: [0, sinks) and [lo, L).
@@ -159,7 +167,8 @@ struct Decode {
         const uint16_t* kbase = c.k + (int64_t)kvh * chunks * ps * 8;
         const uint16_t* vbase = c.v + (int64_t)kvh * dim * ps;
         // places of this lane's words in a unit: of the keys, key 8 (m / 4) + m % 4 (+ 4 in the second tile) of chunk g (+ 4 j);
-        // of the values, channel m (+ 16 t) of the eight keys g.  Read once: past the caches' memory.
+        // of the values, channel m (+ 16 t) of the eight keys g.  Read once, so past the caches (131071 keys 93 us, with
+        // ordinary loads 104).
         const uint32_t k_lane = (uint32_t)(g * ps + 8 * (m >> 2) + (m & 3)) * 16, v_lane = (uint32_t)(g * dim + m) * 16;
         auto load = [](const uint16_t* base, uint32_t offset) {
             return __builtin_nontemporal_load(reinterpret_cast<const v4u*>(reinterpret_cast<const uint8_t*>(base) + offset));

@@ -4,13 +4,17 @@
 // because that is a word of the values' layout: a thread collects one channel of the eight tokens (its neighbours the next
 // channels: whole rows are read) and writes 16 bytes; keys go as one thread a token and eight channels, tokens side by side.
 // A unit that starts or ends inside such a word writes its values as single elements.
+//
+// Measured: five prompts, 8461 tokens in all, 32 heads of 100, 32 bits into f16, 74 us (325 MB, 4.4 TB/s; a large copy
+// reaches 4.9); one token each of 64 sequences 5 us, of which a launch that does nothing takes 1.7: four reads in a row
+// (length, page, row) before the first write.
 #include "kv_cache.hpp"
 
 namespace bitnet {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWantGroups = 4096;    // sixteen work groups a CU (five prompts of 7400 tokens: 74 us against 78 with eight)
+constexpr int kWantGroups = 4096;    // sixteen work groups a CU (those prompts: 74 us, with eight a CU 78, four 85, 32 74)
 
 // Units of sequence b start at floor(q_start[b] / 8) + 2 b: its tokens touch at most ceil(n / 8) + 1 of them, which never
 // reach the next sequence's, so no prefix sum is needed (a few units stay empty).
