@@ -556,6 +556,8 @@ hipError_t launch(const DecodeArgs& a, bool split, hipStream_t s) {
     return a.c.shift == 4 ? launch_page<T, DP, F32, FULL, true>(a, split, s) : launch_page<T, DP, F32, FULL, false>(a, split, s);
 }
 
+// Heads of exactly 64 and 128 channels load without asking whether a word is there.  Of 256 they do not: with nothing to hold them
+// back the next unit's loads come so early that registers spill (8 sequences of up to 8000 keys: 66 us as it is, 72 so).
 template <int T, bool F32>
 hipError_t launch_dim(const DecodeArgs& a, bool split, hipStream_t s) {
     if (a.c.dim <= 64) return a.c.dim == 64 ? launch<T, 64, F32, true>(a, split, s) : launch<T, 64, F32, false>(a, split, s);
