@@ -310,7 +310,7 @@ size_t bitnet_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64
  *             softmax keep 32-bit precision whatever the cache's type; softmax statistics and sums are 32 bits always.
  *   ws        bitnet_attn_decode_workspace_bytes(...) bytes (partial results of long sequences, which are split and joined),
  *             any contents on entry, nothing kept between calls; may be NULL where that is 0, or where n_seqs * n_kv_heads
- *             is 512 and more and a row has at most 2048 visible keys (then no row is split).
+ *             is 512 and more and max_pages * page_size at most 2048 or window (> 0) + n_sink at most 1920 (then no row is split).
  *   n_heads % n_kv_heads == 0, n_heads <= 1024.  Reductions run in a fixed order: the same call gives the same bits.
  *   Values that are not finite reach only the outputs of heads whose query sees them.
  */

@@ -382,3 +382,17 @@ def test_prefill_of_a_chunk_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want), f"replay {step}"
+
+
+@pytest.mark.parametrize("window,sinks,width", [(1919, 1, 80), (0, 0, 64), (1000, 920, 80)])
+def test_decode_of_many_short_rows_needs_no_workspace(window, sinks, width):
+    _announce("decode without a workspace", window, sinks)
+    lens = [2040 if i % 50 == 0 else (13 * i) % 90 for i in range(512)]
+    b = M.Batch(lens, 1, 64, 32, "bf16", seed=27, width=width)
+    q = torch.randn(512, 2 * 64, generator=torch.Generator().manual_seed(27)).to(DEV)
+    t = b.on(DEV)
+    out = torch.full_like(q, float("nan"))
+    B.bitnet_attn_decode(q, *t, out, 0.1, window, sinks, None)
+    torch.cuda.synchronize()
+    assert torch.equal(out, _decode(b, 2, q, 0.1, window, sinks, tensors=t))
+    _check_decode(b, 2, "f32", seed=28, window=window, sinks=sinks, rows=[0, 1, 50, 99, 500, 511])
