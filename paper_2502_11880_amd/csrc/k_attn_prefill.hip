@@ -487,7 +487,7 @@ struct Prefill {
         span = {uniform(span.first), uniform(span.count)};
         const int col0 = (id - uniform(first_tile(a.q_start, b, a.group, kColumns))) * kColumns;
         const int columns = span.count * a.group;
-        if (col0 >= columns) return;
+        if (col0 < 0 || col0 >= columns) return;          // below 0: before the first sequence's tokens, or offsets that decrease
         len = uniform(seq_len(c, b));
         const int p0 = len - span.count;                  // position of the first token (below 0: it sees nothing)
         table = c.table + (int64_t)b * c.max_pages;
@@ -611,6 +611,7 @@ __global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, i
     const Span span = span_of(a.q_start, b, a.n_tokens);
     const int col0 = (id - first_tile(a.q_start, b, a.group, group_columns)) * group_columns;
     const int columns = span.count * a.group;
+    if (col0 < 0) return;
     const int quads = c.dim >> 2, slice = group_columns / gridDim.y;
     const float* parts = a.ws + (int64_t)blockIdx.x * a.splits * part_floats(group_columns, c.dim);
     for (int i = threadIdx.x; i < slice * quads; i += 256) {

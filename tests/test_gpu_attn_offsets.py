@@ -1,0 +1,56 @@
+"""Offsets of a ragged batch that do not start at 0, decrease, or lie outside the batch: rows that no sequence owns are left
+alone, before the tensor, inside it and past it, and the sequences whose offsets hold get theirs."""
+import math
+
+import pytest
+import torch
+
+import paper_2502_11880_amd as B
+from tests import kv_model as M
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def _announce(*what):
+    print("case:", *what, flush=True)
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+# q_start, rows of the batch, cached tokens of each sequence, sequences whose rows have to be right
+SPANS = [([64, 128], 128, [200], [0]), ([5, 5, 21, 40], 50, [9, 40, 19], [1, 2]), ([1000, 1010], 10, [30], []),
+         ([0, 500, 20, 600], 600, [500, 40, 600], []), ([-2 ** 31, 5, 10], 10, [30, 30], [1]), ([300, 0, 100], 100, [300, 100], []),
+         ([0, 2 ** 31 - 1, 7], 7, [9, 9], []), ([3, 9, 2 ** 31 - 1], 12, [6, 40], [0])]
+
+
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("start,rows,lens,right", SPANS)
+def test_prefill_writes_only_rows_that_a_sequence_owns(start, rows, lens, right, split):
+    _announce("prompt offsets", start, rows, split)
+    H, Hkv, D, page, before = 32, 8, 64, 16, 1100
+    b = M.Batch(lens, Hkv, D, page, "bf16", seed=rows, width=150)
+    k, v, table, kv_len = b.on(DEV)
+    q = torch.randn(rows, H * D, generator=torch.Generator().manual_seed(31))
+    room = torch.full((before + rows + 300, H * D), 7.0, device=DEV)
+    out = room[before:before + rows]
+    need = B.bitnet_attn_prefill_workspace_bytes(1, 0, len(lens), rows, H, Hkv, D, page, table.shape[1])
+    ws = torch.full((need + 16,), 0xFF, dtype=torch.uint8, device=DEV) if split else torch.empty(16, dtype=torch.uint8, device=DEV)
+    B.bitnet_attn_prefill(q.to(DEV), _i32(start), k, v, table, kv_len, out, 1 / math.sqrt(D), ws=ws)
+    torch.cuda.synchronize()
+    owned = torch.zeros(rows, dtype=torch.bool)
+    for s in range(len(lens)):
+        if 0 <= start[s] <= start[s + 1] <= rows:
+            owned[start[s]:start[s + 1]] = True
+    assert bool((room[:before] == 7.0).all()), "rows before the tensor"
+    assert bool((room[before + rows:] == 7.0).all()), "rows past the tensor"
+    got = out.cpu()
+    assert bool((got[~owned] == 7.0).all()), "rows that no sequence owns"
+    for s in right:
+        n, L = start[s + 1] - start[s], lens[s]
+        want, tol = M.attention(q[start[s]:start[s + 1]].view(n, H, D), b.k[s], b.v[s], M.visible(torch.arange(L - n, L), L, 0, 0),
+                                1 / math.sqrt(D), M.io_eps("f32"), 0.0)
+        M.check(got[start[s]:start[s + 1]].view(n, H, D), want, tol, f"sequence {s}")
