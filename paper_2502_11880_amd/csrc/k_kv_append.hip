@@ -30,7 +30,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvCache c, const vo
     const int low = p0 > 0 ? p0 : 0;
     const int unit = (low >> 3) + (q_start ? id - first_unit(q_start, b) : 0);
     const int base = unit * 8;
-    if (base >= len || span.count == 0) return;
+    // below 0: units before the first sequence's (offsets that start past 0 or decrease), lengths next to 2^31
+    if (base < 0 || base >= len || span.count == 0) return;
     const int at = base >> c.shift;
     if (at >= c.max_pages) return;
     const int page = c.table[(int64_t)b * c.max_pages + at];

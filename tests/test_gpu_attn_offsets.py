@@ -54,3 +54,26 @@ def test_prefill_writes_only_rows_that_a_sequence_owns(start, rows, lens, right,
         want, tol = M.attention(q[start[s]:start[s + 1]].view(n, H, D), b.k[s], b.v[s], M.visible(torch.arange(L - n, L), L, 0, 0),
                                 1 / math.sqrt(D), M.io_eps("f32"), 0.0)
         M.check(got[start[s]:start[s + 1]].view(n, H, D), want, tol, f"sequence {s}")
+
+
+@pytest.mark.parametrize("start,rows,lens", [([64, 128], 128, [200]), ([512, 520], 600, [8]), ([9, 9, 30, 75], 80, [5, 33, 47]),
+                                             ([600, 0, 90], 90, [20, 90]), ([-2 ** 31, 5, 10], 10, [30, 30]), ([0, 8, 16], 16, [2 ** 31 - 1, 20])])
+def test_append_reads_only_its_sequences_rows_of_the_table(start, rows, lens):
+    _announce("append offsets", start, rows, lens)
+    H, D, page = 4, 64, 16
+    held = [n if n < 10 ** 6 else 0 for n in lens]
+    b = M.Batch(held, H, D, page, "f16", seed=rows, fill=0.5, width=20)
+    kc, vc, table, _ = b.on(DEV)
+    k, v = (torch.randn(rows, H, D, generator=torch.Generator().manual_seed(s)).to(b.dtype) for s in (32, 33))
+    sure = []
+    for s, n in enumerate(held):
+        new = start[s + 1] - start[s]
+        if start[s] >= 0 and 0 < new and start[s + 1] <= rows and n:
+            sure.append(s)
+            first = max(0, n - new)
+            at = slice(start[s + 1] - (n - first), start[s + 1])
+            b.write(s, first, k[at], v[at])
+    B.bitnet_kv_append(k.to(DEV), v.to(DEV), _i32(start), kc, vc, table, _i32(lens))
+    torch.cuda.synchronize()
+    if start == sorted(start):               # offsets that decrease: what else is written is not said, only where
+        assert torch.equal(kc.cpu(), b.k_cache) and torch.equal(vc.cpu(), b.v_cache)
