@@ -318,7 +318,7 @@ bitnet_status bitnet_attn_decode(const bitnet_kv_cache* cache, const void* q, in
                                  int64_t window, int64_t n_sink, void* out, void* ws, size_t ws_bytes, void* stream);
 
 /* Workspace bytes with which bitnet_attn_prefill splits the keys of few queries (0 is a valid answer; 0 also for unsupported
- * sizes).  dtype is that of q and out. */
+ * sizes).  At most some 40 MB, however many sequences and tokens.  dtype is that of q and out. */
 size_t bitnet_attn_prefill_workspace_bytes(int cache_dtype, int dtype, int64_t n_seqs, int64_t n_tokens, int64_t n_heads,
                                            int64_t n_kv_heads, int64_t head_dim, int64_t page_size, int64_t max_pages,
                                            int64_t window, int64_t n_sink);

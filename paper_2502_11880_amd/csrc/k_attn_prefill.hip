@@ -38,19 +38,38 @@ struct PrefillArgs {
     float scale2;                    // scale * log2 e
     int window, n_sink;
     int tiles;                       // work groups of a kv head
-    int splits;                      // parts that the keys of each are divided into
-    float* ws;                       // their results, where there are several
+    int splits;                      // parts that the keys of each are divided into, at most
+    int places;                      // work groups that the device holds at a time
+    float* ws;                       // the parts' results, where there are several
 };
 
-// What a work group of `columns` columns leaves for joining: reference and sum of every column, then its output.
-__host__ __device__ __forceinline__ int64_t part_floats(int columns, int dim) { return (int64_t)columns * (2 + dim); }
+// What the parts of a row of out (a token under a head) leave for joining: their references and sums, then their outputs.  By rows
+// of out, not by work groups: sequences without tokens take no room.
+__host__ __device__ __forceinline__ int held_parts(int splits) { return (splits + 1) & ~1; }   // outputs start at 16 bytes
+__host__ __device__ __forceinline__ int64_t row_floats(int splits, int dim) { return (int64_t)held_parts(splits) * (2 + dim); }
 
-// Work groups of sequence b start at floor(q_start[b] group / columns) + b.
-__device__ __forceinline__ int first_tile(const int32_t* q_start, int b, int group, int columns) {
-    return (int)((int64_t)q_start[b] * group / columns) + b;
+// Work groups of sequence b start at floor(q group / columns) + min(b, q), q = q_start[b]: its n tokens take at most
+// floor(n group / columns) + 1 of them, and no more than q sequences before it have tokens.
+__device__ __forceinline__ int first_tile(const int32_t* q_start, int b, int n_tokens, int group, int columns) {
+    const int q = min(max(q_start[b], 0), n_tokens);
+    return (int)((int64_t)q * group / columns) + min(b, q);
 }
 
-template <int T, int DP, bool F32, int WAVES, bool FULL>
+// Parts of this call: as many as find a place beside the work groups that have tokens, which only the device can count where
+// there are several sequences (one without tokens has none, one with a single token as many as kv heads).  Whole waves only.
+__device__ __forceinline__ int parts_of(const PrefillArgs& a, int columns) {
+    if (a.c.n_seqs == 1) return a.splits;
+    int tiles = 0;
+    for (int b = threadIdx.x & 63; b < a.c.n_seqs; b += 64) tiles += (span_of(a.q_start, b, a.n_tokens).count * a.group + columns - 1) / columns;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) tiles += __shfl_xor(tiles, i);
+    tiles = __builtin_amdgcn_readfirstlane(tiles);
+    if (tiles <= 0 || tiles > a.places) return 1;
+    const int parts = a.places / (tiles * a.c.kv_heads);
+    return parts < 1 ? 1 : parts < a.splits ? parts : a.splits;
+}
+
+template <int T, int DP, bool F32, int WAVES, bool FULL, bool SPLIT>
 struct Prefill {
     static constexpr int kQParts = F32 ? Elem<T>::kExactParts : 1;
     static constexpr int kPParts = kQParts;
@@ -58,7 +77,6 @@ struct Prefill {
     static constexpr int kSteps = DP / 16, kBlocks = (DP + 31) / 32;
     static constexpr int kWords = kTile * DP / 8;         // 16-byte words of a tile's keys (and at most of its values)
     static constexpr int kLoads = (kWords + kThreads - 1) / kThreads;
-    static constexpr bool kSplit = WAVES == 4;            // work groups of 8 waves are only taken where they are enough
     static constexpr int kAhead = 4;                      // words of the keys on their way from LDS
     static constexpr int kSchedMfma = 0x8, kSchedLds = 0x100;
 
@@ -77,6 +95,7 @@ struct Prefill {
     int group_first, group_last;                          // tiles that all columns of the work group see
     int sink_end;                                         // tiles with sinks end here
     int sink_tiles, first, n_tiles, part_first;           // (n_tiles from part_first on are this work group's)
+    int parts;                                            // of every work group's keys
     const int32_t* table;
     const uint16_t *kbase, *vbase;
     int key_row;
@@ -88,7 +107,7 @@ struct Prefill {
 
     // Tiles are numbered by their first key / 64; the t-th that the work group looks at:
     __device__ __forceinline__ int tile_of(int t) const {
-        if constexpr (kSplit) t += part_first;
+        if constexpr (SPLIT) t += part_first;
         return t < sink_tiles ? t : t - sink_tiles + first;
     }
     __device__ __forceinline__ int channels() const { return FULL ? DP : dim; }
@@ -439,18 +458,18 @@ struct Prefill {
 
     // Channels 32 d .. of this lane's column: divided by the sum, or, where the keys are split, as they are, with m and l.
     __device__ __forceinline__ void store_block(int d, const v16f& o, const v16f& more, float m, float l, int64_t row) const {
-        if (kSplit && a.splits > 1) {
-            float* part = a.ws + ((int64_t)blockIdx.x * a.splits + blockIdx.y) * part_floats(kColumns, dim);
-            const int col = (tid >> 6) * 32 + n;
+        if (SPLIT && parts > 1) {
+            const int held = held_parts(a.splits), z = blockIdx.y;
+            float* part = a.ws + row * row_floats(a.splits, dim);
             if (d == 0 && half == 0) {
-                part[col] = m;
-                part[kColumns + col] = l;
+                part[z] = m;
+                part[held + z] = l;
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int at = 32 * d + 8 * i + 4 * half;
                 if (FULL || at < dim)
-                    *reinterpret_cast<v4f*>(part + 2 * kColumns + (int64_t)col * dim + at) =
+                    *reinterpret_cast<v4f*>(part + 2 * held + z * dim + at) =
                         v4f{o[4 * i] + more[4 * i], o[4 * i + 1] + more[4 * i + 1], o[4 * i + 2] + more[4 * i + 2], o[4 * i + 3] + more[4 * i + 3]};
             }
             return;
@@ -460,7 +479,7 @@ struct Prefill {
         for (int i = 0; i < 4; ++i) {
             const int at = 32 * d + 8 * i + 4 * half;
             if (FULL || at < dim)
-                store4<T, F32>(a.out, row + at, o[4 * i] * inv + more[4 * i], o[4 * i + 1] * inv + more[4 * i + 1],
+                store4<T, F32>(a.out, row * dim + at, o[4 * i] * inv + more[4 * i], o[4 * i + 1] * inv + more[4 * i + 1],
                                o[4 * i + 2] * inv + more[4 * i + 2], o[4 * i + 3] * inv + more[4 * i + 3]);
         }
     }
@@ -481,13 +500,17 @@ struct Prefill {
         // the head's keys), the last tiles, which have the most keys before them, first
         kvh = blockIdx.x % c.kv_heads;
         const int id = a.tiles - 1 - (int)(blockIdx.x / c.kv_heads);
-        b = find_last(c.n_seqs, id, [&](int i) { return first_tile(a.q_start, i, a.group, kColumns); });
+        b = find_last(c.n_seqs, id, [&](int i) { return first_tile(a.q_start, i, a.n_tokens, a.group, kColumns); });
         b = uniform(b);
         Span span = span_of(a.q_start, b, a.n_tokens);
         span = {uniform(span.first), uniform(span.count)};
-        const int col0 = (id - uniform(first_tile(a.q_start, b, a.group, kColumns))) * kColumns;
+        const int col0 = (id - uniform(first_tile(a.q_start, b, a.n_tokens, a.group, kColumns))) * kColumns;
         const int columns = span.count * a.group;
         if (col0 < 0 || col0 >= columns) return;          // below 0: before the first sequence's tokens, or offsets that decrease
+        if constexpr (SPLIT) {
+            parts = parts_of(a, kColumns);
+            if ((int)blockIdx.y >= parts) return;
+        }
         len = uniform(seq_len(c, b));
         const int p0 = len - span.count;                  // position of the first token (below 0: it sees nothing)
         table = c.table + (int64_t)b * c.max_pages;
@@ -499,7 +522,7 @@ struct Prefill {
         const int token = (used ? col : columns - 1) / a.group, in_group = (used ? col : columns - 1) - token * a.group;
         pos = p0 + token;
         low = a.window > 0 ? pos - a.window : -1;
-        const int64_t row = ((int64_t)(span.first + token) * a.heads + kvh * a.group + in_group) * dim;
+        const int64_t row = (int64_t)(span.first + token) * a.heads + kvh * a.group + in_group;   // of q and out
 
         // The tiles of the work group: those of the sinks, then from the window's first to the last position's.  Positions of
         // its and of this wave's columns (an unused wave sees nothing):
@@ -514,9 +537,9 @@ struct Prefill {
         sink_tiles = sink_tiles < first ? sink_tiles : first;
         n_tiles = pos_hi < 0 ? 0 : sink_tiles + pos_hi / kTile + 1 - first;
         sink_end = (a.n_sink + kTile - 1) / kTile;
-        if constexpr (kSplit) {
-            part_first = (int)((int64_t)n_tiles * blockIdx.y / a.splits);
-            n_tiles = (int)((int64_t)n_tiles * (blockIdx.y + 1) / a.splits) - part_first;
+        if constexpr (SPLIT) {                            // (a row has up to 2^18 tiles, a call 32 parts)
+            part_first = n_tiles * (int)blockIdx.y / parts;
+            n_tiles = n_tiles * ((int)blockIdx.y + 1) / parts - part_first;
         }
         wave_first = uniform(behind(wpos_lo) / kTile);
         wave_last = uniform(wpos_hi < 0 ? -1 : wpos_hi / kTile);
@@ -538,8 +561,8 @@ struct Prefill {
         for (int s = 0; s < kSteps; ++s) {
             const int d = 8 * (2 * s + half);
             x[s][0] = x[s][1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (FULL || d < dim) x[s][0] = load4<T, F32>(a.q, row + d);
-            if (FULL || d + 4 < dim) x[s][1] = load4<T, F32>(a.q, row + d + 4);
+            if (FULL || d < dim) x[s][0] = load4<T, F32>(a.q, row * dim + d);
+            if (FULL || d + 4 < dim) x[s][1] = load4<T, F32>(a.q, row * dim + d + 4);
         }
         if constexpr (kQParts < 3) begin(pages, there);
         // q as operands: chunk 2 s + half of this lane's column, in parts.  The factor of the scores is positive (a negative
@@ -595,35 +618,39 @@ struct Prefill {
     }
 };
 
-template <int T, int DP, bool F32, int WAVES, int PER_SIMD, bool FULL>
+template <int T, int DP, bool F32, int WAVES, int PER_SIMD, bool FULL, bool SPLIT>
 __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attn_prefill_kernel(PrefillArgs a) {
-    using P = Prefill<T, DP, F32, WAVES, FULL>;
+    using P = Prefill<T, DP, F32, WAVES, FULL, SPLIT>;
     __shared__ typename P::Lds lds;
     P(a, lds).run();
 }
 
-// The parts of every column in the order of the keys.  A thread four channels; blockIdx.y: slices of a work group's columns.
+// The parts of every row in the order of the keys.  A thread four channels; blockIdx.y: slices of a work group's columns.
 template <int T, bool F32>
 __global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, int group_columns) {
     const KvCache& c = a.c;
     const int kvh = blockIdx.x % c.kv_heads, id = a.tiles - 1 - (int)(blockIdx.x / c.kv_heads);
-    const int b = find_last(c.n_seqs, id, [&](int i) { return first_tile(a.q_start, i, a.group, group_columns); });
+    const int b = find_last(c.n_seqs, id, [&](int i) { return first_tile(a.q_start, i, a.n_tokens, a.group, group_columns); });
     const Span span = span_of(a.q_start, b, a.n_tokens);
-    const int col0 = (id - first_tile(a.q_start, b, a.group, group_columns)) * group_columns;
+    const int slice = group_columns / gridDim.y;
+    const int col0 = (id - first_tile(a.q_start, b, a.n_tokens, a.group, group_columns)) * group_columns + (int)blockIdx.y * slice;
     const int columns = span.count * a.group;
-    if (col0 < 0) return;
-    const int quads = c.dim >> 2, slice = group_columns / gridDim.y;
-    const float* parts = a.ws + (int64_t)blockIdx.x * a.splits * part_floats(group_columns, c.dim);
+    if (col0 < 0 || col0 >= columns) return;
+    const int parts = parts_of(a, group_columns);
+    if (parts == 1) return;                               // the work groups wrote out themselves
+    const int quads = c.dim >> 2, held = held_parts(a.splits);
     for (int i = threadIdx.x; i < slice * quads; i += 256) {
-        const int in_slice = i / quads, d = 4 * (i - in_slice * quads), local = blockIdx.y * slice + in_slice, col = col0 + local;
+        const int in_slice = i / quads, d = 4 * (i - in_slice * quads), col = col0 + in_slice;
         if (col >= columns) continue;
+        const int token = col / a.group, head = kvh * a.group + col - token * a.group;
+        const int64_t row = (int64_t)(span.first + token) * a.heads + head;
+        const float* part = a.ws + row * row_floats(a.splits, c.dim);
         float m = kNegInf, l = 0.0f;
         v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-        for (int z = 0; z < a.splits; ++z) {
-            const float* part = parts + (int64_t)z * part_floats(group_columns, c.dim);
-            const float pm = part[local], pl = part[group_columns + local];
-            const v4f po = *reinterpret_cast<const v4f*>(part + 2 * group_columns + (int64_t)local * c.dim + d);
+        for (int z = 0; z < parts; ++z) {
+            const float pm = part[z], pl = part[held + z];
+            const v4f po = *reinterpret_cast<const v4f*>(part + 2 * held + z * c.dim + d);
             const float top = fmaxf(m, pm);
             const float fa = m == kNegInf ? 0.0f : exp2_fast(m - top), fb = pm == kNegInf ? 0.0f : exp2_fast(pm - top);
             o = o * fa + po * fb;
@@ -631,9 +658,7 @@ __global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, i
             m = top;
         }
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const int token = col / a.group, head = kvh * a.group + col - token * a.group;
-        store4<T, F32>(a.out, ((int64_t)(span.first + token) * a.heads + head) * c.dim + d, o[0] * inv, o[1] * inv, o[2] * inv,
-                       o[3] * inv);
+        store4<T, F32>(a.out, row * c.dim + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
     }
 }
 
@@ -645,48 +670,69 @@ __global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, i
 // where 8 waves do not divide a tile evenly (heads of 96: 124 / 102; of 100 without a window the large ones stay ahead, 170 / 176).
 // Two parts of q fit 256 registers only in the large ones (f16 heads of 100 behind a window 174 / 220), three in neither: one
 // wave a SIMD (8192 tokens, window 1024: 465; 8 waves with what does not fit in memory 525).
-// Where even groups of 4 waves leave half of their places empty (a chunk of a prompt behind a long cache, a short prompt),
-// each one's keys are split into parts of four tiles and more, and a second launch joins them (64 tokens behind 8000: 184 us
-// whole, 30 split).
+// Where they leave half of their places empty (a chunk of a prompt behind a long cache, a short prompt), each one's keys are split
+// into parts of four tiles and more, and a second launch joins them (64 tokens behind 8000: 184 us whole, 30 split).  How many
+// work groups have tokens is known on the device (parts_of); here the fewest that there can be give the most parts, so that a
+// workspace holds no more rows of out than the places have columns (up to 42 MB).  Where all sequences turn out to have tokens the
+// second launch and the parts left out cost 2 to 12 us (8 sequences of 8 tokens behind 1000, f16 heads of 100: 44 us, never split 35;
+// 32 of 2 behind 500 92 and 80), where one of them has them all the parts save several times that (64 tokens behind 8000 in one
+// of 64 sequences 53 us against 187, of 1024 64 against 188; f16 from 32 bits, one of 32: 79 against 360).  Sequences without
+// tokens still cost work groups that find nothing; parts whose number would make more than kEmptyRounds rounds of those are not
+// taken (bound of 4 rounds: one of 64 91 us, of 256 98; none: 87 and 110; 16: 70 and 82, all before such groups left first).
 constexpr int kCus = 256;
+constexpr int kEmptyRounds = 16;
+constexpr int kMostSeqs = 1024;      // sequences that are counted on the device: past them nothing is split
 struct Plan {
     int waves, splits, tiles;        // tiles: work groups of a kv head
+    int places;
 };
 Plan plan_of(int64_t n_seqs, int64_t n_tokens, int heads, int kv_heads, int dim, int page_size, int64_t max_pages, int window,
              int n_sink, bool three_parts, bool f32) {
-    const int64_t group = heads / kv_heads, rows = n_tokens * group;
+    const int64_t group = heads / kv_heads, rows = n_tokens * group, most_seqs = n_seqs < n_tokens ? n_seqs : n_tokens;
     const bool one_a_simd = three_parts ? dim > 64 : dim > 128 || (f32 && dim > 64);
-    Plan p{4, 1, 0};
+    Plan p{4, 1, 0, one_a_simd ? kCus : 2 * kCus};
     constexpr int kLongKeys = 2048;
     const bool brief = (window > 0 && window <= kLongKeys) || (dim == 128 && n_tokens <= kLongKeys * n_seqs);
     const bool wide = !three_parts && dim > 64 && dim <= 128 && (f32 || (dim > 96 && !brief));
-    if (wide && (rows / 256 + n_seqs) * kv_heads >= kCus) p.waves = 8;
-    const int columns = 32 * p.waves;
-    p.tiles = (int)(rows / columns + n_seqs);
-    if (p.waves == 4) {
-        const int64_t busy = ((rows + columns - 1) / columns) * kv_heads, places = one_a_simd ? kCus : 2 * kCus;
-        int64_t tiles = (max_pages * page_size + kTile - 1) / kTile;
-        if (window > 0) {
-            const int64_t near = ((int64_t)window + columns / group + kTile - 1) / kTile + 2 + ((int64_t)n_sink + kTile - 1) / kTile;
-            tiles = near < tiles ? near : tiles;
-        }
-        int64_t splits = places / busy;
-        splits = splits < tiles / 4 ? splits : tiles / 4;
-        p.splits = (int)(splits < 1 ? 1 : splits > 32 ? 32 : splits);
+    if (wide && (rows / 256 + most_seqs) * kv_heads >= kCus) {
+        p.waves = 8;
+        p.places = kCus;
     }
+    const int columns = 32 * p.waves;
+    p.tiles = (int)(rows / columns + most_seqs);
+    const int64_t busy = (rows + columns - 1) / columns * kv_heads;
+    int64_t tiles = (max_pages * page_size + kTile - 1) / kTile;
+    if (window > 0) {
+        const int64_t near = ((int64_t)window + columns / group + kTile - 1) / kTile + 2 + ((int64_t)n_sink + kTile - 1) / kTile;
+        tiles = near < tiles ? near : tiles;
+    }
+    int64_t splits = p.places / busy;
+    splits = splits < tiles / 4 ? splits : tiles / 4;
+    splits = splits < 32 ? splits : 32;
+    const int64_t most = n_seqs > kMostSeqs ? 1 : kEmptyRounds * (int64_t)p.places / ((int64_t)p.tiles * kv_heads);
+    splits = splits < most ? splits : most;
+    p.splits = (int)(splits < 1 ? 1 : splits);
     return p;
+}
+
+template <int T, int DP, bool F32, int WAVES, int PER_SIMD, bool FULL>
+hipError_t launch_full(const PrefillArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)a.tiles * (unsigned)a.c.kv_heads, (unsigned)a.splits), block(64 * WAVES);
+    if (a.splits == 1) {
+        hipLaunchKernelGGL((attn_prefill_kernel<T, DP, F32, WAVES, PER_SIMD, FULL, false>), grid, block, 0, s, a);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((attn_prefill_kernel<T, DP, F32, WAVES, PER_SIMD, FULL, true>), grid, block, 0, s, a);
+    unsigned slices = 16;
+    while (slices > 1 && grid.x * slices > 4096) slices /= 2;
+    hipLaunchKernelGGL((attn_prefill_join_kernel<T, F32>), dim3(grid.x, slices), dim3(256), 0, s, a, 32 * WAVES);
+    return hipGetLastError();
 }
 
 template <int T, int DP, bool F32, int WAVES, int PER_SIMD>
 hipError_t launch(const PrefillArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)a.tiles * (unsigned)a.c.kv_heads, (unsigned)a.splits), block(64 * WAVES);
-    if (DP != 112 && a.c.dim == DP)
-        hipLaunchKernelGGL((attn_prefill_kernel<T, DP, F32, WAVES, PER_SIMD, DP != 112>), grid, block, 0, s, a);
-    else
-        hipLaunchKernelGGL((attn_prefill_kernel<T, DP, F32, WAVES, PER_SIMD, false>), grid, block, 0, s, a);
-    if (a.splits > 1)
-        hipLaunchKernelGGL((attn_prefill_join_kernel<T, F32>), dim3(grid.x, 16), dim3(256), 0, s, a, 32 * WAVES);
-    return hipGetLastError();
+    if (DP != 112 && a.c.dim == DP) return launch_full<T, DP, F32, WAVES, PER_SIMD, DP != 112>(a, s);
+    return launch_full<T, DP, F32, WAVES, PER_SIMD, false>(a, s);
 }
 
 template <int T, bool F32, int DP>
@@ -711,8 +757,8 @@ hipError_t launch_dim(const PrefillArgs& a, int waves, hipStream_t s) {
     return launch<T, 256, F32, 4, 1>(a, s);
 }
 
-size_t parts_bytes(const Plan& p, int kv_heads, int dim) {
-    return p.splits > 1 ? (size_t)p.tiles * kv_heads * p.splits * (size_t)part_floats(32 * p.waves, dim) * 4 : 0;
+size_t parts_bytes(const Plan& p, int64_t n_tokens, int heads, int dim) {
+    return p.splits > 1 ? (size_t)(n_tokens * heads) * (size_t)row_floats(p.splits, dim) * 4 : 0;
 }
 
 }  // namespace
@@ -720,13 +766,13 @@ size_t parts_bytes(const Plan& p, int kv_heads, int dim) {
 size_t attn_prefill_workspace_bytes(int64_t n_seqs, int64_t n_tokens, int heads, int kv_heads, int dim, int page_size,
                                     int64_t max_pages, int window, int n_sink, bool three_parts, bool f32) {
     return parts_bytes(plan_of(n_seqs, n_tokens, heads, kv_heads, dim, page_size, max_pages, window, n_sink, three_parts, f32),
-                       kv_heads, dim);
+                       n_tokens, heads, dim);
 }
 
 hipError_t launch_attn_prefill(const KvCache& c, int dtype, const AttnArgs& args, void* ws, size_t ws_bytes, hipStream_t s) {
     Plan p = plan_of(c.n_seqs, args.n_tokens, args.heads, c.kv_heads, c.dim, 1 << c.shift, c.max_pages, args.window, args.n_sink,
                      args.f32 && dtype == kBf16, args.f32);
-    if (!ws || ws_bytes < parts_bytes(p, c.kv_heads, c.dim)) p.splits = 1;
+    if (!ws || ws_bytes < parts_bytes(p, args.n_tokens, args.heads, c.dim)) p.splits = 1;
     PrefillArgs a{};
     a.c = c;
     a.q = args.q;
@@ -740,6 +786,7 @@ hipError_t launch_attn_prefill(const KvCache& c, int dtype, const AttnArgs& args
     a.n_sink = args.n_sink;
     a.tiles = p.tiles;
     a.splits = p.splits;
+    a.places = p.places;
     a.ws = static_cast<float*>(ws);
     if (dtype == kBf16) return args.f32 ? launch_dim<kBf16, true>(a, p.waves, s) : launch_dim<kBf16, false>(a, p.waves, s);
     return args.f32 ? launch_dim<kF16, true>(a, p.waves, s) : launch_dim<kF16, false>(a, p.waves, s);

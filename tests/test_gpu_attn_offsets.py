@@ -77,3 +77,33 @@ def test_append_reads_only_its_sequences_rows_of_the_table(start, rows, lens):
     torch.cuda.synchronize()
     if start == sorted(start):               # offsets that decrease: what else is written is not said, only where
         assert torch.equal(kc.cpu(), b.k_cache) and torch.equal(vc.cpu(), b.v_cache)
+
+
+@pytest.mark.parametrize("dtype,io,D", [("bf16", "bf16", 128), ("f16", "f32", 100), ("bf16", "f32", 64)])
+@pytest.mark.parametrize("new,past", [([0] * 20 + [64] + [0] * 11, 1900), ([1] * 64, 1100), ([0, 3] * 40 + [90, 0, 0, 1], 700),
+                                      ([0] * 700 + [70] + [0] * 200 + [2], 1500), ([0] * 1100 + [33], 1500)])
+def test_prefill_of_tables_with_rows_that_have_no_tokens(new, past, dtype, io, D):
+    """Split or not, however many rows of the table bring tokens: workspaces as the size query says, any contents."""
+    _announce("sparse batch", len(new), sum(new), dtype, io, D)
+    H, Hkv, page, n = 32, 8 if D == 128 else 32, 16, sum(new)
+    b = M.Batch([c + past if c else (7 * i) % 40 for i, c in enumerate(new)], 1, D, page, dtype, seed=n + D, width=130)
+    b.heads = Hkv                             # the same keys and values for every kv head
+    k, v, table, kv_len = b.on(DEV)
+    k, v = k.expand(-1, Hkv, -1, -1, -1).contiguous(), v.expand(-1, Hkv, -1, -1, -1).contiguous()
+    start = torch.tensor([0] + new).cumsum(0).tolist()
+    q = torch.randn(n, H * D, generator=torch.Generator().manual_seed(35)).to(M.DTYPES[io])
+    kinds = {"f32": 0, "bf16": 1, "f16": 2}
+    need = B.bitnet_attn_prefill_workspace_bytes(kinds[dtype], kinds[io], len(new), n, H, Hkv, D, page, 130)
+    room = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device=DEV)
+    out = torch.full((n, H * D), 7.0, dtype=M.DTYPES[io], device=DEV)
+    B.bitnet_attn_prefill(q.to(DEV), _i32(start), k, v, table, kv_len, out, 0.1, ws=room[:need] if need else room[:16])
+    torch.cuda.synchronize()
+    assert bool((room[need:] == 0xFF).all()), "bytes past the workspace"
+    got = out.cpu().view(n, H, D)
+    weight = 0.0 if io == "f32" else {"bf16": 2.0 ** -8, "f16": 2.0 ** -10}[io]
+    for s in [i for i, c in enumerate(new) if c][:6] + [i for i, c in enumerate(new) if c][-3:]:
+        L, rows = b.lens[s], slice(start[s], start[s + 1])
+        for heads in (slice(0, 2), slice(H - 2, H)):
+            want, tol = M.attention(q[rows].view(-1, H, D)[:, heads], b.k[s], b.v[s], M.visible(torch.arange(L - new[s], L), L, 0, 0),
+                                    0.1, M.io_eps(io), weight)
+            M.check(got[rows, heads], want, tol, f"sequence {s}")
