@@ -13,6 +13,10 @@
 // length for every work group, which its four waves take in turn.  A row that crosses shares leaves partial results (maximum,
 // sum, unnormalised output) in the workspace, and a second launch joins them.
 //
+// A value that is infinite makes its channel so, whatever its weight.  The products do not: an infinity meets parts of weights, and
+// weights, that are 0 in 32 bits.  But they leave no such channel finite, so that finite outputs need no look at the values; where
+// one is not, the row's values are read once more, and those that are not finite added up (infinite).
+//
 // Measured (kernel times; D = 128, 32 heads of 8 kv heads unless said): one sequence of 131071 keys 82 us (6.6 TB/s of keys and
 // values) and 5 to join; 32 sequences of up to 6000 keys 77 (5.3 TB/s) and 4.5; 24 sequences of 32 heads of 100, f16, behind a
 // window of 1024, 57 us whole (5.3 TB/s); one of 61 keys 5.7 us.  A large plain read reaches 6.4 to 7.0 TB/s here.  What is
@@ -295,6 +299,31 @@ struct Decode {
         for (int it = 0; it + 1 < count; ++it) step(it, std::true_type{});
         step(count - 1, std::false_type{});
     }
+
+    // Channels d .. d + 3 of the values in units u0 .. u1 - 1 that are visible and not finite, added up (none: 0).
+    static __device__ __forceinline__ v4f infinite(const KvCache& c, int b, int kvh, const Sight& sight, int u0, int u1, int d) {
+        const int32_t* table = c.table + (int64_t)b * c.max_pages;
+        const int ps = 1 << c.shift;
+        const uint16_t* base = c.v + (int64_t)kvh * c.dim * ps + d * 8;
+        v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 4 * u0; i < 4 * u1; ++i) {           // words of eight keys
+            const int key = unit_key(sight, i >> 2) + 8 * (i & 3);
+            if (key >= sight.len) break;
+            const int page = table[key >> c.shift];
+            if (!page_ok(c, page)) continue;
+            const uint16_t* word = base + (int64_t)page * c.v_page + (key & (ps - 1)) * c.dim;
+            uint32_t seen = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) seen |= (key + e < sight.len) & ((key + e >= sight.lo) | (key + e < sight.sinks)) ? 1u << e : 0u;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const v4u w = *reinterpret_cast<const v4u*>(word + 8 * t);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[t] += (seen >> e) & 1 ? only_infinite<T>(w[e >> 1] >> (16 * (e & 1)) & 0xFFFFu) : 0.0f;
+            }
+        }
+        return sum;
+    }
 };
 
 template <int T, int DP, bool F32, bool FULL, bool PAGE16>
@@ -427,16 +456,21 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_de
         if (!complete) {
             slot = reinterpret_cast<float*>(a.ws) + kPrefixBytes / 4 +
                    (2 * (int64_t)blockIdx.x + (pos == start ? 0 : 1)) * slot_floats(a.rows, dim);
-            if (tid < 16) {
-                float mm = kNegInf, ll = 0.0f;
+        }
+        // the sum of a head's weights, and the reference it is of
+        auto total = [&](int head, float& mm) {
+            float ll = 0.0f;
+            mm = kNegInf;
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, wave_m[w][tid]);
+            for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, wave_m[w][head]);
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w)
-                    ll += wave_l[w][tid] * (wave_m[w][tid] == kNegInf ? 0.0f : exp2_fast(wave_m[w][tid] - mm));
-                slot[tid] = mm;
-                slot[16 + tid] = ll;
-            }
+            for (int w = 0; w < kWaves; ++w) ll += wave_l[w][head] * (wave_m[w][head] == kNegInf ? 0.0f : exp2_fast(wave_m[w][head] - mm));
+            return ll;
+        };
+        if (!complete && tid < 16) {
+            float mm;
+            slot[16 + tid] = total(tid, mm);
+            slot[tid] = mm;
         }
         const int quads = dim >> 2;
         for (int i = tid; i < count * quads; i += kThreads) {
@@ -444,16 +478,15 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_de
             v4f o = *reinterpret_cast<const v4f*>(&wave_o[head * DP + d]);
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) o += *reinterpret_cast<const v4f*>(&wave_o[(w * a.rows + head) * DP + d]);
+            float mm;
+            if (!all_finite(o)) {
+                const float ll = total(head, mm);         // a score that is no number makes all of its row so
+                if (ll == ll) o = or_infinite(o, D::infinite(a.c, b, kvh, sight, u0, stop, d));
+            }
             if (complete) {
-                float mm = kNegInf, ll = 0.0f;
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, wave_m[w][head]);
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w)
-                    ll += wave_l[w][head] * (wave_m[w][head] == kNegInf ? 0.0f : exp2_fast(wave_m[w][head] - mm));
-                const bool none = ll == 0.0f;             // nothing visible
-                store4<T, F32>(a.out, ((int64_t)b * a.heads + head0 + head) * dim + d, none ? 0.0f : o[0] / ll,
-                               none ? 0.0f : o[1] / ll, none ? 0.0f : o[2] / ll, none ? 0.0f : o[3] / ll);
+                float ll = total(head, mm);
+                ll = ll == 0.0f ? 1.0f : ll;              // no weight, nothing visible: o is 0
+                store4<T, F32>(a.out, ((int64_t)b * a.heads + head0 + head) * dim + d, o[0] / ll, o[1] / ll, o[2] / ll, o[3] / ll);
             } else {
                 *reinterpret_cast<v4f*>(slot + 32 + (int64_t)head * dim + d) = o;
             }
@@ -514,10 +547,17 @@ __global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
         l = l * fa + part_l[w][lane] * fb;
         m = top;
     }
-    const bool none = l == 0.0f;
+    if (!all_finite(o) && l == l) {
+        v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int w = w0; w <= w1; ++w) {
+            const int which = w == w0 && first != (int64_t)w0 * share ? 1 : 0;
+            sum = add_infinite(sum, *reinterpret_cast<const v4f*>(slots + (2 * (int64_t)w + which) * step + 32 + (int64_t)head * dim + d));
+        }
+        o = or_infinite(o, sum);
+    }
+    l = l == 0.0f ? 1.0f : l;                             // no weight: o is 0
     const int64_t at = ((int64_t)(a.first_seq + s) * a.heads + kvh * a.group + tile * 16 + head) * dim + d;
-    store4<T, F32>(a.out, at, none ? 0.0f : o[0] / l, none ? 0.0f : o[1] / l, none ? 0.0f : o[2] / l,
-                   none ? 0.0f : o[3] / l);
+    store4<T, F32>(a.out, at, o[0] / l, o[1] / l, o[2] / l, o[3] / l);
 }
 
 template <int T, int DP, bool F32, bool FULL, bool PAGE16>

@@ -183,6 +183,27 @@ __device__ __forceinline__ float unmark(float sum) {
     return n >= 16384 || (pos && neg) ? __builtin_nanf("") : pos ? -kNegInf : neg ? kNegInf : 0.0f;
 }
 
+// The kind of a value that is not finite of type T: the value itself, 0 for one that is finite.
+template <int T>
+__device__ __forceinline__ float only_infinite(uint32_t h) {
+    return (h & 0x7FFFu) < (T == kBf16 ? 0x7F80u : 0x7C00u) ? 0.0f : Elem<T>::to((uint16_t)h);
+}
+__device__ __forceinline__ bool all_finite(const v4f& x) {
+    return x[0] * 0.0f + x[1] * 0.0f + (x[2] * 0.0f + x[3] * 0.0f) == 0.0f;
+}
+// more + those of x that are not finite: what is left of partial outputs whose factors may be 0 in 32 bits.
+__device__ __forceinline__ v4f add_infinite(v4f more, const v4f& x) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) more[t] += x[t] * 0.0f == 0.0f ? 0.0f : x[t];
+    return more;
+}
+// o, but where a sum of infinite values has something
+__device__ __forceinline__ v4f or_infinite(v4f o, const v4f& sum) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] = sum[t] == 0.0f ? o[t] : sum[t];
+    return o;
+}
+
 // The softmax weights are exp2(x - m + kLift<T>): f16 parts hold small weights best near the top of their range.
 template <int T>
 constexpr float kLift = T == kF16 ? 14.0f : 0.0f;
