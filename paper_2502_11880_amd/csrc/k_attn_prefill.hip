@@ -10,9 +10,10 @@
 // the second product.  Statistics and both products accumulate in 32 bits.  Inputs in the cache's type: weights are
 // rounded once to that type (their sum is not), as the output is; 32-bit inputs go in as exact sums of parts (see Elem).
 //
-// A value that is not finite must not reach a query that does not see it, but 0 times it in the product is no 0.  Tiles that
-// are masked for some query are looked through while they are staged; where one has such a value, the product takes the
-// finite ones and a second one counts the others that each query sees.
+// A value that is not finite must not reach a query that does not see it, and makes its channel infinite for one that does, however
+// small its weight.  The product does neither (0 times it is no number, and weights go in parts, some of them 0), but it leaves
+// no such channel finite: finite outputs need no look at the values, and a work group that has others forms its products once
+// more of the finite values and counts the rest that each query sees (careful).
 //
 // Measured (kernel times; D = 128, 32 heads of 8 kv heads unless said), TFLOP/s of the visible pairs: bf16 throughout, 4096
 // tokens 152 us (905; a large library product reaches 1131 here); 32-bit inputs over bf16, 8192 tokens behind a window of 1024, 465
@@ -83,7 +84,7 @@ struct Prefill {
     struct Lds {
         uint4 k[2][kLoads * kThreads];                    // [chunk][key]
         uint4 v[2][kWords + 32];                          // [eight keys][channel]; reads of channels past D run on
-        int odd;                                          // a masked tile has values that are not finite
+        int odd;                                          // an output is not finite
     };
 
     const PrefillArgs& a;
@@ -211,19 +212,14 @@ struct Prefill {
     }
     __device__ __forceinline__ void store_values(int buf, int tile, uint32_t there) {
         if (there != 15 || tile < group_first || tile > group_last) {
-            uint32_t odd = 0;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int eight = eight_of(held_word(i));
                 int held = len - (tile * kTile + 8 * eight);
                 held = (there >> ((eight >> 1) & 3)) & 1 ? held : 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    stage_v[i][e] &= (held > 2 * e ? 0x0000FFFFu : 0u) | (held > 2 * e + 1 ? 0xFFFF0000u : 0u);
-                    odd |= not_finite<T>(stage_v[i][e]);
-                }
+                for (int e = 0; e < 4; ++e) stage_v[i][e] &= (held > 2 * e ? 0x0000FFFFu : 0u) | (held > 2 * e + 1 ? 0xFFFF0000u : 0u);
             }
-            if (odd) lds.odd = 1;
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -474,7 +470,7 @@ struct Prefill {
             }
             return;
         }
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;    // l is 0 where nothing was visible
+        const float inv = l == 0.0f ? 1.0f : 1.0f / l;    // no weight, nothing visible: o is 0
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int at = 32 * d + 8 * i + 4 * half;
@@ -604,11 +600,19 @@ struct Prefill {
             for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
 
         all_tiles(pages, there, qf, gain, m, l, o);
+        l = sum_xor32(l);
+        float odd = 0.0f;                                 // of channels past D nothing is known
+#pragma unroll
+        for (int t = 0; t < kBlocks; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (FULL || 32 * t + 8 * i + 4 * half < dim) odd += o[t][4 * i] * 0.0f + o[t][4 * i + 1] * 0.0f + (o[t][4 * i + 2] * 0.0f + o[t][4 * i + 3] * 0.0f);
+        if (used && odd != 0.0f && l == l) lds.odd = 1;   // (a score that is no number makes all of its row so)
+        __syncthreads();
         if (uniform(lds.odd)) {
             careful(qf, gain, used, row);
             return;
         }
-        l = sum_xor32(l);
         if (!used) return;
         v16f none;
 #pragma unroll
@@ -657,7 +661,12 @@ __global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, i
             l = l * fa + pl * fb;
             m = top;
         }
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        if (!all_finite(o) && l == l) {
+            v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int z = 0; z < parts; ++z) sum = add_infinite(sum, *reinterpret_cast<const v4f*>(part + 2 * held + z * c.dim + d));
+            o = or_infinite(o, sum);
+        }
+        const float inv = l == 0.0f ? 1.0f : 1.0f / l;
         store4<T, F32>(a.out, row * c.dim + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
     }
 }

@@ -94,3 +94,50 @@ def test_decode_infinite_values_of_weights_that_vanish(dtype, io, key):
     want, tol = M.attention(q.view(1, 2, 64), b.k[0], b.v[0], torch.ones(1, 9001, dtype=torch.bool), 0.2, M.io_eps(io),
                             2.0 ** -15 if io != "f32" else 0.0)
     M.check(out, want, tol)
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("io", ["f32", "cache"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("H,Hkv,D,page", [(4, 1, 64, 16), (6, 2, 100, 64), (8, 2, 128, 32), (3, 1, 256, 16)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (400, 20)])
+def test_prefill_values_that_are_seen(H, Hkv, D, page, dtype, io, window, sinks, split):
+    _announce("prompt infinite values", H, Hkv, D, page, dtype, io, window, split)
+    new, past = [1, 130, 40], [0, 1000, 1700]
+    b = M.Batch([n + p for n, p in zip(new, past)], Hkv, D, page, dtype, seed=D + 1)
+    b.v[0][0, 0, 1] = INF                    # a weight of exactly 1
+    _plant(b.v[1], 900)                      # in tiles that every query sees whole
+    _plant(b.v[2], 1300)
+    b.v[1][1100, 0, 7] = INF                 # among the new tokens: seen by the later ones only
+    b.v[2][3, 0, 9] = -INF                   # a sink, or behind the window
+    for s in range(3):
+        b.write(s, 0, b.k[s], b.v[s])
+    io = dtype if io == "cache" else io
+    weight = 0.0 if io == "f32" else {"bf16": 2.0 ** -8, "f16": 2.0 ** -10}[io]
+    q = torch.randn(sum(new), H * D, generator=torch.Generator().manual_seed(43)).to(M.DTYPES[io])
+    out = _prefill(b, H, q.to(DEV), new, 0.1, window, sinks, split)
+    at = 0
+    for s, n in enumerate(new):
+        L = b.lens[s]
+        want, tol = M.attention(q[at:at + n].view(n, H, D), b.k[s], b.v[s], M.visible(torch.arange(L - n, L), L, window, sinks), 0.1,
+                                M.io_eps(io), weight)
+        M.check(out[at:at + n], want, tol, f"sequence {s}")
+        at += n
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("dtype,io", [("bf16", "f32"), ("f16", "f32"), ("bf16", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("key", [5, 2990])
+def test_prefill_infinite_values_of_weights_that_vanish(dtype, io, key, split):
+    _announce("prompt infinite values of no weight", dtype, io, key, split)
+    b = _towering(3000, 1, 64, dtype, 44, 64, key)
+    b.v[0][1000, 0, 3] = INF
+    b.v[0][1001, 0, 9] = -INF
+    b.v[0][2950, 0, 11] = INF
+    b.v[0][30, 0, 13] = NAN
+    b.write(0, 0, b.k[0], b.v[0])
+    q = torch.rand(70, 2 * 64, generator=torch.Generator().manual_seed(44)).to(M.DTYPES[io]) + 0.5
+    weight = 0.0 if io == "f32" else {"bf16": 2.0 ** -8, "f16": 2.0 ** -10}[io]
+    out = _prefill(b, 2, q.to(DEV), [70], 0.2, split=split)
+    want, tol = M.attention(q.view(70, 2, 64), b.k[0], b.v[0], M.visible(torch.arange(2930, 3000), 3000, 0, 0), 0.2, M.io_eps(io), weight)
+    M.check(out, want, tol)
