@@ -313,7 +313,8 @@ size_t bitnet_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64
  *             is 512 and more and max_pages * page_size at most 2048 or window (> 0) + n_sink at most 1920 (then no row is split).
  *   n_heads % n_kv_heads == 0, n_heads <= 1024.  Reductions run in a fixed order: the same call gives the same bits.
  *   Values that are not finite reach only the outputs of heads whose query sees them, and all of those: an infinite value makes
- *   its channel infinite however small its weight (values of both signs, or a NaN: NaN).
+ *   its channel infinite however small its weight (values of both signs, or a NaN: NaN).  A key whose score is -inf has no
+ *   weight (out is 0 where all are such); a score of +inf or NaN makes the head's out NaN.
  */
 bitnet_status bitnet_attn_decode(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads, float scale,
                                  int64_t window, int64_t n_sink, void* out, void* ws, size_t ws_bytes, void* stream);

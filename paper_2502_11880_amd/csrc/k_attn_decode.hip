@@ -300,6 +300,40 @@ struct Decode {
         step(count - 1, std::false_type{});
     }
 
+    // The same for one head of a row, key by key in plain 32-bit products: taken where the sum of its weights has turned out to be
+    // no number, because an infinite channel of a key may have met a part of q that is 0 or of the other sign.  A lane holds
+    // channels d = 4 lane .. of q and of the output; every lane the maximum and the sum.
+    static __device__ __forceinline__ void plain(const DecodeArgs& a, int b, int head, int kvh, const Sight& sight, int u0, int u1,
+                                                 int d, float& m, float& l, v4f& o) {
+        const KvCache& c = a.c;
+        const int32_t* table = c.table + (int64_t)b * c.max_pages;
+        const int ps = 1 << c.shift;
+        const bool in = d < c.dim;
+        const int ch = in ? d : 0;                        // lanes past D read the first channels and hold none
+        const float4 q = load4<T, F32>(a.q, ((int64_t)b * a.heads + head) * c.dim + ch);
+        m = kNegInf;
+        l = 0.0f;
+        o = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = kUnit * u0; i < kUnit * u1; ++i) {
+            const int j = unit_key(sight, i / kUnit) + i % kUnit;
+            if (j >= sight.len || (j < sight.lo && j >= sight.sinks)) continue;
+            const int page = table[j >> c.shift], slot = j & (ps - 1);
+            if (!page_ok(c, page)) continue;
+            const float4 k = load4<T, false>(c.k, (int64_t)page * c.k_page + ((int64_t)(kvh * c.chunks + (ch >> 3)) * ps + slot) * 8 + (ch & 4));
+            const uint16_t* v = c.v + (int64_t)page * c.v_page + (int64_t)kvh * c.dim * ps + ((slot >> 3) * c.dim + ch) * 8 + (slot & 7);
+            float x = in ? q.x * k.x + q.y * k.y + (q.z * k.z + q.w * k.w) : 0.0f;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) x += __int_as_float(dpp_row_step(__float_as_int(x), t));
+            x = sum_xor32(sum_xor16(x)) * a.scale2;
+            const float top = fmaxf(m, x);
+            const float alpha = m == top ? 1.0f : exp2_fast(m - top), p = exp2_fast(x - (top == kNegInf ? 0.0f : top) + kLift<T>);
+            m = top;
+            l = l * alpha + p;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) o[t] = o[t] * alpha + p * Elem<T>::to(v[8 * t]);
+        }
+    }
+
     // Channels d .. d + 3 of the values in units u0 .. u1 - 1 that are visible and not finite, added up (none: 0).
     static __device__ __forceinline__ v4f infinite(const KvCache& c, int b, int kvh, const Sight& sight, int u0, int u1, int d) {
         const int32_t* table = c.table + (int64_t)b * c.max_pages;
@@ -439,15 +473,34 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_de
             wave_l[wave][n] = r.l;
         }
         __syncthreads();
-        float top = wave_m[0][n];
+        int late = tid;
+        asm volatile("" : "+v"(late));                    // what follows from it is worked out here, not kept in registers from the start on
+        const int col = late & 15;
+        const float all = wave_l[0][col] + wave_l[1][col] + (wave_l[2][col] + wave_l[3][col]);
+        if (D::kQParts > 1 && __builtin_expect(__any(all != all), 0)) {
+            __syncthreads();
+            const int d = 4 * (late & 63);
+            for (int head = wave; head < count; head += kWaves) {
+                float m, l;
+                v4f o;
+                D::plain(a, b, head0 + head, kvh, sight, u0, stop, d, m, l, o);
+                for (int w = 0; w < kWaves; ++w) {        // the whole of it as the first wave's, the others have nothing
+                    wave_m[w][head] = w == 0 ? m : kNegInf;
+                    wave_l[w][head] = w == 0 ? l : 0.0f;
+                    if (d < dim) *reinterpret_cast<v4f*>(&wave_o[(w * a.rows + head) * DP + d]) = w == 0 ? o : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                }
+            }
+        } else {
+            float top = wave_m[0][n];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, wave_m[w][n]);
-        const float f = r.m == kNegInf ? 0.0f : exp2_fast(r.m - top);
-        if (n < count) {
+            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, wave_m[w][n]);
+            const float f = r.m == kNegInf ? 0.0f : exp2_fast(r.m - top);
+            if (n < count) {
 #pragma unroll
-            for (int t = 0; t < DP / 16; ++t) {
-                const v4f o = r.o[t] * f;
-                *reinterpret_cast<v4f*>(&wave_o[(wave * a.rows + n) * DP + 16 * t + 4 * g]) = o;
+                for (int t = 0; t < DP / 16; ++t) {
+                    const v4f o = r.o[t] * f;
+                    *reinterpret_cast<v4f*>(&wave_o[(wave * a.rows + n) * DP + 16 * t + 4 * g]) = o;
+                }
             }
         }
         __syncthreads();
@@ -479,7 +532,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_de
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) o += *reinterpret_cast<const v4f*>(&wave_o[(w * a.rows + head) * DP + d]);
             float mm;
-            if (!all_finite(o)) {
+            if (__builtin_expect(!all_finite(o), 0)) {
                 const float ll = total(head, mm);         // a score that is no number makes all of its row so
                 if (ll == ll) o = or_infinite(o, D::infinite(a.c, b, kvh, sight, u0, stop, d));
             }
@@ -547,7 +600,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(DecodeArgs a) {
         l = l * fa + part_l[w][lane] * fb;
         m = top;
     }
-    if (!all_finite(o) && l == l) {
+    if (__builtin_expect(!all_finite(o) && l == l, 0)) {
         v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int w = w0; w <= w1; ++w) {
             const int which = w == w0 && first != (int64_t)w0 * share ? 1 : 0;

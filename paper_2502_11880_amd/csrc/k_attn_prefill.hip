@@ -392,6 +392,38 @@ struct Prefill {
         }
     }
 
+    // Scores of infinite keys, whose products with parts of q that are 0 are no numbers: of 32 keys, the finite channels' products,
+    // and where there are others an infinity if all of those meet a q of their sign, or all one of the other sign, else NaN.
+    __device__ __forceinline__ void careful_scores(const v4u (&qf)[kQParts][kSteps], v16f (&s)[2]) const {
+        constexpr uint32_t one = T == kBf16 ? 0x3F803F80u : 0x3C003C00u;
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            v16f sum, signs, count;                       // of the finite; of the infinite, by sign; how many are not finite
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[i] = signs[i] = count[i] = 0.0f;
+#pragma unroll
+            for (int st = 0; st < kSteps; ++st) {
+                v4u kf = __builtin_bit_cast(v4u, lds.k[0][(2 * st + half) * kTile + 32 * blk + key_row]), inf, odd, ones = {one, one, one, one}, sq;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t bad = not_finite<T>(kf[e]);
+                    inf[e] = sign_of_infinite<T>(kf[e]);
+                    odd[e] = bad & one;
+                    kf[e] &= ~bad;
+                    sq[e] = sign_of<T>(qf[0][st][e]);     // (a value's first part has its sign, and is 0 where the value is next to none)
+                }
+                signs = Elem<T>::mfma32(inf, sq, signs);
+                count = Elem<T>::mfma32(odd, ones, count);
+#pragma unroll
+                for (int p = 0; p < kQParts; ++p) sum = Elem<T>::mfma32(kf, qf[p][st], sum);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                s[blk][i] = count[i] == 0.0f ? sum[i] : signs[i] == count[i] ? -kNegInf : signs[i] == -count[i] ? kNegInf : __builtin_nanf("");
+        }
+    }
+
     // All tiles once more, twice for every block of 32 channels: first the values that are not finite, counted as the marks of
     // each kind that a column sees (see mark_half), then the product without them.
     __device__ __forceinline__ void careful(const v4u (&qf)[kQParts][kSteps], float gain, bool used, int64_t row) {
@@ -431,7 +463,8 @@ struct Prefill {
                     for (int i = 0; i < 16; ++i) odd[i] += unmark(marks[i]);
                 } else {
                     v16f s[2];
-                    scores(0, qf, s);
+                    if constexpr (kQParts > 1) careful_scores(qf, s);
+                    else scores(0, qf, s);
                     if (!sees_all(tile, there)) mask(key, there, s);
                     o *= softmax(s, gain, m, l);
 #pragma unroll
@@ -607,9 +640,11 @@ struct Prefill {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (FULL || 32 * t + 8 * i + 4 * half < dim) odd += o[t][4 * i] * 0.0f + o[t][4 * i + 1] * 0.0f + (o[t][4 * i + 2] * 0.0f + o[t][4 * i + 3] * 0.0f);
-        if (used && odd != 0.0f && l == l) lds.odd = 1;   // (a score that is no number makes all of its row so)
+        // A score that is no number makes all of its row so, and there is nothing to be careful about, unless an infinite key met a
+        // part of q that is 0 (one part: the score is what it has to be).
+        if (used && odd != 0.0f && (kQParts > 1 || l == l)) lds.odd = 1;
         __syncthreads();
-        if (uniform(lds.odd)) {
+        if (__builtin_expect(uniform(lds.odd), 0)) {
             careful(qf, gain, used, row);
             return;
         }
@@ -661,7 +696,7 @@ __global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, i
             l = l * fa + pl * fb;
             m = top;
         }
-        if (!all_finite(o) && l == l) {
+        if (__builtin_expect(!all_finite(o) && l == l, 0)) {
             v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
             for (int z = 0; z < parts; ++z) sum = add_infinite(sum, *reinterpret_cast<const v4f*>(part + 2 * held + z * c.dim + d));
             o = or_infinite(o, sum);

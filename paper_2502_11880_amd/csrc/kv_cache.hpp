@@ -177,6 +177,18 @@ __device__ __forceinline__ uint32_t mark_half(uint32_t h) {
     constexpr uint32_t one = T == kBf16 ? 0x3F80u : 0x3C00u, b = T == kBf16 ? 0x4300u : 0x5800u, c = T == kBf16 ? 0x4680u : 0x7400u;
     return (h & 0x7FFFu) < inf ? 0u : h == inf ? one : h == (inf | 0x8000u) ? b : c;
 }
+// The halves of a word that are infinite as 1 or -1, others as 0; and the halves that are no 0 as 1 or -1, 0 as 0.
+template <int T>
+__device__ __forceinline__ uint32_t sign_of_infinite(uint32_t w) {
+    constexpr uint32_t inf = T == kBf16 ? 0x7F80u : 0x7C00u, one = T == kBf16 ? 0x3F80u : 0x3C00u;
+    const uint32_t a = w & 0xFFFFu, b = w >> 16;
+    return ((a & 0x7FFFu) == inf ? one | (a & 0x8000u) : 0u) | ((b & 0x7FFFu) == inf ? one | (b & 0x8000u) : 0u) << 16;
+}
+template <int T>
+__device__ __forceinline__ uint32_t sign_of(uint32_t w) {
+    constexpr uint32_t one = T == kBf16 ? 0x3F80u : 0x3C00u;
+    return (w & 0x7FFFu ? one | (w & 0x8000u) : 0u) | (w & 0x7FFF0000u ? one << 16 | (w & 0x80000000u) : 0u);
+}
 __device__ __forceinline__ float unmark(float sum) {
     const int n = (int)sum;
     const bool pos = (n & 127) != 0, neg = ((n >> 7) & 127) != 0;

@@ -141,3 +141,78 @@ def test_prefill_infinite_values_of_weights_that_vanish(dtype, io, key, split):
     out = _prefill(b, 2, q.to(DEV), [70], 0.2, split=split)
     want, tol = M.attention(q.view(70, 2, 64), b.k[0], b.v[0], M.visible(torch.arange(2930, 3000), 3000, 0, 0), 0.2, M.io_eps(io), weight)
     M.check(out, want, tol)
+
+
+@pytest.mark.parametrize("dtype,io", [("bf16", "f32"), ("f16", "f32"), ("bf16", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("scale", [0.1, -0.1])
+@pytest.mark.parametrize("D", [64, 128, 100, 256])
+def test_keys_whose_score_is_minus_infinity_have_no_weight(D, scale, dtype, io):
+    """Channels of some keys are infinite; heads whose query has the sign that makes the score -inf leave them out, the others,
+    whose score is +inf, become NaN."""
+    _announce("infinite keys", D, scale, dtype, io)
+    L, n, H, sign = 400, 50, 4, 1.0 if scale > 0 else -1.0
+    b = M.Batch([L], 1, D, 32, dtype, seed=D + 2)
+    bad = {10: (0, -INF), 200: (5, INF), 201: (D - 1, -INF), 350: (2, INF), 399: (7, -INF)}
+    for key, (channel, x) in bad.items():
+        b.k[0][key, 0, channel] = x * sign
+    b.k[0][300, 0, 0] = b.k[0][300, 0, 7] = -INF * sign      # twice in one key
+    b.write(0, 0, b.k[0], b.v[0])
+    g = torch.Generator().manual_seed(45)
+    q = torch.randn(n, H, D, generator=g)
+    for channel, x in list(bad.values()) + [(0, -INF), (7, -INF)]:
+        q[:, :, channel] = q[:, :, channel].abs().clamp(min=1e-6) * (1.0 if x < 0 else -1.0)
+    q[::3, :, 0] = 1.0                       # exact in one part: the others are 0
+    q[1::3, :, 0] = 0.333251953125           # 11 bits, and a rest
+    q[:, 3, 0] *= -1.0                       # this head's score of key 10 is +inf
+    q = q.to(M.DTYPES[io])
+    left = torch.ones(L, dtype=torch.bool)
+    left[list(bad) + [300]] = False
+    k = b.k[0].clone()
+    k[~left] = 0.0
+    seen = M.visible(torch.arange(L - n, L), L, 0, 0) & left
+    weight = 0.0 if io == "f32" else {"bf16": 2.0 ** -8, "f16": 2.0 ** -10}[io]
+    want, tol = M.attention(q, k, b.v[0], seen, scale, M.io_eps(io), weight)
+    want[:, 3] = NAN
+    out = _prefill(b, H, q.view(n, -1).to(DEV), [n], scale)
+    M.check(out, want, tol, "prompt")
+    out = _decode(b, H, q[-1:].reshape(1, -1).to(DEV), scale)
+    M.check(out, want[-1:], tol[-1:], "decode")
+
+
+@pytest.mark.parametrize("dtype,io", [("bf16", "f32"), ("f16", "f32"), ("bf16", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("H,Hkv,D,window,sinks", [(4, 1, 64, 0, 0), (17, 1, 100, 0, 0), (8, 2, 128, 0, 0), (4, 1, 256, 4500, 300), (6, 2, 36, 4500, 300)])
+def test_decode_infinite_keys_among_many(H, Hkv, D, window, sinks, dtype, io):
+    """Long rows in shares, of which one holds the infinite key; pages that are missing; an infinite value besides; and a row
+    with a key that is no number beside one without."""
+    _announce("infinite keys of long rows", H, Hkv, D, window, dtype, io)
+    b = M.Batch([9001, 9001, 40], Hkv, D, 32, dtype, seed=D + 3)
+    for s in (0, 1):
+        b.k[s][6000, Hkv - 1, D - 1] = -INF
+        b.k[s][100, 0, 2] = -INF
+        b.v[s][6001, Hkv - 1, 3] = INF
+        b.v[s][6000, 0, 3] = -1.5
+        b.table[s, 200] = -1                 # positions 6400 to 6431
+    b.k[1][8000, 0, 1] = NAN
+    for s in range(3):
+        for lo, hi in ((0, min(6400, b.lens[s])), (6432, b.lens[s])):
+            if hi > lo:
+                b.write(s, lo, b.k[s][lo:hi], b.v[s][lo:hi])
+    q = torch.randn(3, H, D, generator=torch.Generator().manual_seed(46))
+    q[:, :, D - 1], q[:, :, 2] = q[:, :, D - 1].abs() + 0.01, q[:, :, 2].abs() + 0.01
+    q = q.to(M.DTYPES[io])
+    out = _decode(b, H, q.view(3, -1).to(DEV), 0.1, window, sinks)
+    for s in range(3):
+        n = b.lens[s]
+        there = (b.table[s].repeat_interleave(32)[:n] >= 0)[None]
+        seen = M.visible(torch.tensor([n - 1]), n, window, sinks) & there
+        for h in range(Hkv):
+            heads = slice(h * (H // Hkv), (h + 1) * (H // Hkv))
+            k, left = b.k[s][:, h:h + 1].clone(), seen.clone()
+            gone = ~torch.isfinite(k).all(2)[:, 0]
+            if bool((torch.isnan(k).any(2)[:, 0] & seen[0]).any()):
+                assert bool(torch.isnan(out[s, heads]).all()), f"sequence {s}, kv head {h}: a key that is no number"
+                continue
+            left[0, gone] = False
+            k[gone] = 0.0
+            want, tol = M.attention(q[s:s + 1, heads], k, b.v[s][:, h:h + 1], left, 0.1, M.io_eps(io), 2.0 ** -15 if io != "f32" else 0.0)
+            M.check(out[s:s + 1, heads], want, tol, f"sequence {s}, kv head {h}")
