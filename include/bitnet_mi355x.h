@@ -376,8 +376,11 @@ bitnet_status bitnet_kv_copy_pages(const bitnet_kv_pool* pool, const int32_t* sr
 
 /*
  * bitnet_kv_reserve -- n_new[i] more tokens for sequence seqs[i]: pages for them in its row, kv_len += n_new[i].  A
- * sequence that cannot have them (too few free pages left by those before it in the list, its row too short, n_new < 0)
- * stays as it is.  n_short (device int32 [1]): how many did not get theirs.  No sequence may be named twice.
+ * sequence that cannot have them stays as it is: its row is too short, n_new < 0, or too few free pages are left.  Pages go
+ * strictly by the list: after the first sequence that the free pages do not suffice for, no later one gets any, however few
+ * it needs (a large request is not overtaken for ever by small ones; list it last where that is wanted), but those whose
+ * last page has room for their tokens are served.  n_short (device int32 [1]): how many did not get theirs.  No sequence may be
+ * named twice.
  */
 bitnet_status bitnet_kv_reserve(const bitnet_kv_tables* tables, const int32_t* seqs, const int32_t* n_new, int64_t n,
                                 int64_t page_size, int32_t* n_short, void* ws, size_t ws_bytes, void* stream);

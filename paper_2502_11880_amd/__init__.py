@@ -480,7 +480,8 @@ def bitnet_kv_copy_pages(k_pool, v_pool, src, dst, stream=None) -> None:
 
 def bitnet_kv_reserve(table, kv_len, refs, seqs, n_new, page_size: int, n_short, ws, stream=None) -> None:
     """Pages for n_new[i] more tokens of sequence seqs[i], counted in kv_len; n_short (int32 [1]) receives the number of
-    sequences that could not have them and stayed as they were."""
+    sequences that could not have them and stayed as they were.  In the list's order: once the free pages do not suffice for
+    one, later ones are only served where their tokens need no new page."""
     t = _tables(table, kv_len, refs)
     n = seqs.numel()
     st = lib().bitnet_kv_reserve(ctypes.byref(t), _list(seqs, "seqs"), _list(n_new, "n_new", n), n, page_size,

@@ -79,7 +79,8 @@ __device__ int lowest_free(const int32_t* refs, int n_pages, int want, int32_t* 
     return found < want ? found : want;
 }
 
-// Pages for new tokens.  One work group; a thread a sequence.
+// Pages for new tokens.  One work group; a thread a sequence.  What a sequence wants counts against all after it whether it
+// gets it or not: the list's order is kept, and one running sum decides.
 __global__ __launch_bounds__(kPlanThreads) void kv_reserve_kernel(KvTables t, const int32_t* seqs, const int32_t* n_new, int n,
                                                                   int shift, int32_t* n_short, int32_t* ws) {
     __shared__ int part[kPlanThreads / 64];

@@ -343,3 +343,14 @@ def test_decode_step_in_a_graph():
         assert captured.count.item() == 0 and captured.lens.tolist() == [15 + i, 301 + i, 2 + i]
         for t in ("out", "table", "lens", "refs", "k", "v"):
             assert torch.equal(getattr(eager, t), getattr(captured, t)), (i, t)
+
+
+def test_reserve_keeps_the_order_of_its_list():
+    _announce("reserve in order")
+    for want, short in (([10, 1, 0], 2), ([1, 10, 1], 2), ([1, 1, 10], 1), ([2, 3, 0], 0)):
+        d = Device(M.Pages(3, 12, 5, 16))
+        n_new = [16 * w for w in want]
+        assert d.m.reserve([0, 1, 2], n_new) == short
+        B.bitnet_kv_reserve(d.table, d.lens, d.refs, _i32([0, 1, 2]), _i32(n_new), 16, d.count, d.ws)
+        d.check(holds=False)
+        assert d.count.item() == short
