@@ -13,12 +13,9 @@ namespace {
 
 thread_local char g_last_error[512] = "";
 
-bitnet_status fail(bitnet_status st, const char* fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
-    va_end(ap);
-    return st;
+template <typename... Args>
+bitnet_status fail(bitnet_status st, const char* fmt, Args... args) {
+    return (bitnet_status)bitnet::fail(st, fmt, args...);
 }
 
 bitnet_status ok() {

@@ -105,7 +105,6 @@ struct Elem;
 
 template <>
 struct Elem<kBf16> {
-    using Frag = bf16x8;
     static constexpr int kExactParts = 3;
     static __device__ __forceinline__ uint16_t from(float x) {
         return __builtin_bit_cast(uint16_t, (__bf16)x);
@@ -135,7 +134,6 @@ struct Elem<kBf16> {
 
 template <>
 struct Elem<kF16> {
-    using Frag = f16x8;
     static constexpr int kExactParts = 2;
     static __device__ __forceinline__ uint16_t from(float x) {
         return __builtin_bit_cast(uint16_t, (_Float16)x);
