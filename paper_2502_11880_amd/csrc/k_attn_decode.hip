@@ -13,9 +13,9 @@
 // length for every work group, which its four waves take in turn.  A row that crosses shares leaves partial results (maximum,
 // sum, unnormalised output) in the workspace, and a second launch joins them.
 //
-// A value that is infinite makes its channel so, whatever its weight.  The products do not: an infinity meets parts of weights, and
-// weights, that are 0 in 32 bits.  But they leave no such channel finite, so that finite outputs need no look at the values; where
-// one is not, the row's values are read once more, and those that are not finite added up (infinite).
+// A value that is infinite makes its channel so, whatever its weight, and a key whose score is -inf has no weight.  The products
+// give NaN for both, because infinities meet weights, and parts of weights and of q, that are 0.  But they leave no such output
+// finite: finite ones need no look at keys and values, and a share with others is gone through once more, key by key (plain).
 //
 // Measured (kernel times; D = 128, 32 heads of 8 kv heads unless said): one sequence of 131071 keys 82 us (6.6 TB/s of keys and
 // values) and 5 to join; 32 sequences of up to 6000 keys 77 (5.3 TB/s) and 4.5; 24 sequences of 32 heads of 100, f16, behind a
@@ -77,6 +77,59 @@ struct DecodeArgs {
     int first_seq, n_seqs;           // of this launch
     int32_t* ws;                     // null: one work group a row
 };
+
+// What a work group is at: a row, or the units of one that its share reaches, from `pos` on (prefix: units of all sequences
+// before each of them; unused where rows stay whole).
+struct Place {
+    int b, kvh, head0, count;            // sequence, kv head, first query head and number of them
+    int u0, u1, units, stop;             // units [u0, u1) of the row's; those that hold keys end at stop
+    Sight sight;
+};
+__device__ __forceinline__ Place place_of(const DecodeArgs& a, const int* prefix, int64_t pos, int64_t end) {
+    const int per_seq = a.c.kv_heads * a.tiles;          // rows of a sequence
+    Place p;
+    int s, row;
+    if (a.ws) {
+        int lo = 0, hi = a.n_seqs - 1;                    // the last sequence that starts at pos or before
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if ((int64_t)prefix[mid] * per_seq <= pos) lo = mid;
+            else hi = mid - 1;
+        }
+        s = lo;
+        p.units = prefix[s + 1] - prefix[s];
+        const int at = (int)(pos - (int64_t)prefix[s] * per_seq);
+        row = at / p.units;
+        p.u0 = at - row * p.units;
+        p.u1 = end - pos < p.units - p.u0 ? p.u0 + (int)(end - pos) : p.units;
+    } else {
+        s = blockIdx.x / per_seq;
+        row = blockIdx.x - s * per_seq;
+        p.u0 = 0;
+    }
+    p.b = a.first_seq + s;
+    p.sight = sight_of(seq_len(a.c, p.b), a.window, a.n_sink);
+    if (!a.ws) p.u1 = p.units = p.sight.units;
+    p.kvh = row / a.tiles;
+    const int tile = row - p.kvh * a.tiles;
+    p.head0 = p.kvh * a.group + tile * 16;
+    p.count = a.group - tile * 16 < 16 ? a.group - tile * 16 : 16;
+    p.stop = p.u1 < p.sight.units ? p.u1 : p.sight.units;
+    return p;
+}
+
+// The share of this work group: units [pos, end) of the line of all (whole rows: one).
+struct Share {
+    int64_t pos, end;
+    int units;
+};
+__device__ __forceinline__ Share share_of(const DecodeArgs& a, const int* prefix) {
+    if (!a.ws) return {0, 1, 0};
+    const int64_t all = (int64_t)prefix[a.n_seqs] * a.c.kv_heads * a.tiles;
+    const int want = (int)((all + gridDim.x - 1) / gridDim.x), units = want < kMinShare ? kMinShare : want;
+    const int64_t pos = (int64_t)blockIdx.x * units;
+    return {pos, pos + units < all ? pos + units : all, units};
+}
 
 // A wave's state of one row: running maximum, sum and unnormalised output; lane (n = lane & 15, g = lane >> 4) holds head n,
 // channels 16 t + 4 g + i of o[t].
@@ -300,9 +353,8 @@ struct Decode {
         step(count - 1, std::false_type{});
     }
 
-    // The same for one head of a row, key by key in plain 32-bit products: taken where the sum of its weights has turned out to be
-    // no number, because an infinite channel of a key may have met a part of q that is 0 or of the other sign.  A lane holds
-    // channels d = 4 lane .. of q and of the output; every lane the maximum and the sum.
+    // A head's keys in units u0 .. u1 - 1 once more, in plain 32-bit products: the finite values weighted, and those that are not
+    // finite added up beside them.  A lane holds channels d = 4 lane .. of q and of the output; every lane the maximum and the sum.
     static __device__ __forceinline__ void plain(const DecodeArgs& a, int b, int head, int kvh, const Sight& sight, int u0, int u1,
                                                  int d, float& m, float& l, v4f& o) {
         const KvCache& c = a.c;
@@ -311,54 +363,83 @@ struct Decode {
         const bool in = d < c.dim;
         const int ch = in ? d : 0;                        // lanes past D read the first channels and hold none
         const float4 q = load4<T, F32>(a.q, ((int64_t)b * a.heads + head) * c.dim + ch);
+        v4f odd = {0.0f, 0.0f, 0.0f, 0.0f};
         m = kNegInf;
         l = 0.0f;
-        o = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int i = kUnit * u0; i < kUnit * u1; ++i) {
-            const int j = unit_key(sight, i / kUnit) + i % kUnit;
-            if (j >= sight.len || (j < sight.lo && j >= sight.sinks)) continue;
-            const int page = table[j >> c.shift], slot = j & (ps - 1);
-            if (!page_ok(c, page)) continue;
-            const float4 k = load4<T, false>(c.k, (int64_t)page * c.k_page + ((int64_t)(kvh * c.chunks + (ch >> 3)) * ps + slot) * 8 + (ch & 4));
-            const uint16_t* v = c.v + (int64_t)page * c.v_page + (int64_t)kvh * c.dim * ps + ((slot >> 3) * c.dim + ch) * 8 + (slot & 7);
-            float x = in ? q.x * k.x + q.y * k.y + (q.z * k.z + q.w * k.w) : 0.0f;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) x += __int_as_float(dpp_row_step(__float_as_int(x), t));
-            x = sum_xor32(sum_xor16(x)) * a.scale2;
-            const float top = fmaxf(m, x);
-            const float alpha = m == top ? 1.0f : exp2_fast(m - top), p = exp2_fast(x - (top == kNegInf ? 0.0f : top) + kLift<T>);
-            m = top;
-            l = l * alpha + p;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) o[t] = o[t] * alpha + p * Elem<T>::to(v[8 * t]);
-        }
-    }
-
-    // Channels d .. d + 3 of the values in units u0 .. u1 - 1 that are visible and not finite, added up (none: 0).
-    static __device__ __forceinline__ v4f infinite(const KvCache& c, int b, int kvh, const Sight& sight, int u0, int u1, int d) {
-        const int32_t* table = c.table + (int64_t)b * c.max_pages;
-        const int ps = 1 << c.shift;
-        const uint16_t* base = c.v + (int64_t)kvh * c.dim * ps + d * 8;
-        v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int i = 4 * u0; i < 4 * u1; ++i) {           // words of eight keys
-            const int key = unit_key(sight, i >> 2) + 8 * (i & 3);
+        o = odd;
+        for (int i = 4 * u0; i < 4 * u1; ++i) {           // eight keys at a time: of one page, and of one word of the values
+            const int key = unit_key(sight, i >> 2) + 8 * (i & 3), slot = key & (ps - 1);
             if (key >= sight.len) break;
             const int page = table[key >> c.shift];
             if (!page_ok(c, page)) continue;
-            const uint16_t* word = base + (int64_t)page * c.v_page + (key & (ps - 1)) * c.dim;
-            uint32_t seen = 0;
+            const int64_t k_at = (int64_t)page * c.k_page + ((int64_t)(kvh * c.chunks + (ch >> 3)) * ps + slot) * 8 + (ch & 4);
+            const uint16_t* v_at = c.v + (int64_t)page * c.v_page + (int64_t)kvh * c.dim * ps + (slot >> 3) * c.dim * 8 + ch * 8;
+            float x[8], top = m;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) seen |= (key + e < sight.len) & ((key + e >= sight.lo) | (key + e < sight.sinks)) ? 1u << e : 0u;
+            for (int e = 0; e < 8; ++e) {
+                const float4 k = load4<T, false>(c.k, k_at + 8 * e);
+                x[e] = in ? q.x * k.x + q.y * k.y + (q.z * k.z + q.w * k.w) : 0.0f;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const v4u w = *reinterpret_cast<const v4u*>(word + 8 * t);
+                for (int t = 0; t < 4; ++t) x[e] += __int_as_float(dpp_row_step(__float_as_int(x[e]), t));
+                const int j = key + e;
+                const bool seen = (j < sight.len) & ((j >= sight.lo) | (j < sight.sinks));
+                x[e] = seen ? sum_xor32(sum_xor16(x[e])) * a.scale2 : kNegInf;
+                top = fmaxf(top, x[e]);
+            }
+            const float alpha = m == top ? 1.0f : exp2_fast(m - top), base = (top == kNegInf ? 0.0f : top) - kLift<T>;
+            m = top;
+            l *= alpha;
+            o *= alpha;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[t] += (seen >> e) & 1 ? only_infinite<T>(w[e >> 1] >> (16 * (e & 1)) & 0xFFFFu) : 0.0f;
+            for (int e = 0; e < 8; ++e) {
+                const int j = key + e;
+                x[e] = exp2_fast(x[e] - base);
+                l += x[e];
+                if (j < sight.len && (j >= sight.lo || j < sight.sinks)) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const float v = Elem<T>::to(v_at[8 * t + e]);
+                        if (v * 0.0f == 0.0f) o[t] += x[e] * v;
+                        else odd[t] += v;
+                    }
+                }
             }
         }
-        return sum;
+        o = or_infinite(o, odd);
     }
 };
+
+// What `plain` gives, in the place of all that a work group has written.  A call, and everything worked out again from the kernel's
+// arguments, so that the kernel keeps its registers and its code to itself: inlined in several ways it cost batches of short rows 5
+// to 10% (52 sequences of up to 110 keys, 16 heads of 100: 12.1 to 12.6 us, this way 11.7, without it 11.4).
+template <int T, int DP, bool F32, bool FULL, bool PAGE16>
+__device__ __noinline__ void redo(uint64_t args, const int* prefix) {
+    args = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(args >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)args);
+    const DecodeArgs a = *(const DecodeArgs*)(const __attribute__((address_space(4))) void*)args;
+    const int dim = a.c.dim, d = 4 * (threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Share share = share_of(a, prefix);
+    for (int64_t pos = share.pos; pos < share.end;) {
+        const Place p = place_of(a, prefix, pos, share.end);
+        const bool whole = p.u0 == 0 && p.u1 == p.units;
+        float* part = reinterpret_cast<float*>(a.ws) + kPrefixBytes / 4 + (2 * (int64_t)blockIdx.x + (pos == share.pos ? 0 : 1)) * slot_floats(a.rows, dim);
+        for (int head = wave; head < p.count; head += kWaves) {
+            float m, l;
+            v4f o;
+            Decode<T, DP, F32, FULL, PAGE16>::plain(a, p.b, p.head0 + head, p.kvh, p.sight, p.u0, p.stop, d, m, l, o);
+            if (d >= dim) continue;
+            if (whole) {
+                l = l == 0.0f ? 1.0f : l;                 // no weight: o is 0
+                store4<T, F32>(a.out, ((int64_t)p.b * a.heads + p.head0 + head) * dim + d, o[0] / l, o[1] / l, o[2] / l, o[3] / l);
+            } else {
+                part[head] = m;
+                part[16 + head] = l;
+                *reinterpret_cast<v4f*>(part + 32 + (int64_t)head * dim + d) = o;
+            }
+        }
+        if (!a.ws) break;
+        pos += p.u1 - p.u0;
+    }
+}
 
 template <int T, int DP, bool F32, bool FULL, bool PAGE16>
 __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_decode_kernel(DecodeArgs a) {
@@ -369,14 +450,14 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_de
     __shared__ int prefix[kMaxSeqs + 1];
     __shared__ int wave_total[kWaves];
     __shared__ int ids[2][kIds];
+    __shared__ int odd;                                   // some output is not finite
     extern __shared__ float wave_o[];                     // [wave][head][channel]
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int per_seq = a.c.kv_heads * a.tiles;           // rows of a sequence
     const int dim = a.c.dim;
 
-    int64_t pos, end;
-    int share = 0;
+    if (tid == 0) odd = 0;
     if (a.ws) {
         // units of all sequences before each of them
         int carry = 0;
@@ -405,49 +486,20 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_de
         }
         if (tid == 0) prefix[a.n_seqs] = carry;
         __syncthreads();
-        const int64_t all = (int64_t)carry * per_seq;
-        share = (int)((all + gridDim.x - 1) / gridDim.x);
-        share = share < kMinShare ? kMinShare : share;
-        if (blockIdx.x == 0) {
-            if (tid == 0) a.ws[0] = share;
-            for (int s = tid; s <= a.n_seqs; s += kThreads) a.ws[kHeadInts + s] = prefix[s];
-        }
-        pos = (int64_t)blockIdx.x * share;
-        end = pos + share < all ? pos + share : all;
-    } else {
-        pos = 0;
-        end = 1;
     }
+    const Share share = share_of(a, prefix);
+    if (a.ws && blockIdx.x == 0) {
+        if (tid == 0) a.ws[0] = share.units;
+        for (int s = tid; s <= a.n_seqs; s += kThreads) a.ws[kHeadInts + s] = prefix[s];
+    }
+    int64_t pos = share.pos;
+    const int64_t end = share.end;
     const int64_t start = pos;
 
     while (pos < end) {
-        int s, row, u0, u1, units;
-        Sight sight;
-        if (a.ws) {
-            int lo = 0, hi = a.n_seqs - 1;                // the last sequence that starts at pos or before
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if ((int64_t)prefix[mid] * per_seq <= pos) lo = mid;
-                else hi = mid - 1;
-            }
-            s = lo;
-            units = prefix[s + 1] - prefix[s];
-            const int at = (int)(pos - (int64_t)prefix[s] * per_seq);
-            row = at / units;
-            u0 = at - row * units;
-            u1 = end - pos < units - u0 ? u0 + (int)(end - pos) : units;
-        } else {
-            s = blockIdx.x / per_seq;
-            row = blockIdx.x - s * per_seq;
-            u0 = 0;
-        }
-        const int b = a.first_seq + s;
-        sight = sight_of(seq_len(a.c, b), a.window, a.n_sink);
-        if (!a.ws) u1 = units = sight.units;
-        const int kvh = row / a.tiles, tile = row - kvh * a.tiles;
-        const int head0 = kvh * a.group + tile * 16;
-        const int count = a.group - tile * 16 < 16 ? a.group - tile * 16 : 16;
-        const int stop = u1 < sight.units ? u1 : sight.units;
+        const Place at = place_of(a, prefix, pos, end);
+        const int b = at.b, head0 = at.head0, count = at.count, kvh = at.kvh, u0 = at.u0, u1 = at.u1, units = at.units, stop = at.stop;
+        const Sight sight = at.sight;
         D::stage_q(a, b, head0, count, qs, gain);
         D::stage_ids(a.c, b, sight, u0, stop < u0 + kIds ? stop : u0 + kIds, ids);
         __syncthreads();
@@ -473,34 +525,15 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_de
             wave_l[wave][n] = r.l;
         }
         __syncthreads();
-        int late = tid;
-        asm volatile("" : "+v"(late));                    // what follows from it is worked out here, not kept in registers from the start on
-        const int col = late & 15;
-        const float all = wave_l[0][col] + wave_l[1][col] + (wave_l[2][col] + wave_l[3][col]);
-        if (D::kQParts > 1 && __builtin_expect(__any(all != all), 0)) {
-            __syncthreads();
-            const int d = 4 * (late & 63);
-            for (int head = wave; head < count; head += kWaves) {
-                float m, l;
-                v4f o;
-                D::plain(a, b, head0 + head, kvh, sight, u0, stop, d, m, l, o);
-                for (int w = 0; w < kWaves; ++w) {        // the whole of it as the first wave's, the others have nothing
-                    wave_m[w][head] = w == 0 ? m : kNegInf;
-                    wave_l[w][head] = w == 0 ? l : 0.0f;
-                    if (d < dim) *reinterpret_cast<v4f*>(&wave_o[(w * a.rows + head) * DP + d]) = w == 0 ? o : v4f{0.0f, 0.0f, 0.0f, 0.0f};
-                }
-            }
-        } else {
-            float top = wave_m[0][n];
+        float top = wave_m[0][n];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, wave_m[w][n]);
-            const float f = r.m == kNegInf ? 0.0f : exp2_fast(r.m - top);
-            if (n < count) {
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, wave_m[w][n]);
+        const float f = r.m == kNegInf ? 0.0f : exp2_fast(r.m - top);
+        if (n < count) {
 #pragma unroll
-                for (int t = 0; t < DP / 16; ++t) {
-                    const v4f o = r.o[t] * f;
-                    *reinterpret_cast<v4f*>(&wave_o[(wave * a.rows + n) * DP + 16 * t + 4 * g]) = o;
-                }
+            for (int t = 0; t < DP / 16; ++t) {
+                const v4f o = r.o[t] * f;
+                *reinterpret_cast<v4f*>(&wave_o[(wave * a.rows + n) * DP + 16 * t + 4 * g]) = o;
             }
         }
         __syncthreads();
@@ -509,21 +542,16 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_de
         if (!complete) {
             slot = reinterpret_cast<float*>(a.ws) + kPrefixBytes / 4 +
                    (2 * (int64_t)blockIdx.x + (pos == start ? 0 : 1)) * slot_floats(a.rows, dim);
-        }
-        // the sum of a head's weights, and the reference it is of
-        auto total = [&](int head, float& mm) {
-            float ll = 0.0f;
-            mm = kNegInf;
+            if (tid < 16) {
+                float mm = kNegInf, ll = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, wave_m[w][head]);
+                for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, wave_m[w][tid]);
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) ll += wave_l[w][head] * (wave_m[w][head] == kNegInf ? 0.0f : exp2_fast(wave_m[w][head] - mm));
-            return ll;
-        };
-        if (!complete && tid < 16) {
-            float mm;
-            slot[16 + tid] = total(tid, mm);
-            slot[tid] = mm;
+                for (int w = 0; w < kWaves; ++w)
+                    ll += wave_l[w][tid] * (wave_m[w][tid] == kNegInf ? 0.0f : exp2_fast(wave_m[w][tid] - mm));
+                slot[tid] = mm;
+                slot[16 + tid] = ll;
+            }
         }
         const int quads = dim >> 2;
         for (int i = tid; i < count * quads; i += kThreads) {
@@ -531,15 +559,17 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_de
             v4f o = *reinterpret_cast<const v4f*>(&wave_o[head * DP + d]);
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) o += *reinterpret_cast<const v4f*>(&wave_o[(w * a.rows + head) * DP + d]);
-            float mm;
-            if (__builtin_expect(!all_finite(o), 0)) {
-                const float ll = total(head, mm);         // a score that is no number makes all of its row so
-                if (ll == ll) o = or_infinite(o, D::infinite(a.c, b, kvh, sight, u0, stop, d));
-            }
+            if (!all_finite(o)) odd = 1;
             if (complete) {
-                float ll = total(head, mm);
-                ll = ll == 0.0f ? 1.0f : ll;              // no weight, nothing visible: o is 0
-                store4<T, F32>(a.out, ((int64_t)b * a.heads + head0 + head) * dim + d, o[0] / ll, o[1] / ll, o[2] / ll, o[3] / ll);
+                float mm = kNegInf, ll = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, wave_m[w][head]);
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w)
+                    ll += wave_l[w][head] * (wave_m[w][head] == kNegInf ? 0.0f : exp2_fast(wave_m[w][head] - mm));
+                const bool none = ll == 0.0f;             // nothing visible
+                store4<T, F32>(a.out, ((int64_t)b * a.heads + head0 + head) * dim + d, none ? 0.0f : o[0] / ll,
+                               none ? 0.0f : o[1] / ll, none ? 0.0f : o[2] / ll, none ? 0.0f : o[3] / ll);
             } else {
                 *reinterpret_cast<v4f*>(slot + 32 + (int64_t)head * dim + d) = o;
             }
@@ -548,6 +578,8 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : FULL ? 2 : 3) void attn_de
         pos += u1 - u0;
         __syncthreads();
     }
+    __syncthreads();
+    if (__builtin_expect(odd, 0)) redo<T, DP, F32, FULL, PAGE16>((uint64_t)__builtin_amdgcn_kernarg_segment_ptr(), prefix);
 }
 
 // Rows that crossed shares: their partial results, in the order of the keys.  One work group a row and 64 quads of channels

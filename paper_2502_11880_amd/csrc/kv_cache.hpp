@@ -193,11 +193,6 @@ __device__ __forceinline__ float unmark(float sum) {
     return n >= 16384 || (pos && neg) ? __builtin_nanf("") : pos ? -kNegInf : neg ? kNegInf : 0.0f;
 }
 
-// The kind of a value that is not finite of type T: the value itself, 0 for one that is finite.
-template <int T>
-__device__ __forceinline__ float only_infinite(uint32_t h) {
-    return (h & 0x7FFFu) < (T == kBf16 ? 0x7F80u : 0x7C00u) ? 0.0f : Elem<T>::to((uint16_t)h);
-}
 __device__ __forceinline__ bool all_finite(const v4f& x) {
     return x[0] * 0.0f + x[1] * 0.0f + (x[2] * 0.0f + x[3] * 0.0f) == 0.0f;
 }
