@@ -306,8 +306,9 @@ size_t bitnet_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64
  *   out[s, h] = sum_j p_j v_j, p = softmax over the visible j of scale * (q[s, h] . k_j), in the kv head h / (n_heads / n_kv_heads).
  *   Visible: j < kv_len[s], and with window > 0 also j >= kv_len[s] - window or j < n_sink (n_sink first tokens stay in
  *   sight).  window 0: no window.  Where nothing is visible (kv_len 0, no pages) out is 0.
- *   q, out    device [n_seqs, n_heads, head_dim] of dtype BITNET_DTYPE_F32 or the cache's.  With F32 the products and the
- *             softmax keep 32-bit precision whatever the cache's type; softmax statistics and sums are 32 bits always.
+ *   q, out    device [n_seqs, n_heads, head_dim] of dtype BITNET_DTYPE_F32 or the cache's.  Softmax statistics and sums are 32
+ *             bits always.  With F32, q and the weights enter the products with all 24 bits over a bf16 cache and with 22 over
+ *             an f16 one; with the cache's type q as it is and the weights with 16 (bf16) or 22 bits.
  *   ws        bitnet_attn_decode_workspace_bytes(...) bytes (partial results of long sequences, which are split and joined),
  *             any contents on entry, nothing kept between calls; may be NULL where that is 0, or where n_seqs * n_kv_heads
  *             is 512 and more and max_pages * page_size at most 2048 or window (> 0) + n_sink at most 1920 (then no row is split).
@@ -330,9 +331,9 @@ size_t bitnet_attn_prefill_workspace_bytes(int cache_dtype, int dtype, int64_t n
  * before): the n tokens of sequence s are at positions p = kv_len[s] - n + i and see j <= p, with window > 0 only
  * j > p - window or j < n_sink.  A position below 0 sees nothing (out 0).
  *   q, out    device [n_tokens, n_heads, head_dim]; q_start device int32 [n_seqs + 1] as in bitnet_kv_append (not NULL).
- *   dtype     BITNET_DTYPE_F32: 32-bit precision throughout: products in parts, two for f16 caches, three for bf16, each
- *             as long as the product itself;
- *             the cache's type: the weights are rounded to it once before the second product, their sum is not.
+ *   dtype     BITNET_DTYPE_F32: q and the weights with 24 bits over a bf16 cache and 22 over an f16 one: products in three
+ *             and two parts, each as long as the product itself;
+ *             the cache's type: the weights are rounded to it once before the second product, and summed as rounded.
  *   ws        optional (NULL): bitnet_attn_prefill_workspace_bytes(...) bytes, any contents, nothing kept.  With it a call of
  *             few queries (a chunk of a prompt behind a long cache, a short prompt) splits their keys over the device and
  *             joins the parts in a second launch; without, or with less, it does not split.

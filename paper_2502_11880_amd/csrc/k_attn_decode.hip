@@ -7,7 +7,9 @@
 // O^T = V^T P^T.  The rows of the two key tiles are chosen so that a lane's eight scores are those of eight consecutive keys,
 // which is its operand of the second product: the weights never leave their lane.  Maximum and sum of the softmax run along
 // (one pass over the cache), in 32 bits; the matrix instructions have so much room here that q and the weights go in as sums
-// of parts of the cache's type (see Elem), which keeps 32-bit inputs exact.
+// of parts of the cache's type (see Elem): from 32-bit inputs three of bf16 (all 24 bits) or two of f16 (22 bits); of the cache's
+// type q is one part as it is, and the weights two, 16 bits of bf16 and 22 of f16, beside a sum of all their bits: less than
+// 2^-15 of the output, a 64th of its own rounding.
 //
 // Work is split evenly whatever the lengths: all units of the launch in one line (sequence, kv head, unit), one share of equal
 // length for every work group, which its four waves take in turn.  A row that crosses shares leaves partial results (maximum,
@@ -17,10 +19,12 @@
 // give NaN for both, because infinities meet weights, and parts of weights and of q, that are 0.  But they leave no such output
 // finite: finite ones need no look at keys and values, and a share with others is gone through once more, key by key (plain).
 //
-// Measured (kernel times; D = 128, 32 heads of 8 kv heads unless said): one sequence of 131071 keys 82 us (6.6 TB/s of keys and
-// values) and 5 to join; 32 sequences of up to 6000 keys 77 (5.3 TB/s) and 4.5; 24 sequences of 32 heads of 100, f16, behind a
-// window of 1024, 57 us whole (5.3 TB/s); one of 61 keys 5.7 us.  A large plain read reaches 6.4 to 7.0 TB/s here.  What is
-// left is a share's start: length, pages and first keys are three reads in a row, and rows that end inside a share start anew.
+// Measured (kernel times; D = 128, 32 heads of 8 kv heads unless said): one sequence of 131071 keys 82 us (6.5 TB/s of keys and
+// values) and 5 to join; 32 sequences of up to 6000 keys 76 (5.3 TB/s) and 5; 24 sequences of 32 heads of 100, f16, behind a
+// window of 1024, 57 us whole (5.3 TB/s); one of 61 keys 5.8 us (in a table of 5 pages; where the table has room for more than
+// 256 keys, rows may be split and a second launch joins them: the pass takes 12 us, not 8).  A large plain read reaches 6.4 to
+// 7.0 TB/s here.  What is left is a share's start: length, pages and first keys are three reads in a row, and rows that end inside
+// a share start anew.
 #include "kv_cache.hpp"
 
 #include <type_traits>
@@ -34,7 +38,7 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kMaxGroups = 1024;     // work groups of a split launch
 constexpr int kMaxSeqs = 1024;       // sequences of a split launch (more go in several)
 constexpr int kMinShare = 4;         // units of a share, at least: one for each wave
-// Rows of up to kWholeUnits units are never split (61 keys: 5.7 us in one launch, where the join alone takes 4.5), nor rows of up
+// Rows of up to kWholeUnits units are never split (61 keys: 5.8 us in one launch, where the join alone takes 4 to 5), nor rows of up
 // to kManyUnits where there are kManyRows of them: a work group a row is enough then, and the join is saved (24 x 32 rows of
 // 1028 keys: 57 us whole).
 constexpr int kWholeUnits = 8;
@@ -414,14 +418,16 @@ struct Decode {
 // to 10% (52 sequences of up to 110 keys, 16 heads of 100: 12.1 to 12.6 us, this way 11.7, without it 11.4).
 template <int T, int DP, bool F32, bool FULL, bool PAGE16>
 __device__ __noinline__ void redo(uint64_t args, const int* prefix) {
-    args = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(args >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)args);
+    const uint32_t low = __builtin_amdgcn_readfirstlane((int)args), high = __builtin_amdgcn_readfirstlane((int)(args >> 32));
+    args = (uint64_t)high << 32 | low;
     const DecodeArgs a = *(const DecodeArgs*)(const __attribute__((address_space(4))) void*)args;
     const int dim = a.c.dim, d = 4 * (threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Share share = share_of(a, prefix);
     for (int64_t pos = share.pos; pos < share.end;) {
         const Place p = place_of(a, prefix, pos, share.end);
         const bool whole = p.u0 == 0 && p.u1 == p.units;
-        float* part = reinterpret_cast<float*>(a.ws) + kPrefixBytes / 4 + (2 * (int64_t)blockIdx.x + (pos == share.pos ? 0 : 1)) * slot_floats(a.rows, dim);
+        float* part = reinterpret_cast<float*>(a.ws) + kPrefixBytes / 4 +
+                      (2 * (int64_t)blockIdx.x + (pos == share.pos ? 0 : 1)) * slot_floats(a.rows, dim);
         for (int head = wave; head < p.count; head += kWaves) {
             float m, l;
             v4f o;

@@ -8,7 +8,9 @@
 // LDS in tiles of 64, double-buffered.  S^T = K Q^T and O^T = V^T P^T on 32x32x16 instructions: a column's scores lie in two
 // lanes (maximum and sum need one exchange), and the rows of the key tiles are chosen so that a lane's scores are its operand of
 // the second product.  Statistics and both products accumulate in 32 bits.  Inputs in the cache's type: weights are
-// rounded once to that type (their sum is not), as the output is; 32-bit inputs go in as exact sums of parts (see Elem).
+// rounded once to that type (and summed as rounded), as the output is: a second part would double the longer half of the work,
+// and the error against 64 bits is 2.1e-3 of the output's size where rounding the output alone makes 1.6e-3 (4096 tokens, bf16).
+// 32-bit inputs go in as sums of parts (see Elem): three of bf16, which are exact, or two of f16, which hold 22 bits.
 //
 // A value that is not finite must not reach a query that does not see it, and makes its channel infinite for one that does, however
 // small its weight.  The product does neither (0 times it is no number, and weights go in parts, some of them 0), but it leaves
@@ -16,13 +18,13 @@
 // more of the finite values and counts the rest that each query sees (careful).
 //
 // Measured (kernel times; D = 128, 32 heads of 8 kv heads unless said), TFLOP/s of the visible pairs: bf16 throughout, 4096
-// tokens 152 us (905; a large library product reaches 1131 here); 32-bit inputs over bf16, 8192 tokens behind a window of 1024, 465
-// us (278, 834 in its three parts); 32-bit inputs over f16, six chunks of up to 1500 tokens, 32 heads of 100, window 512, 170
-// us (207, 415 in two parts); 37 tokens 11 us (a start of four reads in a row, then one tile).  At 4096 tokens the matrix cores are
-// busy 37% of the kernel's cycles; a wave waits 32% of its time, is ready but not issued 31% and issues 37%: exponentials and
+// tokens 148 us (930; a large library product reaches 1131 here); 32-bit inputs over bf16, 8192 tokens behind a window of 1024, 456
+// us (284, 851 in its three parts); 32-bit inputs over f16, six chunks of up to 1500 tokens, 32 heads of 100, window 512, 175
+// us (202, 403 in two parts); 37 tokens 11 us (a start of four reads in a row, then one tile).  At 4096 tokens the matrix cores are
+// busy 37% of the kernel's cycles; a wave waits 31% of its time, is ready but not issued 31% and issues 38%: exponentials and
 // weights of one wave against the products of the other.  Slower: softmax of one tile between the products of the next in one
 // wave (190 us against 166), halves of the waves taking turns at a barrier (173), products in a fixed order (156), keys and
-// values staged through the same registers (162), all against 151 to 152.
+// values staged through the same registers (162), all against 151 to 152 then.
 #include "kv_cache.hpp"
 
 namespace bitnet {
@@ -61,7 +63,8 @@ __device__ __forceinline__ int first_tile(const int32_t* q_start, int b, int n_t
 __device__ __forceinline__ int parts_of(const PrefillArgs& a, int columns) {
     if (a.c.n_seqs == 1) return a.splits;
     int tiles = 0;
-    for (int b = threadIdx.x & 63; b < a.c.n_seqs; b += 64) tiles += (span_of(a.q_start, b, a.n_tokens).count * a.group + columns - 1) / columns;
+    for (int b = threadIdx.x & 63; b < a.c.n_seqs; b += 64)
+        tiles += (span_of(a.q_start, b, a.n_tokens).count * a.group + columns - 1) / columns;
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) tiles += __shfl_xor(tiles, i);
     tiles = __builtin_amdgcn_readfirstlane(tiles);
@@ -403,7 +406,8 @@ struct Prefill {
             for (int i = 0; i < 16; ++i) sum[i] = signs[i] = count[i] = 0.0f;
 #pragma unroll
             for (int st = 0; st < kSteps; ++st) {
-                v4u kf = __builtin_bit_cast(v4u, lds.k[0][(2 * st + half) * kTile + 32 * blk + key_row]), inf, odd, ones = {one, one, one, one}, sq;
+                const v4u ones = {one, one, one, one};
+                v4u kf = __builtin_bit_cast(v4u, lds.k[0][(2 * st + half) * kTile + 32 * blk + key_row]), inf, odd, sq;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const uint32_t bad = not_finite<T>(kf[e]);
@@ -420,7 +424,10 @@ struct Prefill {
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                s[blk][i] = count[i] == 0.0f ? sum[i] : signs[i] == count[i] ? -kNegInf : signs[i] == -count[i] ? kNegInf : __builtin_nanf("");
+                s[blk][i] = count[i] == 0.0f         ? sum[i]
+                            : signs[i] == count[i]  ? -kNegInf
+                            : signs[i] == -count[i] ? kNegInf
+                                                    : __builtin_nanf("");
         }
     }
 
@@ -638,8 +645,8 @@ struct Prefill {
 #pragma unroll
         for (int t = 0; t < kBlocks; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (FULL || 32 * t + 8 * i + 4 * half < dim) odd += o[t][4 * i] * 0.0f + o[t][4 * i + 1] * 0.0f + (o[t][4 * i + 2] * 0.0f + o[t][4 * i + 3] * 0.0f);
+            for (int i = 0; i < 16; ++i)
+                if (FULL || 32 * t + 8 * (i >> 2) + 4 * half < dim) odd += o[t][i] * 0.0f;
         // A score that is no number makes all of its row so, and there is nothing to be careful about, unless an infinite key met a
         // part of q that is 0 (one part: the score is what it has to be).
         if (used && odd != 0.0f && (kQParts > 1 || l == l)) lds.odd = 1;
@@ -713,16 +720,18 @@ __global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, i
 // 89 / 83; 8192 tokens behind a window of 4096 447 / 455, 2048 309 / 290, 1024 190 / 182; heads of 100, 512: 134 / 129) or
 // where 8 waves do not divide a tile evenly (heads of 96: 124 / 102; of 100 without a window the large ones stay ahead, 170 / 176).
 // Two parts of q fit 256 registers only in the large ones (f16 heads of 100 behind a window 174 / 220), three in neither: one
-// wave a SIMD (8192 tokens, window 1024: 465; 8 waves with what does not fit in memory 525).
+// wave a SIMD (8192 tokens, window 1024: 456; 8 waves with what does not fit in memory 525).
 // Where they leave half of their places empty (a chunk of a prompt behind a long cache, a short prompt), each one's keys are split
-// into parts of four tiles and more, and a second launch joins them (64 tokens behind 8000: 184 us whole, 30 split).  How many
+// into parts of four tiles and more, and a second launch joins them (64 tokens behind 8000: 184 us whole, 31 split).  How many
 // work groups have tokens is known on the device (parts_of); here the fewest that there can be give the most parts, so that a
-// workspace holds no more rows of out than the places have columns (up to 42 MB).  Where all sequences turn out to have tokens the
-// second launch and the parts left out cost 2 to 12 us (8 sequences of 8 tokens behind 1000, f16 heads of 100: 44 us, never split 35;
-// 32 of 2 behind 500 92 and 80), where one of them has them all the parts save several times that (64 tokens behind 8000 in one
-// of 64 sequences 53 us against 187, of 1024 64 against 188; f16 from 32 bits, one of 32: 79 against 360).  Sequences without
-// tokens still cost work groups that find nothing; parts whose number would make more than kEmptyRounds rounds of those are not
-// taken (bound of 4 rounds: one of 64 91 us, of 256 98; none: 87 and 110; 16: 70 and 82, all before such groups left first).
+// workspace holds no more rows of out than the places have columns (up to 42 MB).  Where all sequences turn out to have tokens
+// the second launch and the parts left out cost 6 to 12 us (from 32 bits over f16, heads of 100: 8 sequences of 8 tokens behind 1000
+// 44 us, whole 35; 32 of 2 behind 500 92 and 80); where one has them all the parts save several times that (64 tokens behind
+// 8000 in one of 64 rows of the table 54 us, whole 187, of 1024 65 and 188; from 32 bits over f16, one of 32 rows, 67 and 360).
+// Sequences without tokens still cost work groups that find nothing; parts that would make more than kEmptyRounds rounds of those
+// are not taken (one of 64, 256 and 1024 rows: 54, 60 and 65 us; 4 rounds 79, 81, 85; no bound 70, 80, 87).
+// The keys are counted by the room of the table: in one much wider than its sequences some parts have nothing to do (37 tokens in
+// a table of 8192 positions 16 us, in one of 64 11).
 constexpr int kCus = 256;
 constexpr int kEmptyRounds = 16;
 constexpr int kMostSeqs = 1024;      // sequences that are counted on the device: past them nothing is split

@@ -5,7 +5,7 @@
 // number first, in the order of the call's sequences, whatever the launch shape: results are reproducible.  Only copying
 // moves bytes that count; it reads and writes every page once, in pieces of 16 KiB that a fixed grid shares out.
 //
-// Measured: compacting a pool of which half is live (1678 MB read and written) 330 to 342 us for the moves (4.9 to 5.1 TB/s; a large
+// Measured: compacting a pool of which half is live (1678 MB read and written) 328 to 342 us for the moves (4.9 to 5.1 TB/s; a large
 // copy reaches 4.9) and 5 for the pairs; forking beams over 32 layers (235 MB) 30 us (the source pages are still in the last
 // cache) and 5.6 for the plan, freeing 4 and reserving 5.6.  Plans take one work group because a page number depends on
 // all before it: up to 8192 pages one pass of 1024 threads, and for compaction past that a work group for each 8192 of them.

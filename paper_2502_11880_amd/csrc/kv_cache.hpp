@@ -98,8 +98,10 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 // The cache's element types: conversions, matrix instructions, and 32-bit values as a sum of parts of that type.
 // bf16: a part keeps the upper 16 bits of what is left (truncated, so every part has the value's sign); three parts hold all
-// 24 bits, two hold 16.  f16: a part is rounded to nearest; two parts hold 22 bits of a value near the top of the range, so
-// values are brought there by a power of two first.
+// 24 bits of a value, which is exact, and two hold 16 (cut off: less than 2^-15 of it).  f16: a part is rounded to nearest; two parts
+// hold 22 bits of a value near the top of the range, so values are brought there by a power of two first.  What is left out then,
+// 2^-23 of a value or 2^-38 of its row's largest, is of the size of the roundings that 32-bit sums make anyway, and a third
+// part would cost a third product.
 template <int T>
 struct Elem;
 
