@@ -725,15 +725,18 @@ __global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillArgs a, i
 // into parts of four tiles and more, and a second launch joins them (64 tokens behind 8000: 184 us whole, 31 split).  How many
 // work groups have tokens is known on the device (parts_of); here the fewest that there can be give the most parts, so that a
 // workspace holds no more rows of out than the places have columns (up to 42 MB).  Where all sequences turn out to have tokens
-// the second launch and the parts left out cost 6 to 12 us (from 32 bits over f16, heads of 100: 8 sequences of 8 tokens behind 1000
-// 44 us, whole 35; 32 of 2 behind 500 92 and 80); where one has them all the parts save several times that (64 tokens behind
-// 8000 in one of 64 rows of the table 54 us, whole 187, of 1024 65 and 188; from 32 bits over f16, one of 32 rows, 67 and 360).
+// the second launch and the parts left out cost some us (from 32 bits over f16, heads of 100: 8 sequences of 8 tokens behind 1000
+// 44 us, whole 35); where one has them all the parts save several times that (64 tokens behind 8000 in one of 64 rows of the
+// table 53 us, whole 187, of 1024 64 and 188; from 32 bits over f16, one of 32 rows, 66 and 360).  The large work groups are split
+// where that gives kLargeParts parts and more: fewer cost more where they prove empty than they could save (8 sequences of 128 tokens
+// behind 300, two parts: 32 us, whole 26; 1024 tokens in one of 8 rows 59 and 66).
 // Sequences without tokens still cost work groups that find nothing; parts that would make more than kEmptyRounds rounds of those
-// are not taken (one of 64, 256 and 1024 rows: 54, 60 and 65 us; 4 rounds 79, 81, 85; no bound 70, 80, 87).
+// are not taken (one of 64, 256 and 1024 rows: 53, 59 and 64 us; 4 rounds 79, 81, 85; no bound 70, 80, 87).
 // The keys are counted by the room of the table: in one much wider than its sequences some parts have nothing to do (37 tokens in
 // a table of 8192 positions 16 us, in one of 64 11).
 constexpr int kCus = 256;
 constexpr int kEmptyRounds = 16;
+constexpr int kLargeParts = 4;       // parts of groups of 8 waves, at least
 constexpr int kMostSeqs = 1024;      // sequences that are counted on the device: past them nothing is split
 struct Plan {
     int waves, splits, tiles;        // tiles: work groups of a kv head
@@ -764,6 +767,7 @@ Plan plan_of(int64_t n_seqs, int64_t n_tokens, int heads, int kv_heads, int dim,
     splits = splits < 32 ? splits : 32;
     const int64_t most = n_seqs > kMostSeqs ? 1 : kEmptyRounds * (int64_t)p.places / ((int64_t)p.tiles * kv_heads);
     splits = splits < most ? splits : most;
+    if (p.waves == 8 && splits < kLargeParts) splits = 1;
     p.splits = (int)(splits < 1 ? 1 : splits);
     return p;
 }
