@@ -296,6 +296,87 @@ size_t bitnet_kv_page_bytes(int dtype, int64_t page_size, int64_t n_kv_heads, in
 bitnet_status bitnet_kv_append(const bitnet_kv_cache* cache, const void* k, const void* v, int src_dtype,
                                const int32_t* q_start, int64_t n_tokens, void* stream);
 
+/*
+ * What stands between the products of a layer and its attention: the norm that makes a product's int8 activation, and rotary
+ * positions.
+ *
+ * bitnet_norm_quantize -- the residual's addition, a root-mean-square norm, and bitnet_quantize_act, of M rows of K values:
+ *   r   = x + residual in 32 bits, rounded to residual_dtype (without a residual: x);
+ *   inv = fp32(1 / sqrt(sum_k r^2 / K + eps)), the sum and what follows in 64 bits;
+ *   n   = fp32(fp32(r * inv) * gamma);  xq, x_scale and x_rowsum as bitnet_quantize_act makes them of n.
+ *   x             device [M, K] of x_dtype: BITNET_DTYPE_F32 or the residual's (any type without a residual).
+ *   residual      device [M, K] of residual_dtype, or NULL (then residual_dtype is not looked at); residual_out: r, or NULL.
+ *   gamma         device fp32 [K], or NULL (ones).  eps > 0.
+ *   y             device [M, K] of y_dtype: n, rounded once; or NULL.
+ *   xq, x_scale, x_rowsum   as in bitnet_quantize_act; x_rowsum, or all three, may be NULL.  y or xq is needed.
+ *   residual_out and y may each be x or the residual themselves (same type); outputs overlap inputs in no other way, nor each
+ *   other.  Values must be finite, as in bitnet_quantize_act; others spoil their own row only.  The codes do not depend on the
+ *   launch shape (a sum in 64 bits rounds to the same inv in any order, but for one row in some 2^29).
+ *   0 <= M <= 2^24, 1 <= K <= 1048576.  x_scale and x_rowsum 4-byte aligned, all others 16-byte.
+ */
+bitnet_status bitnet_norm_quantize(const void* x, int x_dtype, const void* residual, void* residual_out, int residual_dtype,
+                                   const float* gamma, float eps, int64_t M, int64_t K, void* y, int y_dtype, int8_t* xq,
+                                   float* x_scale, int32_t* x_rowsum, void* stream);
+
+/*
+ * bitnet_rotation: how the heads of tokens are turned by their positions.  The first rot_dim channels of a head are pairs
+ * (a, b) = (x[i], x[i + rot_dim / 2]), or with interleaved (x[2i], x[2i + 1]), and become
+ *   gain * (a cos t - b sin t, b cos t + a sin t),  t = 2 pi p freqs[i]  for a token at position p;
+ * the other channels stay as they are.  Angles are worked out in 64 bits, products in 32, and each result is rounded once to
+ * its type.  rot_dim even, 2 <= rot_dim <= head_dim.
+ */
+typedef struct {
+    const double* freqs;      /* device [rot_dim / 2], turns a position (bitnet_rope_freqs) */
+    int64_t rot_dim;
+    int32_t interleaved;      /* 0 or 1 */
+    float gain;               /* 1 unless a scaling for long contexts asks for more */
+} bitnet_rotation;
+
+/*
+ * bitnet_rope_freqs -- freqs[i] = f_i = theta^(-2 i / rot_dim) / (2 pi), stretched by `factor` for contexts that are longer than
+ * the `original` (in tokens):
+ *   NONE    f_i as it is (factor, original, low and high are not looked at; nor, where not named, below);
+ *   LINEAR  f_i / factor: every position that much closer;
+ *   BASE    with theta * factor^(rot_dim / (rot_dim - 2)) for theta (rot_dim >= 4);
+ *   TURNS   w f_i + (1 - w) f_i / factor, w = clamp((original f_i - low) / (high - low), 0, 1): pairs of few turns over the original
+ *           context are stretched, those of many are not;
+ *   INDEX   the same with w = 1 - clamp((i - lo) / (hi - lo), 0, 1): lo and hi are the indices at which a pair would make `high` and
+ *           `low` turns, rounded down and up, and kept within 0 and rot_dim - 1.
+ * theta > 1, factor > 0, original > 0, 0 < low < high.  freqs: device [rot_dim / 2], rot_dim even and up to 256.
+ */
+typedef enum {
+    BITNET_ROPE_NONE = 0,
+    BITNET_ROPE_LINEAR = 1,
+    BITNET_ROPE_BASE = 2,
+    BITNET_ROPE_TURNS = 3,
+    BITNET_ROPE_INDEX = 4
+} bitnet_rope_scaling;
+
+bitnet_status bitnet_rope_freqs(int scaling, double theta, int64_t rot_dim, double factor, double original, double low, double high,
+                                double* freqs, void* stream);
+
+/*
+ * bitnet_rope -- out = x with the heads of token t turned to position pos[t].
+ *   x, out   device [n_tokens, n_heads, head_dim] of dtype (any bitnet_dtype); out may be x, and overlaps it in no other way.
+ *   pos      device int32 [n_tokens], any values.
+ *   0 <= n_tokens <= 2^24, 1 <= n_heads <= 1024, head_dim a multiple of 4 up to 256.  x and out 16-byte aligned.
+ */
+bitnet_status bitnet_rope(const bitnet_rotation* rotation, const void* x, int dtype, int64_t n_tokens, int64_t n_heads,
+                          int64_t head_dim, const int32_t* pos, void* out, void* stream);
+
+/*
+ * bitnet_kv_append_rope -- bitnet_kv_append with the keys turned to their positions before they are rounded and written, and the
+ * query heads of the same tokens turned on the way (what bitnet_rope would make of them).
+ *   q, q_out  device [n_tokens, n_heads, head_dim] of src_dtype, n_heads % n_kv_heads == 0, n_heads <= 1024; q_out may be q, and
+ *             overlaps no input in another way.  Both NULL: keys and values only (n_heads is not looked at).
+ *   A token's position is where it goes in its sequence: kv_len[s] - n .. kv_len[s] - 1.  Tokens at positions below 0, and those
+ *   that no sequence owns, are left out: their rows of q_out are not written.  A token without a page has its q turned all the same.
+ *   Other arguments as bitnet_kv_append.  16-byte aligned: q, q_out, k, v and the cache.
+ */
+bitnet_status bitnet_kv_append_rope(const bitnet_kv_cache* cache, const bitnet_rotation* rotation, const void* q, int64_t n_heads,
+                                    const void* k, const void* v, int src_dtype, const int32_t* q_start, int64_t n_tokens,
+                                    void* q_out, void* stream);
+
 /* Workspace bytes with which bitnet_attn_decode serves n_seqs sequences and fewer (0 is a valid answer; 0 also for unsupported
  * sizes). */
 size_t bitnet_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,

@@ -65,6 +65,19 @@ _SIGNATURES = [
      [ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int]),
     ("bitnet_kv_append", ctypes.c_int,
      [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    ("bitnet_norm_quantize", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_float,
+      ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+      ctypes.c_void_p]),
+    ("bitnet_rope_freqs", ctypes.c_int,
+     [ctypes.c_int, ctypes.c_double, ctypes.c_int64, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+      ctypes.c_void_p, ctypes.c_void_p]),
+    ("bitnet_rope", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+      ctypes.c_void_p, ctypes.c_void_p]),
+    ("bitnet_kv_append_rope", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int,
+      ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]),
     ("bitnet_attn_decode_workspace_bytes", ctypes.c_size_t, [ctypes.c_int64] * 8),
     ("bitnet_attn_decode", ctypes.c_int,
      [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_int64, ctypes.c_int64,
@@ -383,6 +396,108 @@ def bitnet_kv_append(k, v, q_start, k_cache, v_cache, table, kv_len, stream=None
     st = lib().bitnet_kv_append(ctypes.byref(c), _ptr(k, "k"), _ptr(v, "v"), _dtype(k, "k"),
                                 None if q_start is None else _q_start(q_start, c.n_seqs), n, _stream(stream))
     _check("bitnet_kv_append", st)
+
+
+# ------------------------------------------------------------------------------------------------
+# Between the products: the norm and rotary positions
+# ------------------------------------------------------------------------------------------------
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "turns": 3, "index": 4}      # bitnet_rope_scaling
+
+
+class _Rotation(ctypes.Structure):         # bitnet_rotation
+    _fields_ = [("freqs", ctypes.c_void_p), ("rot_dim", ctypes.c_int64), ("interleaved", ctypes.c_int32), ("gain", ctypes.c_float)]
+
+
+def _rotation(freqs, interleaved, gain):
+    import torch
+    return _Rotation(_ptr(freqs, "freqs", torch.float64), 2 * freqs.numel(), 1 if interleaved else 0, gain)
+
+
+def _here(*tensors) -> None:
+    """A call runs on the current device: its tensors have to be there."""
+    import torch
+    now = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() not in (now, -1):        # tensors of the host have been refused, or will be
+            raise ValueError(f"tensors must be on the current device {now}, got one on {t.get_device()}")
+
+
+def bitnet_norm_quantize(x, gamma, eps: float, xq=None, x_scale=None, x_rowsum=None, residual=None, residual_out=None, y=None,
+                         stream=None) -> None:
+    """Root-mean-square norm of the rows of x ([M, K], float32, or any of the three types that the residual, if any, has too), with
+    the residual's addition before it (residual_out: the sum, in the residual's type) and the int8 codes of a product's activation behind it (xq, x_scale,
+    x_rowsum as bitnet_quantize_act writes them).  y: the normed rows themselves, in any of the three types.  gamma: float32
+    [K], or None."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError(f"x must be [M, K], got {tuple(x.shape)}")
+    M, K = x.shape
+    for t, name in ((residual, "residual"), (residual_out, "residual_out"), (y, "y"), (xq, "xq")):
+        if t is not None and t.shape != x.shape:
+            raise ValueError(f"{name} must have x's shape {tuple(x.shape)}, got {tuple(t.shape)}")
+    for t, name, n in ((gamma, "gamma", K), (x_scale, "x_scale", M), (x_rowsum, "x_rowsum", M)):
+        if t is not None and t.numel() != n:
+            raise ValueError(f"{name} must have {n} entries, got {t.numel()}")
+    if residual_out is not None and residual is not None and residual_out.dtype != residual.dtype:
+        raise TypeError(f"residual_out must be {residual.dtype}, got {residual_out.dtype}")
+    pointers = (_ptr(x, "x"), _ptr(residual, "residual"), _ptr(residual_out, "residual_out"), _ptr(gamma, "gamma", torch.float32),
+                _ptr(y, "y"), _ptr(xq, "xq", torch.int8), _ptr(x_scale, "x_scale", torch.float32),
+                _ptr(x_rowsum, "x_rowsum", torch.int32))
+    _here(x, residual, residual_out, gamma, y, xq, x_scale, x_rowsum)
+    st = lib().bitnet_norm_quantize(pointers[0], _dtype(x, "x"), pointers[1], pointers[2],
+                                    0 if residual is None else _dtype(residual, "residual"), pointers[3], eps, M, K, pointers[4],
+                                    0 if y is None else _dtype(y, "y"), pointers[5], pointers[6], pointers[7], _stream(stream))
+    _check("bitnet_norm_quantize", st)
+
+
+def bitnet_rope_freqs(freqs, theta: float, scaling="none", factor: float = 1.0, original: float = 0.0, low: float = 1.0,
+                      high: float = 32.0, stream=None) -> None:
+    """Turns a position of each pair of a rotation of 2 * freqs.numel() channels, into freqs (float64): theta^(-2i / rot_dim) /
+    2 pi, stretched for contexts longer than `original` as `scaling` says (none, linear, base, turns or index)."""
+    import torch
+    kind = ROPE_SCALINGS[scaling] if isinstance(scaling, str) else int(scaling)
+    pointer = _ptr(freqs, "freqs", torch.float64)
+    _here(freqs)
+    st = lib().bitnet_rope_freqs(kind, theta, 2 * freqs.numel(), factor, original, low, high, pointer, _stream(stream))
+    _check("bitnet_rope_freqs", st)
+
+
+def bitnet_rope(x, pos, freqs, out, head_dim: int, interleaved: bool = False, gain: float = 1.0, stream=None) -> None:
+    """out (which may be x) = x ([tokens, H * head_dim], float32, bfloat16 or float16) with the first 2 * freqs.numel() channels of
+    every head turned to the token's position pos (int32)."""
+    n = x.shape[0]
+    if out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("out must have x's size and type")
+    heads, rest = divmod(x.numel(), max(1, n) * head_dim) if n else (1, 0)
+    if rest:
+        raise ValueError(f"x {tuple(x.shape)} must have rows of whole heads of {head_dim}")
+    r, pointers = _rotation(freqs, interleaved, gain), (_ptr(x, "x"), _list(pos, "pos", n), _ptr(out, "out"))
+    _here(x, pos, freqs, out)
+    st = lib().bitnet_rope(ctypes.byref(r), pointers[0], _dtype(x, "x"), n, heads, head_dim, pointers[1], pointers[2], _stream(stream))
+    _check("bitnet_rope", st)
+
+
+def bitnet_kv_append_rope(k, v, q_start, k_cache, v_cache, table, kv_len, freqs, interleaved: bool = False, gain: float = 1.0,
+                          q=None, q_out=None, stream=None) -> None:
+    """bitnet_kv_append with the keys turned to their positions before they are written; with q ([tokens, H * D], of k's type), q_out
+    (which may be q) receives the query heads of the same tokens turned."""
+    c = _cache(k_cache, v_cache, table, kv_len)
+    n = _rows(k, "k", c.n_kv_heads * c.head_dim)
+    if v.numel() != k.numel() or v.dtype != k.dtype:
+        raise ValueError("k and v must have one size and type")
+    heads = 0
+    if q is not None or q_out is not None:
+        if q is None or q_out is None or q.dtype != k.dtype:
+            raise ValueError("q and q_out go together and have k's type")
+        if q.shape[0] != n:
+            raise ValueError(f"q must have one row for each of the {n} tokens, got {q.shape[0]}")
+        heads = _heads(q, q_out, c, n)
+    r = _rotation(freqs, interleaved, gain)
+    pointers = (_ptr(q, "q"), _ptr(k, "k"), _ptr(v, "v"), None if q_start is None else _q_start(q_start, c.n_seqs), _ptr(q_out, "q_out"))
+    _here(k, v, q_start, k_cache, v_cache, table, kv_len, freqs, q, q_out)
+    st = lib().bitnet_kv_append_rope(ctypes.byref(c), ctypes.byref(r), pointers[0], heads, pointers[1], pointers[2],
+                                     _dtype(k, "k"), pointers[3], n, pointers[4], _stream(stream))
+    _check("bitnet_kv_append_rope", st)
 
 
 def bitnet_attn_decode_workspace_bytes(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int,

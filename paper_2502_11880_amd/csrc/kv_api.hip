@@ -1,7 +1,7 @@
 // C entry points of the paged key-value cache and its attention: argument validation and dispatch.  As in bitnet_api.hip,
 // every check runs on the host before anything is enqueued, and no call allocates, copies to the host or synchronises.
 #include "bitnet_mi355x.h"
-#include "kv_cache.hpp"
+#include "rows.hpp"
 
 namespace {
 
@@ -66,6 +66,23 @@ bitnet::KvCache view_of(const bitnet_kv_cache* c) {
     v.dim = c->head_dim;
     v.chunks = (c->head_dim + 7) / 8;
     return v;
+}
+
+// What both append calls need of their rows.
+int check_append(const bitnet_kv_cache* cache, int src_dtype, const int32_t* q_start, int64_t n_tokens, bool work) {
+    if (const int e = check_cache(cache, work)) return e;
+    if (src_dtype != BITNET_DTYPE_F32 && src_dtype != cache->dtype)
+        return fail(BITNET_E_INVALID, "src_dtype %d: f32 (0) or the cache's (%d) is needed", src_dtype, cache->dtype);
+    if (n_tokens < 0 || n_tokens > kMaxTokens) return fail(BITNET_E_SHAPE, "need 0 <= n_tokens <= 2^24; got %lld", (long long)n_tokens);
+    if (!q_start && n_tokens != cache->n_seqs)
+        return fail(BITNET_E_SHAPE, "without q_start every sequence has one token: n_tokens=%lld, n_seqs=%lld",
+                    (long long)n_tokens, (long long)cache->n_seqs);
+    return BITNET_OK;
+}
+
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
 }
 
 // What both attention calls need of their queries.
@@ -142,13 +159,7 @@ size_t bitnet_kv_page_bytes(int dtype, int64_t page_size, int64_t n_kv_heads, in
 bitnet_status bitnet_kv_append(const bitnet_kv_cache* cache, const void* k, const void* v, int src_dtype,
                                const int32_t* q_start, int64_t n_tokens, void* stream) {
     const bool work = n_tokens > 0 && cache && cache->n_seqs > 0;
-    if (const int e = check_cache(cache, work)) return st(e);
-    if (src_dtype != BITNET_DTYPE_F32 && src_dtype != cache->dtype)
-        return st(fail(BITNET_E_INVALID, "src_dtype %d: f32 (0) or the cache's (%d) is needed", src_dtype, cache->dtype));
-    if (n_tokens < 0 || n_tokens > kMaxTokens) return st(fail(BITNET_E_SHAPE, "need 0 <= n_tokens <= 2^24; got %lld", (long long)n_tokens));
-    if (!q_start && n_tokens != cache->n_seqs)
-        return st(fail(BITNET_E_SHAPE, "without q_start every sequence has one token: n_tokens=%lld, n_seqs=%lld",
-                       (long long)n_tokens, (long long)cache->n_seqs));
+    if (const int e = check_append(cache, src_dtype, q_start, n_tokens, work)) return st(e);
     if (!work) return st(hip_status(hipSuccess, ""));
     if (!k || !v) return st(fail(BITNET_E_INVALID, "null pointer argument"));
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(q_start, 4))
@@ -156,6 +167,32 @@ bitnet_status bitnet_kv_append(const bitnet_kv_cache* cache, const void* k, cons
     return st(hip_status(bitnet::launch_kv_append(view_of(cache), cache->dtype, k, v, src_dtype == BITNET_DTYPE_F32, q_start,
                                                   (int)n_tokens, (hipStream_t)stream),
                          "bitnet_kv_append launch"));
+}
+
+bitnet_status bitnet_kv_append_rope(const bitnet_kv_cache* cache, const bitnet_rotation* rotation, const void* q, int64_t n_heads,
+                                    const void* k, const void* v, int src_dtype, const int32_t* q_start, int64_t n_tokens,
+                                    void* q_out, void* stream) {
+    const bool work = n_tokens > 0 && cache && cache->n_seqs > 0;
+    if (const int e = check_append(cache, src_dtype, q_start, n_tokens, work)) return st(e);
+    if (const int e = bitnet::check_rotation(rotation, cache->head_dim, work)) return st(e);
+    if ((q != nullptr) != (q_out != nullptr)) return st(fail(BITNET_E_INVALID, "q and q_out go together"));
+    if (q && (n_heads < 1 || n_heads > kMaxHeads || n_heads % cache->n_kv_heads != 0))
+        return st(fail(BITNET_E_SHAPE, "need n_heads %% n_kv_heads == 0 and n_heads <= 1024; got %lld over %d", (long long)n_heads,
+                       cache->n_kv_heads));
+    if (!work) return st(hip_status(hipSuccess, ""));
+    if (!k || !v) return st(fail(BITNET_E_INVALID, "null pointer argument"));
+    if (!aligned(q, 16) || !aligned(q_out, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_start, 4))
+        return st(fail(BITNET_E_ALIGN, "q, q_out, k and v need 16-byte alignment, q_start 4-byte"));
+    if (q) {
+        const int64_t row = (int64_t)cache->head_dim * (src_dtype == BITNET_DTYPE_F32 ? 4 : 2) * n_tokens;
+        const int64_t q_bytes = row * n_heads, kv_bytes = row * cache->n_kv_heads;
+        if ((q != q_out && overlap(q, q_bytes, q_out, q_bytes)) || overlap(q_out, q_bytes, k, kv_bytes) || overlap(q_out, q_bytes, v, kv_bytes))
+            return st(fail(BITNET_E_INVALID, "q_out must be q or overlap no input"));
+    }
+    return st(hip_status(bitnet::launch_kv_append_rope(view_of(cache), cache->dtype, q, q ? (int)n_heads : cache->n_kv_heads, k, v,
+                                                       src_dtype == BITNET_DTYPE_F32, q_start, (int)n_tokens,
+                                                       bitnet::rope_of(rotation), q_out, (hipStream_t)stream),
+                         "bitnet_kv_append_rope launch"));
 }
 
 size_t bitnet_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,
