@@ -401,6 +401,27 @@ size_t bitnet_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64
 bitnet_status bitnet_attn_decode(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads, float scale,
                                  int64_t window, int64_t n_sink, void* out, void* ws, size_t ws_bytes, void* stream);
 
+/* Workspace bytes with which bitnet_attn_decode_shared serves n_seqs sequences and fewer, however they are grouped (0 for
+ * unsupported sizes). */
+size_t bitnet_attn_decode_shared_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,
+                                                 int64_t page_size, int64_t max_pages, int64_t window, int64_t n_sink);
+
+/*
+ * bitnet_attn_decode_shared -- bitnet_attn_decode for a batch in which groups of neighbouring sequences begin with the same keys
+ * (beams and forks of one prompt, conversations behind one instruction): what a group shares is read and multiplied once for all
+ * of its sequences.
+ *   group_start   device int32 [n_groups + 1]: sequences group_start[g] .. group_start[g+1] - 1 are group g (first 0, last n_seqs,
+ *                 never decreasing; a group may be empty, or one sequence).  Rows of out that no group owns are not written.
+ *   prefix_len    device int32 [n_groups]: the first prefix_len[g] keys and values of every sequence of the group are those of its
+ *                 first sequence, and are read from that one's pages; what the others' rows of the table name there is not looked
+ *                 at.  Any number of tokens, 0 among them; a sequence that is shorter sees its first kv_len only.
+ *   0 <= n_groups <= n_seqs.  ws: bitnet_attn_decode_shared_workspace_bytes(...) bytes, any contents, nothing kept.  All else (types,
+ *   what is visible, what is not finite, one result for one call) as bitnet_attn_decode.
+ */
+bitnet_status bitnet_attn_decode_shared(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads,
+                                        const int32_t* group_start, const int32_t* prefix_len, int64_t n_groups, float scale,
+                                        int64_t window, int64_t n_sink, void* out, void* ws, size_t ws_bytes, void* stream);
+
 /* Workspace bytes with which bitnet_attn_prefill splits the keys of few queries (0 is a valid answer; 0 also for unsupported
  * sizes).  At most some 40 MB, however many sequences and tokens.  dtype is that of q and out. */
 size_t bitnet_attn_prefill_workspace_bytes(int cache_dtype, int dtype, int64_t n_seqs, int64_t n_tokens, int64_t n_heads,

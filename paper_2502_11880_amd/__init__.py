@@ -82,6 +82,10 @@ _SIGNATURES = [
     ("bitnet_attn_decode", ctypes.c_int,
      [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_int64, ctypes.c_int64,
       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    ("bitnet_attn_decode_shared_workspace_bytes", ctypes.c_size_t, [ctypes.c_int64] * 8),
+    ("bitnet_attn_decode_shared", ctypes.c_int,
+     [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
+      ctypes.c_float, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     ("bitnet_attn_prefill_workspace_bytes", ctypes.c_size_t, [ctypes.c_int] * 2 + [ctypes.c_int64] * 9),
     ("bitnet_attn_prefill", ctypes.c_int,
      [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_float,
@@ -528,6 +532,32 @@ def bitnet_attn_decode(q, k_cache, v_cache, table, kv_len, out, scale: float, wi
                                   n_sink, _ptr(out, "out"), _ptr(ws, "ws"),
                                   0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
     _check("bitnet_attn_decode", st)
+
+
+def bitnet_attn_decode_shared_workspace_bytes(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int,
+                                              max_pages: int, window: int = 0, n_sink: int = 0) -> int:
+    return int(lib().bitnet_attn_decode_shared_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim, page_size, max_pages,
+                                                               window, n_sink))
+
+
+def bitnet_attn_decode_shared(q, group_start, prefix_len, k_cache, v_cache, table, kv_len, out, scale: float, window: int = 0,
+                              n_sink: int = 0, ws=None, stream=None) -> None:
+    """bitnet_attn_decode where sequences group_start[g] .. group_start[g + 1] - 1 share their first prefix_len[g] tokens (int32
+    both): those are read from the first sequence's pages, once for the group."""
+    c = _cache(k_cache, v_cache, table, kv_len)
+    if q.shape[0] != c.n_seqs:
+        raise ValueError(f"q must have one row for each of the {c.n_seqs} sequences, got {q.shape[0]}")
+    groups = prefix_len.numel()
+    if group_start.numel() != groups + 1:
+        raise ValueError(f"group_start must have {groups + 1} entries, got {group_start.numel()}")
+    i32 = _types()[0]
+    pointers = (_ptr(q, "q"), _ptr(group_start, "group_start", i32), _ptr(prefix_len, "prefix_len", i32), _ptr(out, "out"), _ptr(ws, "ws"))
+    heads, dtype = _heads(q, out, c, c.n_seqs), _dtype(q, "q")
+    _here(q, group_start, prefix_len, k_cache, v_cache, table, kv_len, out, ws)
+    st = lib().bitnet_attn_decode_shared(ctypes.byref(c), pointers[0], dtype, heads, pointers[1], pointers[2], groups, scale,
+                                         window, n_sink, pointers[3], pointers[4],
+                                         0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
+    _check("bitnet_attn_decode_shared", st)
 
 
 def bitnet_attn_prefill_workspace_bytes(cache_dtype: int, dtype: int, n_seqs: int, n_tokens: int, n_heads: int,

@@ -225,6 +225,35 @@ bitnet_status bitnet_attn_decode(const bitnet_kv_cache* cache, const void* q, in
                          "bitnet_attn_decode launch"));
 }
 
+size_t bitnet_attn_decode_shared_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,
+                                                 int64_t page_size, int64_t max_pages, int64_t window, int64_t n_sink) {
+    if (shift_of(page_size) < 0 || !heads_ok(n_kv_heads, head_dim) || !rows_ok(n_seqs, max_pages, page_size) || n_heads < 1 ||
+        n_heads > kMaxHeads || n_heads % n_kv_heads || window < 0 || n_sink < 0)
+        return 0;
+    return bitnet::attn_shared_workspace_bytes(n_seqs, (int)n_heads, (int)n_kv_heads, (int)head_dim);
+}
+
+bitnet_status bitnet_attn_decode_shared(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads,
+                                        const int32_t* group_start, const int32_t* prefix_len, int64_t n_groups, float scale,
+                                        int64_t window, int64_t n_sink, void* out, void* ws, size_t ws_bytes, void* stream) {
+    const bool work = cache && cache->n_seqs > 0 && n_groups > 0;
+    if (const int e = check_cache(cache, work)) return st(e);
+    if (const int e = check_attn(cache, dtype, n_heads, window, n_sink)) return st(e);
+    if (n_groups < 0 || n_groups > cache->n_seqs)
+        return st(fail(BITNET_E_SHAPE, "need 0 <= n_groups <= n_seqs; got %lld groups of %lld", (long long)n_groups, (long long)cache->n_seqs));
+    if (!work) return st(hip_status(hipSuccess, ""));
+    if (!q || !out || !group_start || !prefix_len) return st(fail(BITNET_E_INVALID, "null pointer argument"));
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(group_start, 4) || !aligned(prefix_len, 4))
+        return st(fail(BITNET_E_ALIGN, "q and out need 16-byte alignment, group_start and prefix_len 4-byte"));
+    const size_t need = bitnet_attn_decode_shared_workspace_bytes(cache->n_seqs, n_heads, cache->n_kv_heads, cache->head_dim,
+                                                                  cache->page_size, cache->max_pages, window, n_sink);
+    if (const int e = check_workspace(ws, ws_bytes, need)) return st(e);
+    const bitnet::AttnArgs a{q, out, group_start, (int)cache->n_seqs, (int)n_heads, scale, clip(window), clip(n_sink),
+                             dtype == BITNET_DTYPE_F32};
+    return st(hip_status(bitnet::launch_attn_shared(view_of(cache), cache->dtype, a, prefix_len, (int)n_groups, ws, (hipStream_t)stream),
+                         "bitnet_attn_decode_shared launch"));
+}
+
 size_t bitnet_attn_prefill_workspace_bytes(int cache_dtype, int dtype, int64_t n_seqs, int64_t n_tokens, int64_t n_heads,
                                            int64_t n_kv_heads, int64_t head_dim, int64_t page_size, int64_t max_pages,
                                            int64_t window, int64_t n_sink) {

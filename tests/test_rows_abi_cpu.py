@@ -101,3 +101,34 @@ def test_nothing_to_append():
     assert B.lib().bitnet_kv_append_rope(ctypes.byref(_cache()), ctypes.byref(_rot()), None, 0, None, None, 0, FAKE, 0, None, None) == 0
     none = _cache(n_seqs=0)
     assert B.lib().bitnet_kv_append_rope(ctypes.byref(none), ctypes.byref(_rot()), None, 0, None, None, 0, None, 0, None, None) == 0
+
+
+def _shared(cache=None, **kw):
+    a = dict(q=FAKE, dtype=0, heads=4, start=FAKE, prefix=FAKE, groups=2, scale=1.0, window=0, sinks=0, out=FAKE, ws=FAKE, ws_bytes=1 << 40)
+    a.update(kw)
+    c = _cache(**(cache or {}))
+    return B.lib().bitnet_attn_decode_shared(ctypes.byref(c), a["q"], a["dtype"], a["heads"], a["start"], a["prefix"], a["groups"], a["scale"],
+                                             a["window"], a["sinks"], a["out"], a["ws"], a["ws_bytes"], None)
+
+
+@cpu_only
+@pytest.mark.parametrize("status,cache,kw", [
+    (1, dict(dtype=0), {}), (2, dict(ps=48), {}), (2, dict(dim=2), {}), (1, dict(table=None), {}), (3, dict(k=FAKE + 8), {}),
+    (1, {}, dict(dtype=2)), (2, {}, dict(heads=3)), (2, {}, dict(heads=0)), (2, {}, dict(heads=1026)), (1, {}, dict(window=-1)), (1, {}, dict(sinks=-1)),
+    (2, {}, dict(groups=3)), (2, {}, dict(groups=-1)), (1, {}, dict(q=None)), (1, {}, dict(out=None)), (1, {}, dict(start=None)),
+    (1, {}, dict(prefix=None)), (3, {}, dict(q=FAKE + 4)), (3, {}, dict(start=FAKE + 2)), (3, {}, dict(prefix=FAKE + 1))])
+def test_shared_refusals(status, cache, kw):
+    assert _shared(cache, **kw) == status, B.bitnet_last_error()
+
+
+@cpu_only
+def test_shared_workspace_and_nothing_to_do():
+    need = B.bitnet_attn_decode_shared_workspace_bytes(2, 4, 2, 128, 16, 2)
+    if need:
+        assert _shared(ws=None) == 5 and _shared(ws_bytes=need - 1) == 5 and _shared(ws=FAKE + 8, ws_bytes=need) == 3
+    assert _shared(groups=0, q=None, out=None) == 0
+    assert _shared(dict(n_seqs=0), groups=0) == 0
+    sizes = [B.bitnet_attn_decode_shared_workspace_bytes(n, 32, 8, 128, 32, 100) for n in (1, 2, 16, 64, 1000, 1024, 5000)]
+    assert sizes == sorted(sizes)                                    # it serves fewer sequences too
+    assert B.bitnet_attn_decode_shared_workspace_bytes(4, 3, 2, 128, 32, 100) == 0
+    assert B.bitnet_attn_decode_shared_workspace_bytes(4, 4, 2, 130, 32, 100) == 0
