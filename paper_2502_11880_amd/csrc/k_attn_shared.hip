@@ -3,13 +3,38 @@
 // (visible as in the decode without groups: j < L, and with a window j >= L - window or j < n_sink; nothing visible: zeros).  Keys
 // below the group's prefix are those of its first sequence, keys from there on the sequence's own.
 //
-// A wave takes one head of one sequence and walks its keys eight at a time (a word of the values) in plain 32-bit products.
+// A row of the work is a kv head's columns over a run of keys: all query heads of all sequences of a group over its prefix, and
+// the query heads of one sequence over its own keys.  Up to W = 64 columns go through together (heads past 128 channels: 32), 16 to a
+// tile of the matrix instruction, so the prefix is read once for 64 of them; more are rows of their own, which lie in the line
+// below so that work groups of one XCD read the same keys at about the same time.  Keys go in units of 32 through registers
+// (S^T = K Q^T, O^T = V^T P^T, as in the decode without groups: the weights never leave their lane), q waits in LDS.
+//
+// All rows stand in one line, weighted by what a unit of their tiles costs, and every work group takes an equal share of it; its
+// waves take the units in turn.  Every row leaves (maximum, sum, unnormalised output) records in the workspace, one for each share
+// that it crosses, and a second launch joins those of a sequence's prefix and own keys.
+//
+// What is not finite: as in the decode without groups, finite results need no look at the inputs, and a share with others is gone
+// through once more, key by key (redo).
 #include "kv_cache.hpp"
+
+#include <type_traits>
 
 namespace bitnet {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kUnit = 32;            // keys of a unit
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kMaxSeqs = 1024;       // sequences of a launch (more go in several)
+constexpr int kMinShare = 4;         // units of a share, at least: one for each wave
+constexpr int kIds = 512;            // units whose pages a work group looks up at a time
+constexpr uint16_t kNobody = 0xFFFF;
+
+__host__ __device__ constexpr int most_tiles(int dim) { return dim <= 128 ? 4 : 2; }
+// What a unit of a row of one, two and four tiles costs.
+__host__ __device__ constexpr int cost_of(int tiles) { return tiles == 1 ? 4 : tiles == 2 ? 5 : 7; }
+constexpr int kMostCost = 7;
+__host__ __device__ __forceinline__ int tiles_of(int columns) { return columns <= 16 ? 1 : columns <= 32 ? 2 : 4; }
 
 struct SharedArgs {
     KvCache c;
@@ -20,7 +45,203 @@ struct SharedArgs {
     int n_groups, heads, group;
     float scale2;                    // scale * log2 e
     int window, n_sink;
+    int first_seq, n_seqs;           // of this launch
+    int columns;                     // of a row, at most (W)
+    uint8_t* ws;
 };
+
+// The launch's sequences: what each belongs to, and the line.
+struct Index {
+    int64_t start[kMaxSeqs + 1];     // cost of the rows of all sequences before (a group's prefix rows are its first sequence's)
+    int prefix[kMaxSeqs];            // of the group whose first sequence (of this launch) it is
+    int low[kMaxSeqs];               // and the first key that any window of that group reaches
+    uint16_t lead[kMaxSeqs];         // first sequence of its group; kNobody: of none
+    uint16_t members[kMaxSeqs];      // of the group whose first sequence it is
+    int first_row;                   // the first group's first sequence, which may be of a launch before
+};
+// Its copy for the join, at the start of the workspace.
+struct Header {
+    int64_t share;
+    int64_t start[kMaxSeqs + 1];
+    int prefix_units[kMaxSeqs];
+    int own_units[kMaxSeqs];
+    uint16_t lead[kMaxSeqs], members[kMaxSeqs];
+};
+constexpr int64_t kHeaderBytes = (sizeof(Header) + 255) / 256 * 256;
+
+// Records of [maximum, sum, -, -, output of dim channels]: of whole rows by (kind, sequence, head), then of parts of rows, two slots
+// of W a work group: for the row that it goes on with and for the one that it leaves unfinished.
+__host__ __device__ __forceinline__ int record_floats(int dim) { return dim + 4; }
+__device__ __forceinline__ float* whole_record(const SharedArgs& a, int own, int s, int head) {
+    return reinterpret_cast<float*>(a.ws + kHeaderBytes) + (((int64_t)own * a.n_seqs + s) * a.heads + head) * record_floats(a.c.dim);
+}
+__device__ __forceinline__ float* part_record(const SharedArgs& a, int64_t share, int slot, int column) {
+    return reinterpret_cast<float*>(a.ws + kHeaderBytes) +
+           ((int64_t)2 * a.n_seqs * a.heads + (2 * share + slot) * a.columns + column) * record_floats(a.c.dim);
+}
+
+// The keys of a row: those of [begin, end) at `low` and past it, and those below n_sink.  In units of 32: first those of the sinks
+// that lie before the others'.
+struct Keys {
+    int begin, end, first_sink, sink_units, first_unit, units;
+};
+__device__ __forceinline__ Keys keys_of(int begin, int end, int low, int n_sink) {
+    Keys k;
+    k.begin = begin;
+    k.end = end;
+    const int from = low > begin ? low : begin, sinks = min(min(n_sink, low), end);
+    k.first_unit = from / kUnit;
+    const int near = from < end ? (end + kUnit - 1) / kUnit - k.first_unit : 0;
+    k.first_sink = begin / kUnit;
+    k.sink_units = sinks > begin ? (sinks + kUnit - 1) / kUnit - k.first_sink : 0;
+    if (near > 0) k.sink_units = min(k.sink_units, k.first_unit - k.first_sink);
+    k.units = k.sink_units + near;
+    return k;
+}
+__device__ __forceinline__ int unit_key(const Keys& k, int u) {
+    return (u < k.sink_units ? k.first_sink + u : k.first_unit + u - k.sink_units) * kUnit;
+}
+
+__device__ __forceinline__ int behind(const SharedArgs& a, int len) { return a.window > 0 && len > a.window ? len - a.window : 0; }
+__device__ __forceinline__ int rows_of(const SharedArgs& a, int columns) { return (columns + a.columns - 1) / a.columns; }
+// The keys of a sequence's own row, and of its group's prefix.
+__device__ __forceinline__ Keys own_keys(const SharedArgs& a, const Index& x, int s) {
+    if (x.lead[s] == kNobody) return {0, 0, 0, 0, 0, 0};
+    const int len = seq_len(a.c, a.first_seq + s), prefix = x.prefix[x.lead[s]];
+    return keys_of(prefix < len ? prefix : len, len, behind(a, len), a.n_sink);
+}
+__device__ __forceinline__ Keys prefix_keys(const SharedArgs& a, const Index& x, int s) {
+    if (x.members[s] == 0) return {0, 0, 0, 0, 0, 0};
+    return keys_of(0, x.prefix[s], x.low[s], a.n_sink);
+}
+__device__ __forceinline__ int64_t cost_of_rows(const SharedArgs& a, int columns, int units) {
+    const int most = columns < a.columns ? columns : a.columns;
+    return (int64_t)units * cost_of(tiles_of(most)) * rows_of(a, columns) * a.c.kv_heads;
+}
+
+// All of it worked out by every work group: the groups' marks, then sums and the last mark before each sequence in one scan.
+__device__ void build_index(const SharedArgs& a, Index& x, int64_t (&wave_cost)[kWaves], int (&wave_lead)[kWaves]) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, most = a.c.max_pages << a.c.shift;
+    for (int s = tid; s < a.n_seqs; s += kThreads) {
+        x.members[s] = 0;
+        x.low[s] = most;
+    }
+    __syncthreads();
+    for (int g = tid; g < a.n_groups; g += kThreads) {
+        const int b0 = a.group_start[g], b1 = a.group_start[g + 1];
+        if (b0 < 0 || b1 <= b0 || b1 > a.c.n_seqs) continue;
+        const int s0 = max(b0 - a.first_seq, 0), s1 = min(b1 - a.first_seq, a.n_seqs);
+        if (s0 >= s1) continue;
+        const int p = a.prefix_len[g];
+        x.members[s0] = (uint16_t)(s1 - s0);
+        x.prefix[s0] = p < 0 ? 0 : p < most ? p : most;
+        if (s0 == 0) x.first_row = b0;
+    }
+    __syncthreads();
+    int carry = -1;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += kThreads) {
+        const int s = s0 + tid;
+        int lead = s < a.n_seqs && x.members[s] > 0 ? s : -1;
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1) {
+            const int other = __shfl_up(lead, i);
+            if (lane >= i) lead = max(lead, other);
+        }
+        if (lane == 63) wave_lead[wave] = lead;
+        __syncthreads();
+        lead = max(lead, carry);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) lead = max(lead, wave_lead[w]);
+            carry = max(carry, wave_lead[w]);
+        }
+        if (s < a.n_seqs) {
+            const bool owned = lead >= 0 && s < lead + x.members[lead];
+            x.lead[s] = owned ? (uint16_t)lead : kNobody;
+            if (owned && a.window > 0) atomicMin(&x.low[lead], behind(a, seq_len(a.c, a.first_seq + s)));
+        }
+        __syncthreads();
+    }
+    if (a.window == 0) {
+        for (int s = tid; s < a.n_seqs; s += kThreads) x.low[s] = 0;
+        __syncthreads();
+    }
+    int64_t before_all = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += kThreads) {
+        const int s = s0 + tid;
+        int64_t cost = 0;
+        if (s < a.n_seqs)
+            cost = cost_of_rows(a, x.members[s] * a.group, prefix_keys(a, x, s).units) + cost_of_rows(a, a.group, own_keys(a, x, s).units);
+        int64_t sum = cost;
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1) {
+            const int64_t other = __shfl_up((long long)sum, i);
+            if (lane >= i) sum += other;
+        }
+        if (lane == 63) wave_cost[wave] = sum;
+        __syncthreads();
+        int64_t before = before_all;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            before += w < wave ? wave_cost[w] : 0;
+            before_all += wave_cost[w];
+        }
+        if (s < a.n_seqs) x.start[s] = before + sum - cost;
+        __syncthreads();
+    }
+    if (tid == 0) x.start[a.n_seqs] = before_all;
+    __syncthreads();
+}
+
+__device__ __forceinline__ int64_t share_of(int64_t all) {
+    const int64_t want = (all + gridDim.x - 1) / gridDim.x;
+    return want < kMinShare * kMostCost ? kMinShare * kMostCost : want;
+}
+
+// A row, and the units [u0, u1) of it that the share from pos to end holds.
+struct Place {
+    int s, own;                      // the sequence (of the launch) that the row belongs to; its own keys or its group's prefix
+    int kvh, col0, count, members;   // kv head, first column and number of them, sequences that the columns belong to
+    int table_row;
+    int u0, u1;
+    int64_t next;                    // where the next row starts in the line
+    Keys keys;
+};
+__device__ __forceinline__ Place place_of(const SharedArgs& a, const Index& x, int64_t pos, int64_t end) {
+    int lo = 0, hi = a.n_seqs - 1;                        // the last sequence that starts at pos or before
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (x.start[mid] <= pos) lo = mid;
+        else hi = mid - 1;
+    }
+    Place p;
+    p.s = lo;
+    p.own = 0;
+    p.members = x.members[lo];
+    p.keys = prefix_keys(a, x, lo);
+    int64_t at = x.start[lo];
+    const int64_t of_prefix = cost_of_rows(a, p.members * a.group, p.keys.units);
+    if (pos - at >= of_prefix) {
+        at += of_prefix;
+        p.own = 1;
+        p.members = 1;
+        p.keys = own_keys(a, x, lo);
+    }
+    const int columns = p.members * a.group, rows = rows_of(a, columns);
+    const int cost = cost_of(tiles_of(columns < a.columns ? columns : a.columns));
+    const int64_t row_cost = (int64_t)p.keys.units * cost;
+    const int row = (int)((pos - at) / row_cost);
+    at += row * row_cost;
+    p.kvh = row / rows;
+    p.col0 = (row - p.kvh * rows) * a.columns;
+    p.count = columns - p.col0 < a.columns ? columns - p.col0 : a.columns;
+    p.u0 = (int)((pos - at + cost - 1) / cost);
+    const int64_t room = (end - at + cost - 1) / cost;
+    p.u1 = room < p.keys.units ? (int)room : p.keys.units;
+    p.next = at + row_cost;
+    p.table_row = p.own == 0 && lo == 0 ? x.first_row : a.first_seq + lo;
+    return p;
+}
 
 // Head h of sequence b over the keys [from, to) that it sees, in the pages of table row `row`, onto m, l, o and the values that are
 // not finite (odd).  A lane holds channels d = 4 lane .. of q and of the output; every lane the maximum and the sum.
@@ -72,40 +293,560 @@ __device__ __forceinline__ void plain_keys(const SharedArgs& a, const float4& q,
     }
 }
 
-template <int T, bool F32>
-__global__ __launch_bounds__(kThreads) void attn_shared_kernel(SharedArgs a) {
-    const KvCache& c = a.c;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int per_seq = (a.heads + 3) >> 2;
-    const int b = blockIdx.x / per_seq, head = (blockIdx.x - b * per_seq) * 4 + wave;
-    if (head >= a.heads) return;
-    // the group that b belongs to
-    int g = -1;
-    for (int i = threadIdx.x & 63; __any(i < a.n_groups) && g < 0; i += 64) {
-        const int start = i < a.n_groups ? a.group_start[i] : 0, end = i < a.n_groups ? a.group_start[i + 1] : 0;
-        const uint64_t has = __ballot(start >= 0 && start <= b && b < end && end <= c.n_seqs);
-        if (has) g = (i & ~63) + __builtin_ctzll(has);
+// A column's sequence (of the launch), head, and record.
+struct Column {
+    int s, head;
+};
+__device__ __forceinline__ Column column_of(const SharedArgs& a, const Place& p, int column) {
+    const int c = p.col0 + column, member = c / a.group;
+    return {p.s + member, p.kvh * a.group + c - member * a.group};
+}
+__device__ __forceinline__ float* record_of(const SharedArgs& a, const Place& p, int column) {
+    if (p.u0 == 0 && p.u1 == p.keys.units) {
+        const Column c = column_of(a, p, column);
+        return whole_record(a, p.own, c.s, c.head);
     }
-    if (g < 0) return;
-    const int first = a.group_start[g];
-    const int most = c.max_pages << c.shift, prefix = a.prefix_len[g] < 0 ? 0 : a.prefix_len[g] < most ? a.prefix_len[g] : most;
-    const int len = seq_len(c, b), lo = a.window > 0 && len > a.window ? len - a.window : 0;
-    const int d = 4 * (threadIdx.x & 63), kvh = head / a.group;
-    const int64_t row = ((int64_t)b * a.heads + head) * c.dim;
-    const float4 q = load4<T, F32>(a.q, row + (d < c.dim ? d : 0));
+    return part_record(a, blockIdx.x, p.u0 > 0 ? 0 : 1, column);
+}
+
+// A wave's state of a row: running maximum, sum and unnormalised output; lane (m = lane & 15, g = lane >> 4) holds column m of
+// tile n, channels 16 t + 4 g + i of o[n][t].
+template <int DP, int NT>
+struct Row {
+    float m[NT], l[NT];
+    v4f o[NT][DP / 16];
+};
+
+// The columns' lengths and windows.
+struct Columns {
+    float gain[64];
+    int len[64], low[64];
+    int least_len, most_low;         // over those that there are
+};
+
+template <int T, int DP, bool F32, bool FULL, bool PAGE16>
+struct Shared {
+    static constexpr int kQParts = F32 ? Elem<T>::kExactParts : 1;
+    static constexpr int kPParts = F32 ? Elem<T>::kExactParts : 2;
+    static constexpr int kChunks = DP / 8;
+    static constexpr int kMost = 16 * most_tiles(DP);     // columns
+    static constexpr int kWords = kQParts * kChunks * kMost > kWaves * 16 * DP / 4 ? kQParts * kChunks * kMost : kWaves * 16 * DP / 4;
+
+    struct Lds {
+        uint4 q[kWords];                                  // q; then the waves' outputs of a tile
+        Index index;
+        Columns cols;
+        float wave_m[kWaves][kMost], wave_l[kWaves][kMost];
+        int ids[2][kIds];
+        int64_t wave_cost[kWaves];
+        int wave_lead[kWaves];
+        int odd;                                          // some output is not finite
+    };
+
+    // q of the row's columns as operands in LDS: [part][chunk][column][8]; zeros past D and past the columns, which see everything.
+    template <int NT>
+    static __device__ __forceinline__ void stage_q(const SharedArgs& a, const Place& p, Lds& lds) {
+        const int n = threadIdx.x >> 4, sub = threadIdx.x & 15;
+#pragma unroll
+        for (int tile = 0; tile < NT; ++tile) {
+            const int column = 16 * tile + n;
+            const bool used = column < p.count;
+            const Column col = column_of(a, p, used ? column : 0);
+            const int64_t at = ((int64_t)(a.first_seq + col.s) * a.heads + col.head) * a.c.dim;
+            float x[DP / 128 ? DP / 128 : 1][8];
+            float top = 0.0f;
+#pragma unroll
+            for (int r = 0; r < (DP + 127) / 128; ++r) {
+                const int d = 8 * (sub + 16 * r);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (used && d + 4 * half < a.c.dim) v = load4<T, F32>(a.q, at + d + 4 * half);
+                    x[r][4 * half] = v.x;
+                    x[r][4 * half + 1] = v.y;
+                    x[r][4 * half + 2] = v.z;
+                    x[r][4 * half + 3] = v.w;
+                    top = fmaxf(top, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
+                }
+            }
+            float up = 1.0f;
+            if constexpr (F32 && T == kF16) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, __int_as_float(dpp_row_step(__float_as_int(top), i)));
+                up = row_gain(top);
+            }
+            if (sub == 0) {
+                const int len = seq_len(a.c, a.first_seq + col.s);
+                lds.cols.gain[column] = a.scale2 / up;
+                lds.cols.len[column] = used ? len : 1 << 30;
+                lds.cols.low[column] = used ? behind(a, len) : 0;
+            }
+#pragma unroll
+            for (int r = 0; r < (DP + 127) / 128; ++r) {
+                const int c = sub + 16 * r;
+                if (c >= kChunks) continue;
+                if constexpr (F32 && T == kF16) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[r][e] *= up;
+                }
+#pragma unroll
+                for (int part = 0; part < kQParts; ++part) {
+                    uint4 w;
+                    if constexpr (kQParts == 1) {         // values of the cache's type: exact
+                        w = make_uint4(Elem<T>::pack(x[r][0], x[r][1]), Elem<T>::pack(x[r][2], x[r][3]),
+                                       Elem<T>::pack(x[r][4], x[r][5]), Elem<T>::pack(x[r][6], x[r][7]));
+                    } else {
+                        w.x = Elem<T>::part(x[r][0], x[r][1]);
+                        w.y = Elem<T>::part(x[r][2], x[r][3]);
+                        w.z = Elem<T>::part(x[r][4], x[r][5]);
+                        w.w = Elem<T>::part(x[r][6], x[r][7]);
+                    }
+                    lds.q[(part * kChunks + c) * (16 * NT) + column] = w;
+                }
+            }
+        }
+    }
+
+    // The pages of units u0 .. u1 - 1 (at most kIds), and, pages of 16, those of their upper halves.
+    static __device__ __forceinline__ void stage_ids(const KvCache& c, const Place& p, int u0, int u1, int (&ids)[2][kIds]) {
+        const int32_t* table = c.table + (int64_t)p.table_row * c.max_pages;
+        for (int i = threadIdx.x; i < u1 - u0; i += kThreads) {
+            const int at = unit_key(p.keys, u0 + i) >> c.shift;
+            ids[0][i] = table[at];
+            if (PAGE16) ids[1][i] = at + 1 < c.max_pages ? table[at + 1] : -1;
+        }
+    }
+
+    // Units u0 .. u1 - 1 of a row (their pages in ids), this wave's every fourth, into its state.
+    template <int NT>
+    static __device__ __forceinline__ void run(const SharedArgs& a, const Place& p, int u0, int u1, const Lds& lds, Row<DP, NT>& row) {
+        const KvCache& c = a.c;
+        const Keys keys = p.keys;
+        const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int ps = PAGE16 ? 16 : 1 << c.shift;
+        const int dim = FULL ? DP : c.dim, chunks = FULL ? DP / 8 : c.chunks;
+        const int first = u0 + wave;
+        const int count = first < u1 ? (u1 - first + kWaves - 1) / kWaves : 0;
+        if (count == 0) return;
+        const uint16_t* kbase = c.k + (int64_t)p.kvh * chunks * ps * 8;
+        const uint16_t* vbase = c.v + (int64_t)p.kvh * dim * ps;
+        // places of this lane's words in a unit: of the keys, key 8 (m / 4) + m % 4 (+ 4 in the second tile) of chunk g (+ 4 j);
+        // of the values, channel m (+ 16 t) of the eight keys g
+        const uint32_t k_lane = (uint32_t)(g * ps + 8 * (m >> 2) + (m & 3)) * 16, v_lane = (uint32_t)(g * dim + m) * 16;
+        auto load = [](const uint16_t* base, uint32_t offset) {
+            return *reinterpret_cast<const v4u*>(reinterpret_cast<const uint8_t*>(base) + offset);
+        };
+        auto page_of = [&](int half, int it) { return __builtin_amdgcn_readfirstlane(lds.ids[half][wave + kWaves * it]); };
+        v4u kf[2][DP / 32], vf[DP / 16];
+        auto issue_k = [&](int it) {
+            const int key = unit_key(keys, first + kWaves * it);
+            int p0 = page_of(0, it);
+            p0 = page_ok(c, p0) ? p0 : 0;
+            const uint16_t* kp = kbase + (int64_t)p0 * c.k_page + (PAGE16 ? 0 : (key & (ps - 1)) * 8);
+            uint32_t at = k_lane;
+            if (PAGE16 && m >= 8) {     // keys 16 to 31 of the unit: the second page's first 16
+                int p1 = page_of(1, it);
+                p1 = page_ok(c, p1) ? p1 : 0;
+                kp = kbase + (int64_t)p1 * c.k_page;
+                at -= 256;
+            }
+#pragma unroll
+            for (int j = 0; j < DP / 32; ++j) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    v4u w = {0u, 0u, 0u, 0u};
+                    if (FULL || 4 * j + g < chunks) w = load(kp + j * 4 * ps * 8, at + 64 * t);
+                    kf[t][j] = w;
+                }
+            }
+        };
+        auto issue_v = [&](int it) {
+            const int key = unit_key(keys, first + kWaves * it);
+            int p0 = page_of(0, it);
+            p0 = page_ok(c, p0) ? p0 : 0;
+            const uint16_t* vp = vbase + (int64_t)p0 * c.v_page + (PAGE16 ? 0 : (key & (ps - 1)) * dim);
+            uint32_t at = v_lane;
+            if (PAGE16 && g >= 2) {
+                int p1 = page_of(1, it);
+                p1 = page_ok(c, p1) ? p1 : 0;
+                vp = vbase + (int64_t)p1 * c.v_page;
+                at -= (uint32_t)dim * 32;
+            }
+#pragma unroll
+            for (int t = 0; t < DP / 16; ++t) {
+                v4u w = {0u, 0u, 0u, 0u};
+                if (FULL || 16 * t + m < dim) w = load(vp, at + 256 * t);
+                vf[t] = w;
+            }
+        };
+
+        issue_k(0);
+        issue_v(0);
+        // one unit; MORE: the next one's keys are asked for as soon as the scores are formed, its values after the product
+        auto step = [&](int it, auto more_) {
+            constexpr bool MORE = decltype(more_)::value;
+            const int key = unit_key(keys, first + kWaves * it);
+            const bool ok0 = page_ok(c, page_of(0, it)), ok1 = PAGE16 ? page_ok(c, page_of(1, it)) : ok0;
+            v4f s[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            int q_at = g * (16 * NT) + m;
+            asm volatile("" : "+v"(q_at));                // q stays in LDS
+#pragma unroll
+            for (int part = 0; part < kQParts; ++part) {
+#pragma unroll
+                for (int j = 0; j < DP / 32; ++j) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const v4u qf = __builtin_bit_cast(v4u, lds.q[(part * kChunks + 4 * j) * (16 * NT) + 16 * n + q_at]);
+                        s[n][0] = Elem<T>::mfma16(kf[0][j], qf, s[n][0]);
+                        s[n][1] = Elem<T>::mfma16(kf[1][j], qf, s[n][1]);
+                    }
+                }
+            }
+            if constexpr (MORE) issue_k(it + 1);
+            const bool in_row = (ok0 & ok1 & (key >= keys.begin) & (key + kUnit <= keys.end)) != 0;
+            const bool whole = in_row & (key + kUnit <= lds.cols.least_len) & ((key >= lds.cols.most_low) | (key + kUnit <= a.n_sink));
+            if (!in_row) {
+                // keys of no row, or of no page, do not enter the second product: 0 times an infinity would be no 0
+                const bool there = g < 2 ? ok0 : ok1;
+                v4u keep;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int j = key + 8 * g + 2 * w;
+                    keep[w] = ((there & (j >= keys.begin) & (j < keys.end)) ? 0x0000FFFFu : 0u) |
+                              ((there & (j + 1 >= keys.begin) & (j + 1 < keys.end)) ? 0xFFFF0000u : 0u);
+                }
+#pragma unroll
+                for (int t = 0; t < DP / 16; ++t) vf[t] &= keep;
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                // scores of the keys key + 8 g + e, e = 4 t + i
+                const float gain = lds.cols.gain[16 * n + m];
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = s[n][e >> 2][e & 3] * gain;
+                if (!whole) {
+                    const bool there = g < 2 ? ok0 : ok1;
+                    const int end = min(keys.end, lds.cols.len[16 * n + m]), low = lds.cols.low[16 * n + m];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int j = key + 8 * g + e;
+                        x[e] = (there & (j >= keys.begin) & (j < end) & ((j >= low) | (j < a.n_sink))) ? x[e] : kNegInf;
+                    }
+                }
+                float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+                top = max_xor32(max_xor16(top));
+                const float m_new = fmaxf(row.m[n], top);
+                if (__any(m_new > row.m[n])) {
+                    const float alpha = m_new == kNegInf ? 1.0f : exp2_fast(row.m[n] - m_new);
+                    row.l[n] *= alpha;
+#pragma unroll
+                    for (int t = 0; t < DP / 16; ++t) row.o[n][t] *= alpha;
+                    row.m[n] = m_new;
+                }
+                const float base = (row.m[n] == kNegInf ? 0.0f : row.m[n]) - kLift<T>;
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = exp2_fast(x[e] - base);
+                    sum += x[e];
+                }
+                row.l[n] += sum;
+#pragma unroll
+                for (int part = 0; part < kPParts; ++part) {
+                    const v4u pf = {Elem<T>::part(x[0], x[1]), Elem<T>::part(x[2], x[3]), Elem<T>::part(x[4], x[5]), Elem<T>::part(x[6], x[7])};
+#pragma unroll
+                    for (int t = 0; t < DP / 16; ++t) row.o[n][t] = Elem<T>::mfma16(vf[t], pf, row.o[n][t]);
+                }
+            }
+            if constexpr (MORE) issue_v(it + 1);
+        };
+        for (int it = 0; it + 1 < count; ++it) step(it, std::true_type{});
+        step(count - 1, std::false_type{});
+    }
+
+    // One row's units [u0, u1): its records.
+    template <int NT>
+    static __device__ __forceinline__ void do_row(const SharedArgs& a, const Place& p, Lds& lds) {
+        const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, g = lane >> 4;
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int dim = a.c.dim;
+        stage_q<NT>(a, p, lds);
+        stage_ids(a.c, p, p.u0, min(p.u1, p.u0 + kIds), lds.ids);
+        __syncthreads();
+        if (wave == 0) {
+            int len = lane < 16 * NT ? lds.cols.len[lane] : 1 << 30, low = lane < 16 * NT ? lds.cols.low[lane] : 0;
+#pragma unroll
+            for (int i = 1; i < 64; i <<= 1) {
+                len = min(len, __shfl_xor(len, i));
+                low = max(low, __shfl_xor(low, i));
+            }
+            if (lane == 0) {
+                lds.cols.least_len = len;
+                lds.cols.most_low = low;
+            }
+        }
+        __syncthreads();
+        Row<DP, NT> r;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            r.m[n] = kNegInf;
+            r.l[n] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < DP / 16; ++t) r.o[n][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        for (int v0 = p.u0; v0 < p.u1; v0 += kIds) {
+            if (v0 > p.u0) {
+                __syncthreads();
+                stage_ids(a.c, p, v0, min(p.u1, v0 + kIds), lds.ids);
+                __syncthreads();
+            }
+            run<NT>(a, p, v0, min(p.u1, v0 + kIds), lds, r);
+        }
+
+        // the four waves' states become one
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            r.l[n] = sum_xor32(sum_xor16(r.l[n]));
+            if (g == 0) {
+                lds.wave_m[wave][16 * n + m] = r.m[n];
+                lds.wave_l[wave][16 * n + m] = r.l[n];
+            }
+        }
+        float* wave_o = reinterpret_cast<float*>(lds.q);   // [wave][column][channel]
+        const int quads = dim >> 2;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int count = p.count - 16 * n < 16 ? p.count - 16 * n : 16;
+            if (count <= 0) break;
+            __syncthreads();                              // q, and the tile before, have been read
+            float top = lds.wave_m[0][16 * n + m];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, lds.wave_m[w][16 * n + m]);
+            const float f = r.m[n] == kNegInf ? 0.0f : exp2_fast(r.m[n] - top);
+            if (m < count) {
+#pragma unroll
+                for (int t = 0; t < DP / 16; ++t) *reinterpret_cast<v4f*>(&wave_o[(wave * 16 + m) * DP + 16 * t + 4 * g]) = r.o[n][t] * f;
+            }
+            __syncthreads();
+            for (int i = tid; i < count * quads; i += kThreads) {
+                const int col = i / quads, d = 4 * (i - col * quads);
+                v4f o = *reinterpret_cast<const v4f*>(&wave_o[col * DP + d]);
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) o += *reinterpret_cast<const v4f*>(&wave_o[(w * 16 + col) * DP + d]);
+                if (!all_finite(o)) lds.odd = 1;
+                float* rec = record_of(a, p, 16 * n + col);
+                *reinterpret_cast<v4f*>(rec + 4 + d) = o;
+                if (d == 0) {
+                    float mm = kNegInf, ll = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, lds.wave_m[w][16 * n + col]);
+#pragma unroll
+                    for (int w = 0; w < kWaves; ++w) {
+                        const float wm = lds.wave_m[w][16 * n + col];
+                        ll += lds.wave_l[w][16 * n + col] * (wm == kNegInf ? 0.0f : exp2_fast(wm - mm));
+                    }
+                    rec[0] = mm;
+                    rec[1] = ll;
+                }
+            }
+        }
+        __syncthreads();
+    }
+};
+
+// The records of all that a work group has written, from plain products key by key.  A call, and everything worked out again from
+// the kernel's arguments, so that the kernel keeps its registers to itself.
+template <int T, bool F32>
+__device__ __noinline__ void redo(uint64_t args, const Index* x) {
+    const uint32_t low = __builtin_amdgcn_readfirstlane((int)args), high = __builtin_amdgcn_readfirstlane((int)(args >> 32));
+    args = (uint64_t)high << 32 | low;
+    const SharedArgs a = *(const SharedArgs*)(const __attribute__((address_space(4))) void*)args;
+    const int dim = a.c.dim, d = 4 * (threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t all = x->start[a.n_seqs], share = share_of(all);
+    int64_t pos = blockIdx.x * share;
+    const int64_t end = pos + share < all ? pos + share : all;
+    while (pos < end) {
+        const Place p = place_of(a, *x, pos, end);
+        pos = p.next;
+        for (int column = wave; column < p.count; column += kWaves) {
+            if (p.u0 >= p.u1) break;
+            const Column col = column_of(a, p, column);
+            const int len = seq_len(a.c, a.first_seq + col.s);
+            const float4 q = load4<T, F32>(a.q, ((int64_t)(a.first_seq + col.s) * a.heads + col.head) * dim + (d < dim ? d : 0));
+            float m = kNegInf, l = 0.0f;
+            v4f o = {0.0f, 0.0f, 0.0f, 0.0f}, odd = o;
+            for (int u = p.u0; u < p.u1; ++u) {
+                const int key = unit_key(p.keys, u);
+                plain_keys<T>(a, q, p.table_row, p.kvh, max(key, p.keys.begin), min(key + kUnit, p.keys.end), len, behind(a, len), d, m, l, o, odd);
+            }
+            o = or_infinite(o, odd);
+            float* rec = record_of(a, p, column);
+            if (d < dim) *reinterpret_cast<v4f*>(rec + 4 + d) = o;
+            if (d == 0) {
+                rec[0] = m;
+                rec[1] = l;
+            }
+        }
+    }
+}
+
+template <int T, int DP, bool F32, bool FULL, bool PAGE16>
+__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_shared_kernel(SharedArgs a) {
+    using S = Shared<T, DP, F32, FULL, PAGE16>;
+    __shared__ typename S::Lds lds;
+    const int tid = threadIdx.x;
+    if (tid == 0) lds.odd = 0;
+    build_index(a, lds.index, lds.wave_cost, lds.wave_lead);
+    const Index& x = lds.index;
+    const int64_t all = x.start[a.n_seqs], share = share_of(all);
+    if (blockIdx.x == 0) {
+        Header* h = reinterpret_cast<Header*>(a.ws);
+        if (tid == 0) {
+            h->share = share;
+            h->start[a.n_seqs] = all;
+        }
+        for (int s = tid; s < a.n_seqs; s += kThreads) {
+            h->start[s] = x.start[s];
+            h->prefix_units[s] = prefix_keys(a, x, s).units;
+            h->own_units[s] = own_keys(a, x, s).units;
+            h->lead[s] = x.lead[s];
+            h->members[s] = x.members[s];
+        }
+    }
+    int64_t pos = blockIdx.x * share;
+    const int64_t end = pos + share < all ? pos + share : all;
+    while (pos < end) {
+        const Place p = place_of(a, x, pos, end);
+        pos = p.next;
+        if (p.u0 >= p.u1) continue;
+        const int tiles = tiles_of(p.count);
+        if (tiles == 1) S::template do_row<1>(a, p, lds);
+        else if (most_tiles(DP) == 2 || tiles == 2) S::template do_row<2>(a, p, lds);
+        else S::template do_row<most_tiles(DP)>(a, p, lds);
+    }
+    __syncthreads();
+    if (__builtin_expect(lds.odd, 0)) redo<T, F32>((uint64_t)__builtin_amdgcn_kernarg_segment_ptr(), &lds.index);
+}
+
+// A sequence's records, first those of the prefix, in the order of the keys.  A work group 64 quads of channels (head, 4
+// channels); its four waves take the records in turn and are added up in order.
+template <int T, bool F32>
+__global__ __launch_bounds__(256) void attn_shared_join_kernel(SharedArgs a) {
+    __shared__ v4f part_o[4][64];
+    __shared__ float part_m[4][64], part_l[4][64];
+    const Header* h = reinterpret_cast<const Header*>(a.ws);
+    const int dim = a.c.dim, quads = dim >> 2, s = blockIdx.x;
+    const int lead = h->lead[s];
+    if (lead == kNobody) return;
+    const int64_t share = h->share;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int i = blockIdx.y * 64 + lane;
+    const bool in = i < a.heads * quads;
+    const int head = in ? i / quads : 0, d = in ? 4 * (i - head * quads) : 0;
+    const int kvh = head / a.group, in_group = head - kvh * a.group;
+
+    // the records of the prefix (0) and of the own keys (1): shares w0 .. w1, one record each, in a column of their row
+    int64_t w0[2];
+    int n[2], column[2];
+#pragma unroll
+    for (int own = 0; own < 2; ++own) {
+        const int at = own ? s : lead, members = own ? 1 : h->members[lead], units = own ? h->own_units[s] : h->prefix_units[lead];
+        const int columns = members * a.group, rows = rows_of(a, columns), cost = cost_of(tiles_of(columns < a.columns ? columns : a.columns));
+        const int col = (own ? 0 : (s - lead) * a.group) + in_group, row = kvh * rows + col / a.columns;
+        column[own] = col % a.columns;
+        int64_t first = h->start[at] + (int64_t)row * units * cost;
+        if (own) first += cost_of_rows(a, h->members[s] * a.group, h->prefix_units[s]);
+        w0[own] = first / share;
+        n[own] = units == 0 ? 0 : (int)((first + (int64_t)(units - 1) * cost) / share - w0[own]) + 1;
+    }
+    auto record = [&](int j) -> const float* {
+        const int own = j >= n[0];
+        if (own) j -= n[0];
+        if (n[own] == 1) return whole_record(a, own, s, head);
+        return part_record(a, w0[own] + j, j == 0 ? 1 : 0, column[own]);
+    };
+    const int total = n[0] + n[1];
     float m = kNegInf, l = 0.0f;
-    v4f o = {0.0f, 0.0f, 0.0f, 0.0f}, odd = o;
-    plain_keys<T>(a, q, first, kvh, 0, prefix < len ? prefix : len, len, lo, d, m, l, o, odd);
-    plain_keys<T>(a, q, b, kvh, prefix, len, len, lo, d, m, l, o, odd);
-    if (d >= c.dim) return;
-    o = or_infinite(o, odd);
-    l = l == 0.0f ? 1.0f : l;
-    store4<T, F32>(a.out, row + d, o[0] / l, o[1] / l, o[2] / l, o[3] / l);
+    v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int j = wave; j < total; j += 4) {
+        const float* rec = record(j);
+        const float pm = rec[0], pl = rec[1];
+        const v4f po = *reinterpret_cast<const v4f*>(rec + 4 + d);
+        const float top = fmaxf(m, pm);
+        const float fa = m == kNegInf ? 0.0f : exp2_fast(m - top), fb = pm == kNegInf ? 0.0f : exp2_fast(pm - top);
+        o = o * fa + po * fb;
+        l = l * fa + pl * fb;
+        m = top;
+    }
+    part_m[wave][lane] = m;
+    part_l[wave][lane] = l;
+    part_o[wave][lane] = o;
+    __syncthreads();
+    if (wave != 0 || !in) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        const float pm = part_m[w][lane];
+        const float top = fmaxf(m, pm);
+        const float fa = m == kNegInf ? 0.0f : exp2_fast(m - top), fb = pm == kNegInf ? 0.0f : exp2_fast(pm - top);
+        o = o * fa + part_o[w][lane] * fb;
+        l = l * fa + part_l[w][lane] * fb;
+        m = top;
+    }
+    if (__builtin_expect(!all_finite(o) && l == l, 0)) {
+        v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < total; ++j) sum = add_infinite(sum, *reinterpret_cast<const v4f*>(record(j) + 4 + d));
+        o = or_infinite(o, sum);
+    }
+    l = l == 0.0f ? 1.0f : l;                             // no weight: o is 0
+    const int64_t at = ((int64_t)(a.first_seq + s) * a.heads + head) * dim + d;
+    store4<T, F32>(a.out, at, o[0] / l, o[1] / l, o[2] / l, o[3] / l);
+}
+
+// Columns of a row, at most: as many tiles as all of a launch's sequences could fill.
+int columns_of(int64_t n_seqs, int group, int dim) {
+    const int64_t all = (n_seqs < kMaxSeqs ? n_seqs : kMaxSeqs) * group;
+    const int most = 16 * most_tiles(dim);
+    return all <= 16 ? 16 : all <= 32 ? 32 : most;
+}
+constexpr int kMaxGroups = 512;      // work groups of a launch
+
+template <int T, int DP, bool F32, bool FULL, bool PAGE16>
+hipError_t launch_page(SharedArgs a, hipStream_t s) {
+    const int places = (DP > 128 ? 1 : 2) * device_cus(), groups = places < kMaxGroups ? places : kMaxGroups;
+    const int total = a.c.n_seqs;
+    for (int at = 0; at < total; at += kMaxSeqs) {
+        a.first_seq = at;
+        a.n_seqs = total - at < kMaxSeqs ? total - at : kMaxSeqs;
+        hipLaunchKernelGGL((attn_shared_kernel<T, DP, F32, FULL, PAGE16>), dim3((unsigned)groups), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((attn_shared_join_kernel<T, F32>), dim3((unsigned)a.n_seqs, (unsigned)((a.heads * (a.c.dim / 4) + 63) / 64)),
+                           dim3(256), 0, s, a);
+    }
+    return hipGetLastError();
+}
+
+template <int T, int DP, bool F32, bool FULL>
+hipError_t launch(const SharedArgs& a, hipStream_t s) {
+    return a.c.shift == 4 ? launch_page<T, DP, F32, FULL, true>(a, s) : launch_page<T, DP, F32, FULL, false>(a, s);
+}
+
+template <int T, bool F32>
+hipError_t launch_dim(const SharedArgs& a, hipStream_t s) {
+    if (a.c.dim <= 64) return a.c.dim == 64 ? launch<T, 64, F32, true>(a, s) : launch<T, 64, F32, false>(a, s);
+    if (a.c.dim <= 128) return a.c.dim == 128 ? launch<T, 128, F32, true>(a, s) : launch<T, 128, F32, false>(a, s);
+    return launch<T, 256, F32, false>(a, s);
 }
 
 }  // namespace
 
-size_t attn_shared_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim) { return 0; }
+size_t attn_shared_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim) {
+    const int64_t n = n_seqs < kMaxSeqs ? n_seqs : kMaxSeqs, records = 2 * n * heads + 2 * kMaxGroups * (int64_t)columns_of(n, heads / kv_heads, dim);
+    return (size_t)kHeaderBytes + (size_t)records * record_floats(dim) * 4;
+}
 
 hipError_t launch_attn_shared(const KvCache& c, int dtype, const AttnArgs& args, const int32_t* prefix_len, int n_groups, void* ws,
                               hipStream_t s) {
@@ -121,15 +862,10 @@ hipError_t launch_attn_shared(const KvCache& c, int dtype, const AttnArgs& args,
     a.scale2 = args.scale * kLog2e;
     a.window = args.window;
     a.n_sink = args.n_sink;
-    const dim3 grid((unsigned)(c.n_seqs * ((args.heads + 3) / 4)));
-    if (dtype == kBf16) {
-        if (args.f32) hipLaunchKernelGGL((attn_shared_kernel<kBf16, true>), grid, dim3(kThreads), 0, s, a);
-        else hipLaunchKernelGGL((attn_shared_kernel<kBf16, false>), grid, dim3(kThreads), 0, s, a);
-    } else {
-        if (args.f32) hipLaunchKernelGGL((attn_shared_kernel<kF16, true>), grid, dim3(kThreads), 0, s, a);
-        else hipLaunchKernelGGL((attn_shared_kernel<kF16, false>), grid, dim3(kThreads), 0, s, a);
-    }
-    return hipGetLastError();
+    a.columns = columns_of(c.n_seqs, a.group, c.dim);
+    a.ws = static_cast<uint8_t*>(ws);
+    if (dtype == kBf16) return args.f32 ? launch_dim<kBf16, true>(a, s) : launch_dim<kBf16, false>(a, s);
+    return args.f32 ? launch_dim<kF16, true>(a, s) : launch_dim<kF16, false>(a, s);
 }
 
 }  // namespace bitnet
