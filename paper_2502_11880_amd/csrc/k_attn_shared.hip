@@ -30,10 +30,16 @@ constexpr int kMinShare = 4;         // units of a share, at least: one for each
 constexpr int kIds = 512;            // units whose pages a work group looks up at a time
 constexpr uint16_t kNobody = 0xFFFF;
 
-__host__ __device__ constexpr int most_tiles(int dim) { return dim <= 128 ? 4 : 2; }
-// What a unit of a row of one, two and four tiles costs.
+__host__ __device__ constexpr int most_tiles(int dim) { return dim <= 64 ? 4 : 2; }
+// What a unit of a row of one, two and four tiles costs, and what its start does (q, pages and first keys are three reads in a row,
+// and in the end the waves' states become one).
 __host__ __device__ constexpr int cost_of(int tiles) { return tiles == 1 ? 4 : tiles == 2 ? 5 : 7; }
-constexpr int kMostCost = 7;
+constexpr int kMostCost = 7, kStartCost = 12;
+__host__ __device__ __forceinline__ int64_t row_cost_of(int units, int cost) { return units == 0 ? 0 : kStartCost + (int64_t)units * cost; }
+// The first unit of a row that starts `before` or later in it: the first at 0, the others behind the start's cost.
+__host__ __device__ __forceinline__ int64_t unit_at(int64_t before, int cost) {
+    return before <= 0 ? 0 : before <= kStartCost + cost ? 1 : (before - kStartCost + cost - 1) / cost;
+}
 __host__ __device__ __forceinline__ int tiles_of(int columns) { return columns <= 16 ? 1 : columns <= 32 ? 2 : 4; }
 
 struct SharedArgs {
@@ -116,7 +122,7 @@ __device__ __forceinline__ Keys prefix_keys(const SharedArgs& a, const Index& x,
 }
 __device__ __forceinline__ int64_t cost_of_rows(const SharedArgs& a, int columns, int units) {
     const int most = columns < a.columns ? columns : a.columns;
-    return (int64_t)units * cost_of(tiles_of(most)) * rows_of(a, columns) * a.c.kv_heads;
+    return row_cost_of(units, cost_of(tiles_of(most))) * rows_of(a, columns) * a.c.kv_heads;
 }
 
 // All of it worked out by every work group: the groups' marks, then sums and the last mark before each sequence in one scan.
@@ -195,7 +201,8 @@ __device__ void build_index(const SharedArgs& a, Index& x, int64_t (&wave_cost)[
 
 __device__ __forceinline__ int64_t share_of(int64_t all) {
     const int64_t want = (all + gridDim.x - 1) / gridDim.x;
-    return want < kMinShare * kMostCost ? kMinShare * kMostCost : want;
+    constexpr int64_t least = kStartCost + kMinShare * kMostCost;   // no share lies within one unit, nor within a start
+    return want < least ? least : want;
 }
 
 // A row, and the units [u0, u1) of it that the share from pos to end holds.
@@ -229,14 +236,14 @@ __device__ __forceinline__ Place place_of(const SharedArgs& a, const Index& x, i
     }
     const int columns = p.members * a.group, rows = rows_of(a, columns);
     const int cost = cost_of(tiles_of(columns < a.columns ? columns : a.columns));
-    const int64_t row_cost = (int64_t)p.keys.units * cost;
+    const int64_t row_cost = row_cost_of(p.keys.units, cost);
     const int row = (int)((pos - at) / row_cost);
     at += row * row_cost;
     p.kvh = row / rows;
     p.col0 = (row - p.kvh * rows) * a.columns;
     p.count = columns - p.col0 < a.columns ? columns - p.col0 : a.columns;
-    p.u0 = (int)((pos - at + cost - 1) / cost);
-    const int64_t room = (end - at + cost - 1) / cost;
+    p.u0 = (int)unit_at(pos - at, cost);
+    const int64_t room = unit_at(end - at, cost);
     p.u1 = room < p.keys.units ? (int)room : p.keys.units;
     p.next = at + row_cost;
     p.table_row = p.own == 0 && lo == 0 ? x.first_row : a.first_seq + lo;
@@ -758,10 +765,11 @@ __global__ __launch_bounds__(256) void attn_shared_join_kernel(SharedArgs a) {
         const int columns = members * a.group, rows = rows_of(a, columns), cost = cost_of(tiles_of(columns < a.columns ? columns : a.columns));
         const int col = (own ? 0 : (s - lead) * a.group) + in_group, row = kvh * rows + col / a.columns;
         column[own] = col % a.columns;
-        int64_t first = h->start[at] + (int64_t)row * units * cost;
+        int64_t first = h->start[at] + row * row_cost_of(units, cost);
         if (own) first += cost_of_rows(a, h->members[s] * a.group, h->prefix_units[s]);
         w0[own] = first / share;
-        n[own] = units == 0 ? 0 : (int)((first + (int64_t)(units - 1) * cost) / share - w0[own]) + 1;
+        const int64_t last = units < 2 ? first : first + kStartCost + (int64_t)(units - 1) * cost;
+        n[own] = units == 0 ? 0 : (int)(last / share - w0[own]) + 1;
     }
     auto record = [&](int j) -> const float* {
         const int own = j >= n[0];
