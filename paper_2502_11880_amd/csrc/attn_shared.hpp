@@ -1,0 +1,125 @@
+// Decode over shared prefixes: the rows of a launch, where their results go, and how the parts of a call find them.
+#pragma once
+
+#include "kv_cache.hpp"
+
+namespace bitnet {
+
+constexpr int kSharedSeqs = 1024;    // sequences of a launch (more go in several)
+constexpr int kSharedGroups = 512;   // work groups of a launch
+constexpr uint16_t kNobody = 0xFFFF;
+// A prefix is gone through in registers for up to this many columns (query heads of a kv head, of all sequences of the group), and
+// in shared memory, kWideColumns at a time, for more.
+constexpr int kNarrowColumns = 64;
+constexpr int kWideColumns = 128;
+constexpr int kWideTile = 64;        // keys
+constexpr int kWideCost = 2, kWideStart = 6;   // of a tile, and of a row's start
+
+struct SharedArgs {
+    KvCache c;
+    const void* q;
+    void* out;
+    const int32_t* group_start;
+    const int32_t* prefix_len;
+    int n_groups, heads, group;
+    float scale2;                    // scale * log2 e
+    int window, n_sink;
+    int first_seq, n_seqs;           // of this launch
+    int columns;                     // of a row, at most (W)
+    int wide_groups;                 // work groups of the launch for wide prefixes; 0: the sequences are too few for one
+    uint8_t* ws;
+};
+
+// The launch's sequences: what each belongs to, and the line.
+struct Index {
+    int64_t start[kSharedSeqs + 1];     // cost of the rows of all sequences before (a group's prefix rows are its first sequence's)
+    int prefix[kSharedSeqs];            // of the group whose first sequence (of this launch) it is
+    int low[kSharedSeqs];               // and the first key that any window of that group reaches
+    int len[kSharedSeqs];
+    uint16_t lead[kSharedSeqs];         // first sequence of its group; kNobody: of none
+    uint16_t members[kSharedSeqs];      // of the group whose first sequence it is
+    int first_row;                   // the first group's first sequence, which may be of a launch before
+};
+// What the later launches need of it, at the start of the workspace: the line, and the line of the prefixes that have a launch of
+// their own (units of kWideTile keys).
+struct Header {
+    int64_t share, wide_share;
+    int64_t start[kSharedSeqs + 1], wide_start[kSharedSeqs + 1];
+    int prefix_units[kSharedSeqs], own_units[kSharedSeqs], prefix[kSharedSeqs], low[kSharedSeqs];
+    uint16_t lead[kSharedSeqs], members[kSharedSeqs];
+    int first_row;
+};
+constexpr int64_t kHeaderBytes = (sizeof(Header) + 255) / 256 * 256;
+
+// Records of [maximum, sum, -, -, output of dim channels]: of whole rows by (kind, sequence, head), then of parts of rows, two slots
+// of W a work group: for the row that it goes on with and for the one that it leaves unfinished.  Then those of the launch for wide
+// prefixes.
+__host__ __device__ __forceinline__ int record_floats(int dim) { return dim + 4; }
+__device__ __forceinline__ float* whole_record(const SharedArgs& a, int own, int s, int head) {
+    return reinterpret_cast<float*>(a.ws + kHeaderBytes) + (((int64_t)own * a.n_seqs + s) * a.heads + head) * record_floats(a.c.dim);
+}
+__device__ __forceinline__ float* part_record(const SharedArgs& a, int64_t share, int slot, int column) {
+    return reinterpret_cast<float*>(a.ws + kHeaderBytes) +
+           ((int64_t)2 * a.n_seqs * a.heads + (2 * share + slot) * a.columns + column) * record_floats(a.c.dim);
+}
+
+__device__ __forceinline__ float* wide_record(const SharedArgs& a, int64_t share, int slot, int column) {
+    return reinterpret_cast<float*>(a.ws + kHeaderBytes) +
+           ((int64_t)2 * a.n_seqs * a.heads + (int64_t)2 * kSharedGroups * a.columns + (2 * share + slot) * kWideColumns + column) *
+               record_floats(a.c.dim);
+}
+
+// The keys of a row: those of [begin, end) at `low` and past it, and those below n_sink.  In units: first those of the sinks
+// that lie before the others'.
+struct Keys {
+    int begin, end, first_sink, sink_units, first_unit, units;
+};
+template <int kUnit>
+__device__ __forceinline__ Keys keys_of(int begin, int end, int low, int n_sink) {
+    Keys k;
+    k.begin = begin;
+    k.end = end;
+    const int from = low > begin ? low : begin, sinks = min(min(n_sink, low), end);
+    k.first_unit = from / kUnit;
+    const int near = from < end ? (end + kUnit - 1) / kUnit - k.first_unit : 0;
+    k.first_sink = begin / kUnit;
+    k.sink_units = sinks > begin ? (sinks + kUnit - 1) / kUnit - k.first_sink : 0;
+    if (near > 0) k.sink_units = min(k.sink_units, k.first_unit - k.first_sink);
+    k.units = k.sink_units + near;
+    return k;
+}
+
+__device__ __forceinline__ int behind(const SharedArgs& a, int len) { return a.window > 0 && len > a.window ? len - a.window : 0; }
+__device__ __forceinline__ bool is_wide(int columns) { return columns > kNarrowColumns; }
+
+// The line: a row of n units costs start + n cost, and nothing where it has none.
+__device__ __forceinline__ int64_t line_cost(int units, int cost, int start) { return units == 0 ? 0 : start + (int64_t)units * cost; }
+// The first unit of a row that starts `before` or later in it: the first at 0, the others behind the start's cost.
+__device__ __forceinline__ int64_t line_unit(int64_t before, int cost, int start) {
+    return before <= 0 ? 0 : before <= start + cost ? 1 : (before - start + cost - 1) / cost;
+}
+// The share of every work group; none lies within one unit, nor within a start.
+__device__ __forceinline__ int64_t line_share(int64_t all, int groups, int64_t least) {
+    const int64_t want = (all + groups - 1) / groups;
+    return want < least ? least : want;
+}
+// a / b of numbers that are not negative: a 64-bit division is a hundred instructions and more.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+// Where a row's parts lie: shares first .. first + count - 1.
+struct Parts {
+    int64_t first;
+    int count;
+};
+__device__ __forceinline__ Parts parts_of_row(int64_t at, int units, int cost, int start, int64_t share) {
+    if (units == 0) return {0, 0};
+    const int64_t first = divide(at, share), last = divide(units < 2 ? at : at + start + (int64_t)(units - 1) * cost, share);
+    return {first, (int)(last - first) + 1};
+}
+
+// The prefixes of more than kNarrowColumns columns (k_attn_shared_wide.hip).
+int attn_shared_wide_groups(int dim, bool f32);
+hipError_t launch_attn_shared_wide(const SharedArgs& a, int dtype, bool f32, hipStream_t s);
+
+}  // namespace bitnet

@@ -15,7 +15,7 @@
 //
 // What is not finite: as in the decode without groups, finite results need no look at the inputs, and a share with others is gone
 // through once more, key by key (redo).
-#include "kv_cache.hpp"
+#include "attn_shared.hpp"
 
 #include <type_traits>
 
@@ -25,104 +25,71 @@ namespace {
 constexpr int kUnit = 32;            // keys of a unit
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kMaxSeqs = 1024;       // sequences of a launch (more go in several)
-constexpr int kMinShare = 4;         // units of a share, at least: one for each wave
 constexpr int kIds = 512;            // units whose pages a work group looks up at a time
-constexpr uint16_t kNobody = 0xFFFF;
 
 __host__ __device__ constexpr int most_tiles(int dim) { return dim <= 64 ? 4 : 2; }
 // What a unit of a row of one, two and four tiles costs, and what its start does (q, pages and first keys are three reads in a row,
 // and in the end the waves' states become one).
 __host__ __device__ constexpr int cost_of(int tiles) { return tiles == 1 ? 4 : tiles == 2 ? 5 : 7; }
-constexpr int kMostCost = 7, kStartCost = 12;
-__host__ __device__ __forceinline__ int64_t row_cost_of(int units, int cost) { return units == 0 ? 0 : kStartCost + (int64_t)units * cost; }
-// The first unit of a row that starts `before` or later in it: the first at 0, the others behind the start's cost.
-__host__ __device__ __forceinline__ int64_t unit_at(int64_t before, int cost) {
-    return before <= 0 ? 0 : before <= kStartCost + cost ? 1 : (before - kStartCost + cost - 1) / cost;
-}
+constexpr int kMostCost = 7, kStartCost = 20;
+constexpr int64_t kLeastShare = kStartCost + 2 * kMostCost;
 __host__ __device__ __forceinline__ int tiles_of(int columns) { return columns <= 16 ? 1 : columns <= 32 ? 2 : 4; }
 
-struct SharedArgs {
-    KvCache c;
-    const void* q;
-    void* out;
-    const int32_t* group_start;
-    const int32_t* prefix_len;
-    int n_groups, heads, group;
-    float scale2;                    // scale * log2 e
-    int window, n_sink;
-    int first_seq, n_seqs;           // of this launch
-    int columns;                     // of a row, at most (W)
-    uint8_t* ws;
-};
-
-// The launch's sequences: what each belongs to, and the line.
-struct Index {
-    int64_t start[kMaxSeqs + 1];     // cost of the rows of all sequences before (a group's prefix rows are its first sequence's)
-    int prefix[kMaxSeqs];            // of the group whose first sequence (of this launch) it is
-    int low[kMaxSeqs];               // and the first key that any window of that group reaches
-    uint16_t lead[kMaxSeqs];         // first sequence of its group; kNobody: of none
-    uint16_t members[kMaxSeqs];      // of the group whose first sequence it is
-    int first_row;                   // the first group's first sequence, which may be of a launch before
-};
-// Its copy for the join, at the start of the workspace.
-struct Header {
-    int64_t share;
-    int64_t start[kMaxSeqs + 1];
-    int prefix_units[kMaxSeqs];
-    int own_units[kMaxSeqs];
-    uint16_t lead[kMaxSeqs], members[kMaxSeqs];
-};
-constexpr int64_t kHeaderBytes = (sizeof(Header) + 255) / 256 * 256;
-
-// Records of [maximum, sum, -, -, output of dim channels]: of whole rows by (kind, sequence, head), then of parts of rows, two slots
-// of W a work group: for the row that it goes on with and for the one that it leaves unfinished.
-__host__ __device__ __forceinline__ int record_floats(int dim) { return dim + 4; }
-__device__ __forceinline__ float* whole_record(const SharedArgs& a, int own, int s, int head) {
-    return reinterpret_cast<float*>(a.ws + kHeaderBytes) + (((int64_t)own * a.n_seqs + s) * a.heads + head) * record_floats(a.c.dim);
-}
-__device__ __forceinline__ float* part_record(const SharedArgs& a, int64_t share, int slot, int column) {
-    return reinterpret_cast<float*>(a.ws + kHeaderBytes) +
-           ((int64_t)2 * a.n_seqs * a.heads + (2 * share + slot) * a.columns + column) * record_floats(a.c.dim);
-}
-
-// The keys of a row: those of [begin, end) at `low` and past it, and those below n_sink.  In units of 32: first those of the sinks
-// that lie before the others'.
-struct Keys {
-    int begin, end, first_sink, sink_units, first_unit, units;
-};
-__device__ __forceinline__ Keys keys_of(int begin, int end, int low, int n_sink) {
-    Keys k;
-    k.begin = begin;
-    k.end = end;
-    const int from = low > begin ? low : begin, sinks = min(min(n_sink, low), end);
-    k.first_unit = from / kUnit;
-    const int near = from < end ? (end + kUnit - 1) / kUnit - k.first_unit : 0;
-    k.first_sink = begin / kUnit;
-    k.sink_units = sinks > begin ? (sinks + kUnit - 1) / kUnit - k.first_sink : 0;
-    if (near > 0) k.sink_units = min(k.sink_units, k.first_unit - k.first_sink);
-    k.units = k.sink_units + near;
-    return k;
-}
 __device__ __forceinline__ int unit_key(const Keys& k, int u) {
     return (u < k.sink_units ? k.first_sink + u : k.first_unit + u - k.sink_units) * kUnit;
 }
-
-__device__ __forceinline__ int behind(const SharedArgs& a, int len) { return a.window > 0 && len > a.window ? len - a.window : 0; }
 __device__ __forceinline__ int rows_of(const SharedArgs& a, int columns) { return (columns + a.columns - 1) / a.columns; }
 // The keys of a sequence's own row, and of its group's prefix.
 __device__ __forceinline__ Keys own_keys(const SharedArgs& a, const Index& x, int s) {
     if (x.lead[s] == kNobody) return {0, 0, 0, 0, 0, 0};
-    const int len = seq_len(a.c, a.first_seq + s), prefix = x.prefix[x.lead[s]];
-    return keys_of(prefix < len ? prefix : len, len, behind(a, len), a.n_sink);
+    const int len = x.len[s], prefix = x.prefix[x.lead[s]];
+    return keys_of<kUnit>(prefix < len ? prefix : len, len, behind(a, len), a.n_sink);
 }
 __device__ __forceinline__ Keys prefix_keys(const SharedArgs& a, const Index& x, int s) {
-    if (x.members[s] == 0) return {0, 0, 0, 0, 0, 0};
-    return keys_of(0, x.prefix[s], x.low[s], a.n_sink);
+    const int members = x.members[s];
+    if (members == 0 || is_wide(members * a.group)) return {0, 0, 0, 0, 0, 0};
+    return keys_of<kUnit>(0, x.prefix[s], x.low[s], a.n_sink);
+}
+__device__ __forceinline__ int cost_of_columns(const SharedArgs& a, int columns) {
+    return cost_of(tiles_of(columns < a.columns ? columns : a.columns));
 }
 __device__ __forceinline__ int64_t cost_of_rows(const SharedArgs& a, int columns, int units) {
-    const int most = columns < a.columns ? columns : a.columns;
-    return row_cost_of(units, cost_of(tiles_of(most))) * rows_of(a, columns) * a.c.kv_heads;
+    return line_cost(units, cost_of_columns(a, columns), kStartCost) * rows_of(a, columns) * a.c.kv_heads;
+}
+// Of a group's wide prefix: its units, and the cost of its rows.
+__device__ __forceinline__ int64_t wide_cost(const SharedArgs& a, const Index& x, int s) {
+    const int columns = x.members[s] * a.group;
+    if (!is_wide(columns)) return 0;
+    const int units = keys_of<kWideTile>(0, x.prefix[s], x.low[s], a.n_sink).units;
+    return line_cost(units, kWideCost, kWideStart) * ((columns + kWideColumns - 1) / kWideColumns) * a.c.kv_heads;
+}
+
+// start[s]: the sum of cost(i) over i < s, for s up to n.
+template <typename F>
+__device__ __forceinline__ void sum_line(int n, F cost_at, int64_t* start, int64_t (&wave_cost)[kWaves]) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int64_t before_all = 0;
+    for (int s0 = 0; s0 < n; s0 += kThreads) {
+        const int s = s0 + tid;
+        const int64_t cost = s < n ? cost_at(s) : 0;
+        int64_t sum = cost;
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1) {
+            const int64_t other = __shfl_up((long long)sum, i);
+            if (lane >= i) sum += other;
+        }
+        if (lane == 63) wave_cost[wave] = sum;
+        __syncthreads();
+        int64_t before = before_all;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            before += w < wave ? wave_cost[w] : 0;
+            before_all += wave_cost[w];
+        }
+        if (s < n) start[s] = before + sum - cost;
+        __syncthreads();
+    }
+    if (tid == 0) start[n] = before_all;
 }
 
 // All of it worked out by every work group: the groups' marks, then sums and the last mark before each sequence in one scan.
@@ -130,7 +97,8 @@ __device__ void build_index(const SharedArgs& a, Index& x, int64_t (&wave_cost)[
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, most = a.c.max_pages << a.c.shift;
     for (int s = tid; s < a.n_seqs; s += kThreads) {
         x.members[s] = 0;
-        x.low[s] = most;
+        x.low[s] = a.window > 0 ? most : 0;
+        x.len[s] = seq_len(a.c, a.first_seq + s);
     }
     __syncthreads();
     for (int g = tid; g < a.n_groups; g += kThreads) {
@@ -164,46 +132,17 @@ __device__ void build_index(const SharedArgs& a, Index& x, int64_t (&wave_cost)[
         if (s < a.n_seqs) {
             const bool owned = lead >= 0 && s < lead + x.members[lead];
             x.lead[s] = owned ? (uint16_t)lead : kNobody;
-            if (owned && a.window > 0) atomicMin(&x.low[lead], behind(a, seq_len(a.c, a.first_seq + s)));
+            if (owned && a.window > 0) atomicMin(&x.low[lead], behind(a, x.len[s]));
         }
         __syncthreads();
     }
-    if (a.window == 0) {
-        for (int s = tid; s < a.n_seqs; s += kThreads) x.low[s] = 0;
-        __syncthreads();
-    }
-    int64_t before_all = 0;
-    for (int s0 = 0; s0 < a.n_seqs; s0 += kThreads) {
-        const int s = s0 + tid;
-        int64_t cost = 0;
-        if (s < a.n_seqs)
-            cost = cost_of_rows(a, x.members[s] * a.group, prefix_keys(a, x, s).units) + cost_of_rows(a, a.group, own_keys(a, x, s).units);
-        int64_t sum = cost;
-#pragma unroll
-        for (int i = 1; i < 64; i <<= 1) {
-            const int64_t other = __shfl_up((long long)sum, i);
-            if (lane >= i) sum += other;
-        }
-        if (lane == 63) wave_cost[wave] = sum;
-        __syncthreads();
-        int64_t before = before_all;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            before += w < wave ? wave_cost[w] : 0;
-            before_all += wave_cost[w];
-        }
-        if (s < a.n_seqs) x.start[s] = before + sum - cost;
-        __syncthreads();
-    }
-    if (tid == 0) x.start[a.n_seqs] = before_all;
+    sum_line(a.n_seqs, [&](int s) {
+        return cost_of_rows(a, x.members[s] * a.group, prefix_keys(a, x, s).units) + cost_of_rows(a, a.group, own_keys(a, x, s).units);
+    }, x.start, wave_cost);
     __syncthreads();
 }
 
-__device__ __forceinline__ int64_t share_of(int64_t all) {
-    const int64_t want = (all + gridDim.x - 1) / gridDim.x;
-    constexpr int64_t least = kStartCost + kMinShare * kMostCost;   // no share lies within one unit, nor within a start
-    return want < least ? least : want;
-}
+__device__ __forceinline__ int64_t share_of(int64_t all) { return line_share(all, gridDim.x, kLeastShare); }
 
 // A row, and the units [u0, u1) of it that the share from pos to end holds.
 struct Place {
@@ -235,15 +174,15 @@ __device__ __forceinline__ Place place_of(const SharedArgs& a, const Index& x, i
         p.keys = own_keys(a, x, lo);
     }
     const int columns = p.members * a.group, rows = rows_of(a, columns);
-    const int cost = cost_of(tiles_of(columns < a.columns ? columns : a.columns));
-    const int64_t row_cost = row_cost_of(p.keys.units, cost);
-    const int row = (int)((pos - at) / row_cost);
+    const int cost = cost_of_columns(a, columns);
+    const int64_t row_cost = line_cost(p.keys.units, cost, kStartCost);
+    const int row = (int)divide(pos - at, row_cost);
     at += row * row_cost;
     p.kvh = row / rows;
     p.col0 = (row - p.kvh * rows) * a.columns;
     p.count = columns - p.col0 < a.columns ? columns - p.col0 : a.columns;
-    p.u0 = (int)unit_at(pos - at, cost);
-    const int64_t room = unit_at(end - at, cost);
+    p.u0 = (int)line_unit(pos - at, cost, kStartCost);
+    const int64_t room = line_unit(end - at, cost, kStartCost);
     p.u1 = room < p.keys.units ? (int)room : p.keys.units;
     p.next = at + row_cost;
     p.table_row = p.own == 0 && lo == 0 ? x.first_row : a.first_seq + lo;
@@ -328,7 +267,6 @@ struct Row {
 struct Columns {
     float gain[64];
     int len[64], low[64];
-    int least_len, most_low;         // over those that there are
 };
 
 template <int T, int DP, bool F32, bool FULL, bool PAGE16>
@@ -383,7 +321,7 @@ struct Shared {
                 up = row_gain(top);
             }
             if (sub == 0) {
-                const int len = seq_len(a.c, a.first_seq + col.s);
+                const int len = lds.index.len[col.s];
                 lds.cols.gain[column] = a.scale2 / up;
                 lds.cols.len[column] = used ? len : 1 << 30;
                 lds.cols.low[column] = used ? behind(a, len) : 0;
@@ -426,7 +364,8 @@ struct Shared {
 
     // Units u0 .. u1 - 1 of a row (their pages in ids), this wave's every fourth, into its state.
     template <int NT>
-    static __device__ __forceinline__ void run(const SharedArgs& a, const Place& p, int u0, int u1, const Lds& lds, Row<DP, NT>& row) {
+    static __device__ __forceinline__ void run(const SharedArgs& a, const Place& p, int u0, int u1, int least_len, int most_low, const Lds& lds,
+                                               Row<DP, NT>& row) {
         const KvCache& c = a.c;
         const Keys keys = p.keys;
         const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
@@ -441,8 +380,11 @@ struct Shared {
         // places of this lane's words in a unit: of the keys, key 8 (m / 4) + m % 4 (+ 4 in the second tile) of chunk g (+ 4 j);
         // of the values, channel m (+ 16 t) of the eight keys g
         const uint32_t k_lane = (uint32_t)(g * ps + 8 * (m >> 2) + (m & 3)) * 16, v_lane = (uint32_t)(g * dim + m) * 16;
+        // rows of one tile are alone with their keys, which are read past the caches
         auto load = [](const uint16_t* base, uint32_t offset) {
-            return *reinterpret_cast<const v4u*>(reinterpret_cast<const uint8_t*>(base) + offset);
+            const v4u* at = reinterpret_cast<const v4u*>(reinterpret_cast<const uint8_t*>(base) + offset);
+            if constexpr (NT == 1) return __builtin_nontemporal_load(at);
+            else return *at;
         };
         auto page_of = [&](int half, int it) { return __builtin_amdgcn_readfirstlane(lds.ids[half][wave + kWaves * it]); };
         v4u kf[2][DP / 32], vf[DP / 16];
@@ -488,6 +430,9 @@ struct Shared {
             }
         };
 
+        float gain[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) gain[n] = lds.cols.gain[16 * n + m];
         issue_k(0);
         issue_v(0);
         // one unit; MORE: the next one's keys are asked for as soon as the scores are formed, its values after the product
@@ -514,7 +459,7 @@ struct Shared {
             }
             if constexpr (MORE) issue_k(it + 1);
             const bool in_row = (ok0 & ok1 & (key >= keys.begin) & (key + kUnit <= keys.end)) != 0;
-            const bool whole = in_row & (key + kUnit <= lds.cols.least_len) & ((key >= lds.cols.most_low) | (key + kUnit <= a.n_sink));
+            const bool whole = in_row & (key + kUnit <= least_len) & ((key >= most_low) | (key + kUnit <= a.n_sink));
             if (!in_row) {
                 // keys of no row, or of no page, do not enter the second product: 0 times an infinity would be no 0
                 const bool there = g < 2 ? ok0 : ok1;
@@ -531,10 +476,9 @@ struct Shared {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 // scores of the keys key + 8 g + e, e = 4 t + i
-                const float gain = lds.cols.gain[16 * n + m];
                 float x[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = s[n][e >> 2][e & 3] * gain;
+                for (int e = 0; e < 8; ++e) x[e] = s[n][e >> 2][e & 3] * gain[n];
                 if (!whole) {
                     const bool there = g < 2 ? ok0 : ok1;
                     const int end = min(keys.end, lds.cols.len[16 * n + m]), low = lds.cols.low[16 * n + m];
@@ -584,19 +528,14 @@ struct Shared {
         stage_q<NT>(a, p, lds);
         stage_ids(a.c, p, p.u0, min(p.u1, p.u0 + kIds), lds.ids);
         __syncthreads();
-        if (wave == 0) {
-            int len = lane < 16 * NT ? lds.cols.len[lane] : 1 << 30, low = lane < 16 * NT ? lds.cols.low[lane] : 0;
+        int least_len = lane < 16 * NT ? lds.cols.len[lane] : 1 << 30, most_low = lane < 16 * NT ? lds.cols.low[lane] : 0;
 #pragma unroll
-            for (int i = 1; i < 64; i <<= 1) {
-                len = min(len, __shfl_xor(len, i));
-                low = max(low, __shfl_xor(low, i));
-            }
-            if (lane == 0) {
-                lds.cols.least_len = len;
-                lds.cols.most_low = low;
-            }
+        for (int i = 1; i < 64; i <<= 1) {
+            least_len = min(least_len, __shfl_xor(least_len, i));
+            most_low = max(most_low, __shfl_xor(most_low, i));
         }
-        __syncthreads();
+        least_len = __builtin_amdgcn_readfirstlane(least_len);
+        most_low = __builtin_amdgcn_readfirstlane(most_low);
         Row<DP, NT> r;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -611,7 +550,7 @@ struct Shared {
                 stage_ids(a.c, p, v0, min(p.u1, v0 + kIds), lds.ids);
                 __syncthreads();
             }
-            run<NT>(a, p, v0, min(p.u1, v0 + kIds), lds, r);
+            run<NT>(a, p, v0, min(p.u1, v0 + kIds), least_len, most_low, lds, r);
         }
 
         // the four waves' states become one
@@ -682,7 +621,7 @@ __device__ __noinline__ void redo(uint64_t args, const Index* x) {
         for (int column = wave; column < p.count; column += kWaves) {
             if (p.u0 >= p.u1) break;
             const Column col = column_of(a, p, column);
-            const int len = seq_len(a.c, a.first_seq + col.s);
+            const int len = x->len[col.s];
             const float4 q = load4<T, F32>(a.q, ((int64_t)(a.first_seq + col.s) * a.heads + col.head) * dim + (d < dim ? d : 0));
             float m = kNegInf, l = 0.0f;
             v4f o = {0.0f, 0.0f, 0.0f, 0.0f}, odd = o;
@@ -715,13 +654,20 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_shared_kernel
         if (tid == 0) {
             h->share = share;
             h->start[a.n_seqs] = all;
+            h->first_row = x.first_row;
         }
         for (int s = tid; s < a.n_seqs; s += kThreads) {
             h->start[s] = x.start[s];
-            h->prefix_units[s] = prefix_keys(a, x, s).units;
+            h->prefix_units[s] = is_wide(x.members[s] * a.group) ? keys_of<kWideTile>(0, x.prefix[s], x.low[s], a.n_sink).units : prefix_keys(a, x, s).units;
             h->own_units[s] = own_keys(a, x, s).units;
             h->lead[s] = x.lead[s];
             h->members[s] = x.members[s];
+            h->prefix[s] = x.prefix[s];
+            h->low[s] = x.low[s];
+        }
+        if (a.wide_groups) {
+            sum_line(a.n_seqs, [&](int s) { return wide_cost(a, x, s); }, h->wide_start, lds.wave_cost);
+            if (tid == 0) h->wide_share = line_share(h->wide_start[a.n_seqs], a.wide_groups, kWideStart + 2 * kWideCost);
         }
     }
     int64_t pos = blockIdx.x * share;
@@ -749,35 +695,33 @@ __global__ __launch_bounds__(256) void attn_shared_join_kernel(SharedArgs a) {
     const int dim = a.c.dim, quads = dim >> 2, s = blockIdx.x;
     const int lead = h->lead[s];
     if (lead == kNobody) return;
-    const int64_t share = h->share;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int i = blockIdx.y * 64 + lane;
     const bool in = i < a.heads * quads;
     const int head = in ? i / quads : 0, d = in ? 4 * (i - head * quads) : 0;
     const int kvh = head / a.group, in_group = head - kvh * a.group;
 
-    // the records of the prefix (0) and of the own keys (1): shares w0 .. w1, one record each, in a column of their row
-    int64_t w0[2];
-    int n[2], column[2];
-#pragma unroll
-    for (int own = 0; own < 2; ++own) {
-        const int at = own ? s : lead, members = own ? 1 : h->members[lead], units = own ? h->own_units[s] : h->prefix_units[lead];
-        const int columns = members * a.group, rows = rows_of(a, columns), cost = cost_of(tiles_of(columns < a.columns ? columns : a.columns));
-        const int col = (own ? 0 : (s - lead) * a.group) + in_group, row = kvh * rows + col / a.columns;
-        column[own] = col % a.columns;
-        int64_t first = h->start[at] + row * row_cost_of(units, cost);
-        if (own) first += cost_of_rows(a, h->members[s] * a.group, h->prefix_units[s]);
-        w0[own] = first / share;
-        const int64_t last = units < 2 ? first : first + kStartCost + (int64_t)(units - 1) * cost;
-        n[own] = units == 0 ? 0 : (int)(last / share - w0[own]) + 1;
-    }
+    // the records of the prefix and of the own keys, and their columns
+    const int members = h->members[lead], columns = members * a.group, col = (s - lead) * a.group + in_group;
+    const bool wide = is_wide(columns);
+    const int width = wide ? kWideColumns : a.columns, rows = (columns + width - 1) / width, row = kvh * rows + col / width;
+    const int units = h->prefix_units[lead], cost = wide ? kWideCost : cost_of_columns(a, columns), start = wide ? kWideStart : kStartCost;
+    const Parts of_prefix = parts_of_row((wide ? h->wide_start : h->start)[lead] + row * line_cost(units, cost, start), units, cost, start,
+                                         wide ? h->wide_share : h->share);
+    const int own_units = h->own_units[s], own_cost = cost_of_columns(a, a.group), own_row = kvh * rows_of(a, a.group) + in_group / a.columns;
+    const Parts of_own = parts_of_row(h->start[s] + cost_of_rows(a, h->members[s] * a.group, is_wide(h->members[s] * a.group) ? 0 : h->prefix_units[s]) +
+                                          own_row * line_cost(own_units, own_cost, kStartCost),
+                                      own_units, own_cost, kStartCost, h->share);
     auto record = [&](int j) -> const float* {
-        const int own = j >= n[0];
-        if (own) j -= n[0];
-        if (n[own] == 1) return whole_record(a, own, s, head);
-        return part_record(a, w0[own] + j, j == 0 ? 1 : 0, column[own]);
+        if (j < of_prefix.count) {
+            if (of_prefix.count == 1) return whole_record(a, 0, s, head);
+            return wide ? wide_record(a, of_prefix.first + j, j == 0 ? 1 : 0, col % width) : part_record(a, of_prefix.first + j, j == 0 ? 1 : 0, col % width);
+        }
+        j -= of_prefix.count;
+        if (of_own.count == 1) return whole_record(a, 1, s, head);
+        return part_record(a, of_own.first + j, j == 0 ? 1 : 0, in_group % a.columns);
     };
-    const int total = n[0] + n[1];
+    const int total = of_prefix.count + of_own.count;
     float m = kNegInf, l = 0.0f;
     v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
@@ -817,20 +761,24 @@ __global__ __launch_bounds__(256) void attn_shared_join_kernel(SharedArgs a) {
 
 // Columns of a row, at most: as many tiles as all of a launch's sequences could fill.
 int columns_of(int64_t n_seqs, int group, int dim) {
-    const int64_t all = (n_seqs < kMaxSeqs ? n_seqs : kMaxSeqs) * group;
+    const int64_t all = (n_seqs < kSharedSeqs ? n_seqs : kSharedSeqs) * (int64_t)group;
     const int most = 16 * most_tiles(dim);
     return all <= 16 ? 16 : all <= 32 ? 32 : most;
 }
-constexpr int kMaxGroups = 512;      // work groups of a launch
 
 template <int T, int DP, bool F32, bool FULL, bool PAGE16>
 hipError_t launch_page(SharedArgs a, hipStream_t s) {
-    const int places = (DP > 128 ? 1 : 2) * device_cus(), groups = places < kMaxGroups ? places : kMaxGroups;
+    const int places = (DP > 128 ? 1 : 2) * device_cus(), groups = places < kSharedGroups ? places : kSharedGroups;
     const int total = a.c.n_seqs;
-    for (int at = 0; at < total; at += kMaxSeqs) {
+    for (int at = 0; at < total; at += kSharedSeqs) {
         a.first_seq = at;
-        a.n_seqs = total - at < kMaxSeqs ? total - at : kMaxSeqs;
+        a.n_seqs = total - at < kSharedSeqs ? total - at : kSharedSeqs;
+        a.wide_groups = a.n_seqs * a.group > kNarrowColumns ? attn_shared_wide_groups(a.c.dim, F32) : 0;
         hipLaunchKernelGGL((attn_shared_kernel<T, DP, F32, FULL, PAGE16>), dim3((unsigned)groups), dim3(kThreads), 0, s, a);
+        if (a.wide_groups) {
+            const hipError_t e = launch_attn_shared_wide(a, T, F32, s);
+            if (e != hipSuccess) return e;
+        }
         hipLaunchKernelGGL((attn_shared_join_kernel<T, F32>), dim3((unsigned)a.n_seqs, (unsigned)((a.heads * (a.c.dim / 4) + 63) / 64)),
                            dim3(256), 0, s, a);
     }
@@ -852,7 +800,9 @@ hipError_t launch_dim(const SharedArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t attn_shared_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim) {
-    const int64_t n = n_seqs < kMaxSeqs ? n_seqs : kMaxSeqs, records = 2 * n * heads + 2 * kMaxGroups * (int64_t)columns_of(n, heads / kv_heads, dim);
+    const int64_t n = n_seqs < kSharedSeqs ? n_seqs : kSharedSeqs, group = heads / kv_heads;
+    const int64_t columns = columns_of(n, (int)group, dim) + (n * group > kNarrowColumns ? kWideColumns : 0);
+    const int64_t records = 2 * n * heads + 2 * kSharedGroups * columns;
     return (size_t)kHeaderBytes + (size_t)records * record_floats(dim) * 4;
 }
 

@@ -83,7 +83,12 @@ class Groups:
                 assert not out[s].any(), "an empty sequence gives zeros"
                 continue
             seen = M.visible(torch.tensor([n - 1]), n, window, sinks) & self.there(s)[None]
-            want, tol = M.attention(q[s].view(1, H, b.dim), b.k[s], b.v[s], seen, scale, M.io_eps(io), 2.0 ** -15 if io != "f32" else 0.0)
+            # weights of the cache's type keep 2^-15; over the prefix of many columns each is rounded to it once (by half a step h at
+            # most) and summed as rounded: h of the weighted sum, and h of the sum that divides it
+            members = max((m for m, _ in self.groups), default=0)
+            half = {"f32": 0.0, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}[io]
+            weights = 2 * half if members * (H // b.heads) > 64 else 2.0 ** -15 if io != "f32" else 0.0
+            want, tol = M.attention(q[s].view(1, H, b.dim), b.k[s], b.v[s], seen, scale, M.io_eps(io), weights)
             M.check(out[s][None], want, tol, f"sequence {s} of {n}")
 
     def run_and_check(self, H, io, seed, window=0, sinks=0, scale=None, rows=None):
