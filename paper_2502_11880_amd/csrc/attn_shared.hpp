@@ -8,10 +8,30 @@ namespace bitnet {
 constexpr int kSharedSeqs = 1024;    // sequences of a launch (more go in several)
 constexpr int kSharedGroups = 512;   // work groups of a launch
 constexpr uint16_t kNobody = 0xFFFF;
-// A prefix is gone through in registers for up to this many columns (query heads of a kv head, of all sequences of the group), and
-// in shared memory, kWideColumns at a time, for more.
-constexpr int kNarrowColumns = 64;
+// A prefix is gone through in registers, up to 64 columns (query heads of a kv head, of all sequences of the group) a pass, or
+// in shared memory, kWideColumns a pass, in a launch of its own.
+constexpr int kNarrowColumns = 64;   // up to so many: always the former
 constexpr int kWideColumns = 128;
+// What decides past that: picoseconds a key and kv head of a pass of either, and the microseconds that the second launch costs by
+// itself.  Measured on 8 kv heads of 4 query heads (us, in registers / in shared memory):
+//   heads of 128, bf16 throughout: 128 columns behind 1024 keys 30 / 41, 6016 41 / 46, 32768 103 / 67; 256 columns 36 / 45,
+//   47 / 53, 177 / 89; q from 32 bits over bf16, 128 columns 33 / 51, 44 / 57, 108 / 98, 256 columns 39 / 55, 51 / 69, 191 / 160; over
+//   f16, 256 columns 37 / 52, 49 / 63, 186 / 138;
+//   heads of 64, bf16, 256 columns 36 / 36, 47 / 42, 109 / 67, from 32 bits 38 / 42, 48 / 49, 115 / 92;
+//   heads of 256, bf16, 256 columns behind 1024 keys 62 / 71, 6016 112 / 88, from 32 bits 68 / 102, 122 / 135.
+struct WideRule {
+    int narrow, wide, start;
+};
+constexpr WideRule wide_rule(int dim, bool f32, bool three_parts) {
+    if (dim <= 64) return f32 ? WideRule{76, 100, 4} : WideRule{72, 61, 2};
+    if (dim <= 128) return three_parts ? WideRule{75, 205, 18} : f32 ? WideRule{73, 168, 15} : WideRule{69, 88, 12};
+    return f32 ? WideRule{167, 412, 37} : WideRule{157, 211, 16};
+}
+__host__ __device__ __forceinline__ bool worth_wide(const WideRule& r, int64_t columns, int narrow_columns, int64_t keys, int kv_heads) {
+    if (columns <= kNarrowColumns) return false;
+    const int64_t narrow = (columns + narrow_columns - 1) / narrow_columns * r.narrow, wide = (columns + kWideColumns - 1) / kWideColumns * r.wide;
+    return keys * kv_heads * (narrow - wide) > (int64_t)r.start * 1000000;
+}
 constexpr int kWideTile = 64;        // keys
 constexpr int kWideCost = 2, kWideStart = 6;   // of a tile, and of a row's start
 
@@ -26,7 +46,8 @@ struct SharedArgs {
     int window, n_sink;
     int first_seq, n_seqs;           // of this launch
     int columns;                     // of a row, at most (W)
-    int wide_groups;                 // work groups of the launch for wide prefixes; 0: the sequences are too few for one
+    int wide_groups;                 // work groups of the launch for wide prefixes; 0: none could be worth it
+    WideRule rule;
     uint8_t* ws;
 };
 
@@ -47,6 +68,7 @@ struct Header {
     int64_t start[kSharedSeqs + 1], wide_start[kSharedSeqs + 1];
     int prefix_units[kSharedSeqs], own_units[kSharedSeqs], prefix[kSharedSeqs], low[kSharedSeqs];
     uint16_t lead[kSharedSeqs], members[kSharedSeqs];
+    uint8_t wide[kSharedSeqs];       // whether the group's prefix has its rows in the other line
     int first_row;
 };
 constexpr int64_t kHeaderBytes = (sizeof(Header) + 255) / 256 * 256;
@@ -90,7 +112,6 @@ __device__ __forceinline__ Keys keys_of(int begin, int end, int low, int n_sink)
 }
 
 __device__ __forceinline__ int behind(const SharedArgs& a, int len) { return a.window > 0 && len > a.window ? len - a.window : 0; }
-__device__ __forceinline__ bool is_wide(int columns) { return columns > kNarrowColumns; }
 
 // The line: a row of n units costs start + n cost, and nothing where it has none.
 __device__ __forceinline__ int64_t line_cost(int units, int cost, int start) { return units == 0 ? 0 : start + (int64_t)units * cost; }

@@ -45,10 +45,16 @@ __device__ __forceinline__ Keys own_keys(const SharedArgs& a, const Index& x, in
     const int len = x.len[s], prefix = x.prefix[x.lead[s]];
     return keys_of<kUnit>(prefix < len ? prefix : len, len, behind(a, len), a.n_sink);
 }
-__device__ __forceinline__ Keys prefix_keys(const SharedArgs& a, const Index& x, int s) {
-    const int members = x.members[s];
-    if (members == 0 || is_wide(members * a.group)) return {0, 0, 0, 0, 0, 0};
+__device__ __forceinline__ Keys all_prefix_keys(const SharedArgs& a, const Index& x, int s) {
+    if (x.members[s] == 0) return {0, 0, 0, 0, 0, 0};
     return keys_of<kUnit>(0, x.prefix[s], x.low[s], a.n_sink);
+}
+__device__ __forceinline__ bool is_wide(const SharedArgs& a, const Index& x, int s) {
+    return a.wide_groups && worth_wide(a.rule, x.members[s] * a.group, a.columns, (int64_t)all_prefix_keys(a, x, s).units * kUnit, a.c.kv_heads);
+}
+__device__ __forceinline__ Keys prefix_keys(const SharedArgs& a, const Index& x, int s) {
+    const Keys k = all_prefix_keys(a, x, s);
+    return is_wide(a, x, s) ? Keys{0, 0, 0, 0, 0, 0} : k;
 }
 __device__ __forceinline__ int cost_of_columns(const SharedArgs& a, int columns) {
     return cost_of(tiles_of(columns < a.columns ? columns : a.columns));
@@ -59,7 +65,7 @@ __device__ __forceinline__ int64_t cost_of_rows(const SharedArgs& a, int columns
 // Of a group's wide prefix: its units, and the cost of its rows.
 __device__ __forceinline__ int64_t wide_cost(const SharedArgs& a, const Index& x, int s) {
     const int columns = x.members[s] * a.group;
-    if (!is_wide(columns)) return 0;
+    if (!is_wide(a, x, s)) return 0;
     const int units = keys_of<kWideTile>(0, x.prefix[s], x.low[s], a.n_sink).units;
     return line_cost(units, kWideCost, kWideStart) * ((columns + kWideColumns - 1) / kWideColumns) * a.c.kv_heads;
 }
@@ -352,13 +358,30 @@ struct Shared {
         }
     }
 
-    // The pages of units u0 .. u1 - 1 (at most kIds), and, pages of 16, those of their upper halves.
-    static __device__ __forceinline__ void stage_ids(const KvCache& c, const Place& p, int u0, int u1, int (&ids)[2][kIds]) {
+    // The pages of units u0 .. u1 - 1 (at most kIds), and, pages of 16, those of their upper halves: asked for, and put to LDS.
+    struct Ids {
+        int lower[kIds / kThreads], upper[kIds / kThreads];
+    };
+    static __device__ __forceinline__ Ids ask_ids(const KvCache& c, const Place& p, int u0, int u1) {
         const int32_t* table = c.table + (int64_t)p.table_row * c.max_pages;
-        for (int i = threadIdx.x; i < u1 - u0; i += kThreads) {
+        Ids ids;
+#pragma unroll
+        for (int k = 0; k < kIds / kThreads; ++k) {
+            const int i = threadIdx.x + k * kThreads;
+            if (i >= u1 - u0) continue;
             const int at = unit_key(p.keys, u0 + i) >> c.shift;
-            ids[0][i] = table[at];
-            if (PAGE16) ids[1][i] = at + 1 < c.max_pages ? table[at + 1] : -1;
+            ids.lower[k] = table[at];
+            if (PAGE16) ids.upper[k] = at + 1 < c.max_pages ? table[at + 1] : -1;
+        }
+        return ids;
+    }
+    static __device__ __forceinline__ void put_ids(const Ids& ids, int u0, int u1, int (&to)[2][kIds]) {
+#pragma unroll
+        for (int k = 0; k < kIds / kThreads; ++k) {
+            const int i = threadIdx.x + k * kThreads;
+            if (i >= u1 - u0) continue;
+            to[0][i] = ids.lower[k];
+            if (PAGE16) to[1][i] = ids.upper[k];
         }
     }
 
@@ -525,8 +548,9 @@ struct Shared {
         const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, g = lane >> 4;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int dim = a.c.dim;
+        const Ids ids = ask_ids(a.c, p, p.u0, min(p.u1, p.u0 + kIds));   // on their way beside q
         stage_q<NT>(a, p, lds);
-        stage_ids(a.c, p, p.u0, min(p.u1, p.u0 + kIds), lds.ids);
+        put_ids(ids, p.u0, min(p.u1, p.u0 + kIds), lds.ids);
         __syncthreads();
         int least_len = lane < 16 * NT ? lds.cols.len[lane] : 1 << 30, most_low = lane < 16 * NT ? lds.cols.low[lane] : 0;
 #pragma unroll
@@ -547,7 +571,7 @@ struct Shared {
         for (int v0 = p.u0; v0 < p.u1; v0 += kIds) {
             if (v0 > p.u0) {
                 __syncthreads();
-                stage_ids(a.c, p, v0, min(p.u1, v0 + kIds), lds.ids);
+                put_ids(ask_ids(a.c, p, v0, min(p.u1, v0 + kIds)), v0, min(p.u1, v0 + kIds), lds.ids);
                 __syncthreads();
             }
             run<NT>(a, p, v0, min(p.u1, v0 + kIds), least_len, most_low, lds, r);
@@ -658,7 +682,9 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_shared_kernel
         }
         for (int s = tid; s < a.n_seqs; s += kThreads) {
             h->start[s] = x.start[s];
-            h->prefix_units[s] = is_wide(x.members[s] * a.group) ? keys_of<kWideTile>(0, x.prefix[s], x.low[s], a.n_sink).units : prefix_keys(a, x, s).units;
+            const bool wide = is_wide(a, x, s);
+            h->wide[s] = wide;
+            h->prefix_units[s] = wide ? keys_of<kWideTile>(0, x.prefix[s], x.low[s], a.n_sink).units : prefix_keys(a, x, s).units;
             h->own_units[s] = own_keys(a, x, s).units;
             h->lead[s] = x.lead[s];
             h->members[s] = x.members[s];
@@ -703,13 +729,13 @@ __global__ __launch_bounds__(256) void attn_shared_join_kernel(SharedArgs a) {
 
     // the records of the prefix and of the own keys, and their columns
     const int members = h->members[lead], columns = members * a.group, col = (s - lead) * a.group + in_group;
-    const bool wide = is_wide(columns);
+    const bool wide = h->wide[lead];
     const int width = wide ? kWideColumns : a.columns, rows = (columns + width - 1) / width, row = kvh * rows + col / width;
     const int units = h->prefix_units[lead], cost = wide ? kWideCost : cost_of_columns(a, columns), start = wide ? kWideStart : kStartCost;
     const Parts of_prefix = parts_of_row((wide ? h->wide_start : h->start)[lead] + row * line_cost(units, cost, start), units, cost, start,
                                          wide ? h->wide_share : h->share);
     const int own_units = h->own_units[s], own_cost = cost_of_columns(a, a.group), own_row = kvh * rows_of(a, a.group) + in_group / a.columns;
-    const Parts of_own = parts_of_row(h->start[s] + cost_of_rows(a, h->members[s] * a.group, is_wide(h->members[s] * a.group) ? 0 : h->prefix_units[s]) +
+    const Parts of_own = parts_of_row(h->start[s] + cost_of_rows(a, h->members[s] * a.group, h->wide[s] ? 0 : h->prefix_units[s]) +
                                           own_row * line_cost(own_units, own_cost, kStartCost),
                                       own_units, own_cost, kStartCost, h->share);
     auto record = [&](int j) -> const float* {
@@ -770,10 +796,13 @@ template <int T, int DP, bool F32, bool FULL, bool PAGE16>
 hipError_t launch_page(SharedArgs a, hipStream_t s) {
     const int places = (DP > 128 ? 1 : 2) * device_cus(), groups = places < kSharedGroups ? places : kSharedGroups;
     const int total = a.c.n_seqs;
+    a.rule = wide_rule(DP, F32, F32 && T == kBf16);
     for (int at = 0; at < total; at += kSharedSeqs) {
         a.first_seq = at;
         a.n_seqs = total - at < kSharedSeqs ? total - at : kSharedSeqs;
-        a.wide_groups = a.n_seqs * a.group > kNarrowColumns ? attn_shared_wide_groups(a.c.dim, F32) : 0;
+        // the most that the launch's sequences could share
+        const bool wide = worth_wide(a.rule, (int64_t)a.n_seqs * a.group, a.columns, (int64_t)a.c.max_pages << a.c.shift, a.c.kv_heads);
+        a.wide_groups = wide ? attn_shared_wide_groups(a.c.dim, F32) : 0;
         hipLaunchKernelGGL((attn_shared_kernel<T, DP, F32, FULL, PAGE16>), dim3((unsigned)groups), dim3(kThreads), 0, s, a);
         if (a.wide_groups) {
             const hipError_t e = launch_attn_shared_wide(a, T, F32, s);
