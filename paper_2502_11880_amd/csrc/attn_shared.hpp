@@ -9,9 +9,10 @@ constexpr int kSharedSeqs = 1024;    // sequences of a launch (more go in severa
 constexpr int kSharedGroups = 512;   // work groups of a launch
 constexpr uint16_t kNobody = 0xFFFF;
 // A prefix is gone through in registers, up to 64 columns (query heads of a kv head, of all sequences of the group) a pass, or
-// in shared memory, kWideColumns a pass, in a launch of its own.
+// in shared memory, 128 or 256 a pass, in a launch of its own.
 constexpr int kNarrowColumns = 64;   // up to so many: always the former
-constexpr int kWideColumns = 128;
+// Columns of a wide pass: four waves' or eight waves' (q in one part leaves registers for two waves a SIMD).
+constexpr int wide_columns(int dim, bool f32) { return !f32 && dim > 64 && dim <= 128 ? 256 : 128; }
 // What decides past that: picoseconds a key and kv head of a pass of either, and the microseconds that the second launch costs by
 // itself.  Measured on 8 kv heads of 4 query heads (us, in registers / in shared memory):
 //   heads of 128, bf16 throughout: 128 columns behind 1024 keys 30 / 41, 6016 41 / 46, 32768 103 / 67; 256 columns 36 / 45,
@@ -27,9 +28,10 @@ constexpr WideRule wide_rule(int dim, bool f32, bool three_parts) {
     if (dim <= 128) return three_parts ? WideRule{75, 205, 18} : f32 ? WideRule{73, 168, 15} : WideRule{69, 88, 12};
     return f32 ? WideRule{167, 412, 37} : WideRule{157, 211, 16};
 }
-__host__ __device__ __forceinline__ bool worth_wide(const WideRule& r, int64_t columns, int narrow_columns, int64_t keys, int kv_heads) {
+__host__ __device__ __forceinline__ bool worth_wide(const WideRule& r, int64_t columns, int narrow_columns, int wide_columns, int64_t keys,
+                                                    int kv_heads) {
     if (columns <= kNarrowColumns) return false;
-    const int64_t narrow = (columns + narrow_columns - 1) / narrow_columns * r.narrow, wide = (columns + kWideColumns - 1) / kWideColumns * r.wide;
+    const int64_t narrow = (columns + narrow_columns - 1) / narrow_columns * r.narrow, wide = (columns + wide_columns - 1) / wide_columns * r.wide;
     return keys * kv_heads * (narrow - wide) > (int64_t)r.start * 1000000;
 }
 constexpr int kWideTile = 64;        // keys
@@ -47,6 +49,7 @@ struct SharedArgs {
     int first_seq, n_seqs;           // of this launch
     int columns;                     // of a row, at most (W)
     int wide_groups;                 // work groups of the launch for wide prefixes; 0: none could be worth it
+    int wide_columns;
     WideRule rule;
     uint8_t* ws;
 };
@@ -87,7 +90,7 @@ __device__ __forceinline__ float* part_record(const SharedArgs& a, int64_t share
 
 __device__ __forceinline__ float* wide_record(const SharedArgs& a, int64_t share, int slot, int column) {
     return reinterpret_cast<float*>(a.ws + kHeaderBytes) +
-           ((int64_t)2 * a.n_seqs * a.heads + (int64_t)2 * kSharedGroups * a.columns + (2 * share + slot) * kWideColumns + column) *
+           ((int64_t)2 * a.n_seqs * a.heads + (int64_t)2 * kSharedGroups * a.columns + (2 * share + slot) * a.wide_columns + column) *
                record_floats(a.c.dim);
 }
 
@@ -128,13 +131,13 @@ __device__ __forceinline__ int64_t line_share(int64_t all, int groups, int64_t l
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
     return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
-// Where a row's parts lie: shares first .. first + count - 1.
+// Where a row's parts lie: shares first .. first + count - 1 (a row of up to `whole` units is one part).
 struct Parts {
     int64_t first;
     int count;
 };
-__device__ __forceinline__ Parts parts_of_row(int64_t at, int units, int cost, int start, int64_t share) {
-    if (units == 0) return {0, 0};
+__device__ __forceinline__ Parts parts_of_row(int64_t at, int units, int whole, int cost, int start, int64_t share) {
+    if (units <= whole) return {0, units > 0 ? 1 : 0};
     const int64_t first = divide(at, share), last = divide(units < 2 ? at : at + start + (int64_t)(units - 1) * cost, share);
     return {first, (int)(last - first) + 1};
 }

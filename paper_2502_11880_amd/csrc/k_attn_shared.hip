@@ -32,6 +32,11 @@ __host__ __device__ constexpr int most_tiles(int dim) { return dim <= 64 ? 4 : 2
 // and in the end the waves' states become one).
 __host__ __device__ constexpr int cost_of(int tiles) { return tiles == 1 ? 4 : tiles == 2 ? 5 : 7; }
 constexpr int kMostCost = 7, kStartCost = 20;
+// Rows of up to so many units are never split: the share that a row starts in takes it whole.
+#ifndef WH
+#define WH 12
+#endif
+constexpr int kWholeUnits = WH;
 constexpr int64_t kLeastShare = kStartCost + 2 * kMostCost;
 __host__ __device__ __forceinline__ int tiles_of(int columns) { return columns <= 16 ? 1 : columns <= 32 ? 2 : 4; }
 
@@ -50,7 +55,7 @@ __device__ __forceinline__ Keys all_prefix_keys(const SharedArgs& a, const Index
     return keys_of<kUnit>(0, x.prefix[s], x.low[s], a.n_sink);
 }
 __device__ __forceinline__ bool is_wide(const SharedArgs& a, const Index& x, int s) {
-    return a.wide_groups && worth_wide(a.rule, x.members[s] * a.group, a.columns, (int64_t)all_prefix_keys(a, x, s).units * kUnit, a.c.kv_heads);
+    return a.wide_groups && worth_wide(a.rule, x.members[s] * a.group, a.columns, a.wide_columns, (int64_t)all_prefix_keys(a, x, s).units * kUnit, a.c.kv_heads);
 }
 __device__ __forceinline__ Keys prefix_keys(const SharedArgs& a, const Index& x, int s) {
     const Keys k = all_prefix_keys(a, x, s);
@@ -67,7 +72,7 @@ __device__ __forceinline__ int64_t wide_cost(const SharedArgs& a, const Index& x
     const int columns = x.members[s] * a.group;
     if (!is_wide(a, x, s)) return 0;
     const int units = keys_of<kWideTile>(0, x.prefix[s], x.low[s], a.n_sink).units;
-    return line_cost(units, kWideCost, kWideStart) * ((columns + kWideColumns - 1) / kWideColumns) * a.c.kv_heads;
+    return line_cost(units, kWideCost, kWideStart) * ((columns + a.wide_columns - 1) / a.wide_columns) * a.c.kv_heads;
 }
 
 // start[s]: the sum of cost(i) over i < s, for s up to n.
@@ -190,6 +195,10 @@ __device__ __forceinline__ Place place_of(const SharedArgs& a, const Index& x, i
     p.u0 = (int)line_unit(pos - at, cost, kStartCost);
     const int64_t room = line_unit(end - at, cost, kStartCost);
     p.u1 = room < p.keys.units ? (int)room : p.keys.units;
+    if (p.keys.units <= kWholeUnits) {                    // whole, or of the share before
+        p.u0 = pos > at ? p.keys.units : 0;
+        p.u1 = p.keys.units;
+    }
     p.next = at + row_cost;
     p.table_row = p.own == 0 && lo == 0 ? x.first_row : a.first_seq + lo;
     return p;
@@ -730,14 +739,14 @@ __global__ __launch_bounds__(256) void attn_shared_join_kernel(SharedArgs a) {
     // the records of the prefix and of the own keys, and their columns
     const int members = h->members[lead], columns = members * a.group, col = (s - lead) * a.group + in_group;
     const bool wide = h->wide[lead];
-    const int width = wide ? kWideColumns : a.columns, rows = (columns + width - 1) / width, row = kvh * rows + col / width;
+    const int width = wide ? a.wide_columns : a.columns, rows = (columns + width - 1) / width, row = kvh * rows + col / width;
     const int units = h->prefix_units[lead], cost = wide ? kWideCost : cost_of_columns(a, columns), start = wide ? kWideStart : kStartCost;
-    const Parts of_prefix = parts_of_row((wide ? h->wide_start : h->start)[lead] + row * line_cost(units, cost, start), units, cost, start,
+    const Parts of_prefix = parts_of_row((wide ? h->wide_start : h->start)[lead] + row * line_cost(units, cost, start), units, wide ? 0 : kWholeUnits, cost, start,
                                          wide ? h->wide_share : h->share);
     const int own_units = h->own_units[s], own_cost = cost_of_columns(a, a.group), own_row = kvh * rows_of(a, a.group) + in_group / a.columns;
     const Parts of_own = parts_of_row(h->start[s] + cost_of_rows(a, h->members[s] * a.group, h->wide[s] ? 0 : h->prefix_units[s]) +
                                           own_row * line_cost(own_units, own_cost, kStartCost),
-                                      own_units, own_cost, kStartCost, h->share);
+                                      own_units, kWholeUnits, own_cost, kStartCost, h->share);
     auto record = [&](int j) -> const float* {
         if (j < of_prefix.count) {
             if (of_prefix.count == 1) return whole_record(a, 0, s, head);
@@ -797,11 +806,12 @@ hipError_t launch_page(SharedArgs a, hipStream_t s) {
     const int places = (DP > 128 ? 1 : 2) * device_cus(), groups = places < kSharedGroups ? places : kSharedGroups;
     const int total = a.c.n_seqs;
     a.rule = wide_rule(DP, F32, F32 && T == kBf16);
+    a.wide_columns = wide_columns(DP, F32);
     for (int at = 0; at < total; at += kSharedSeqs) {
         a.first_seq = at;
         a.n_seqs = total - at < kSharedSeqs ? total - at : kSharedSeqs;
         // the most that the launch's sequences could share
-        const bool wide = worth_wide(a.rule, (int64_t)a.n_seqs * a.group, a.columns, (int64_t)a.c.max_pages << a.c.shift, a.c.kv_heads);
+        const bool wide = worth_wide(a.rule, (int64_t)a.n_seqs * a.group, a.columns, a.wide_columns, (int64_t)a.c.max_pages << a.c.shift, a.c.kv_heads);
         a.wide_groups = wide ? attn_shared_wide_groups(a.c.dim, F32) : 0;
         hipLaunchKernelGGL((attn_shared_kernel<T, DP, F32, FULL, PAGE16>), dim3((unsigned)groups), dim3(kThreads), 0, s, a);
         if (a.wide_groups) {
@@ -830,7 +840,8 @@ hipError_t launch_dim(const SharedArgs& a, hipStream_t s) {
 
 size_t attn_shared_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim) {
     const int64_t n = n_seqs < kSharedSeqs ? n_seqs : kSharedSeqs, group = heads / kv_heads;
-    const int64_t columns = columns_of(n, (int)group, dim) + (n * group > kNarrowColumns ? kWideColumns : 0);
+    // (work groups times columns of the launch for wide prefixes: as many with 128 columns as with 256)
+    const int64_t columns = columns_of(n, (int)group, dim) + (n * group > kNarrowColumns ? 128 : 0);
     const int64_t records = 2 * n * heads + 2 * kSharedGroups * columns;
     return (size_t)kHeaderBytes + (size_t)records * record_floats(dim) * 4;
 }

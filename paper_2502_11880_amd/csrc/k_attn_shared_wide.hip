@@ -10,9 +10,7 @@
 namespace bitnet {
 namespace {
 
-constexpr int kWaves = 4;
-
-// Waves of a SIMD, and so work groups of a CU: q in parts leaves registers for one.
+// Waves of a SIMD: q in parts leaves registers for one.
 constexpr int per_simd(int dim, bool f32) { return dim <= 64 || (dim <= 128 && !f32) ? 2 : 1; }
 
 // The last of n sequences that starts at x or before: 64 lanes probe at once.
@@ -30,9 +28,10 @@ __device__ __forceinline__ int find_start(const int64_t* start, int n, int64_t x
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-template <int T, int DP, bool F32, int PER_SIMD, bool FULL>
-__global__ __launch_bounds__(64 * kWaves, PER_SIMD) void attn_shared_wide_kernel(SharedArgs a) {
-    using P = Prefill<T, DP, F32, kWaves, FULL, kPrefix>;
+template <int T, int DP, bool F32, int PER_SIMD, int WAVES, bool FULL>
+__global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attn_shared_wide_kernel(SharedArgs a) {
+    using P = Prefill<T, DP, F32, WAVES, FULL, kPrefix>;
+    constexpr int kColumns = 32 * WAVES;
     __shared__ typename P::Lds lds;
     const Header* h = reinterpret_cast<const Header*>(a.ws);
     const int64_t all = h->wide_start[a.n_seqs], share = h->wide_share;
@@ -48,7 +47,7 @@ __global__ __launch_bounds__(64 * kWaves, PER_SIMD) void attn_shared_wide_kernel
     args.n_sink = a.n_sink;
     while (pos < end) {
         const int s = find_start(h->wide_start, a.n_seqs, pos);
-        const int columns = h->members[s] * a.group, rows = (columns + kWideColumns - 1) / kWideColumns;
+        const int columns = h->members[s] * a.group, rows = (columns + kColumns - 1) / kColumns;
         const Keys keys = keys_of<kWideTile>(0, h->prefix[s], h->low[s], a.n_sink);
         const int64_t row_cost = line_cost(keys.units, kWideCost, kWideStart);
         const int row = (int)divide(pos - h->wide_start[s], row_cost);
@@ -58,7 +57,7 @@ __global__ __launch_bounds__(64 * kWaves, PER_SIMD) void attn_shared_wide_kernel
         const int u1 = room < keys.units ? (int)room : keys.units;
         pos = at + row_cost;
         if (u0 >= u1) continue;
-        const int kvh = row / rows, col0 = (row - kvh * rows) * kWideColumns;
+        const int kvh = row / rows, col0 = (row - kvh * rows) * kColumns;
         // this lane's column; past the last one, that one once more
         const int col = col0 + (int)(threadIdx.x >> 6) * 32 + (int)(threadIdx.x & 31);
         const bool used = col < columns;
@@ -73,26 +72,28 @@ __global__ __launch_bounds__(64 * kWaves, PER_SIMD) void attn_shared_wide_kernel
     }
 }
 
-template <int T, int DP, bool F32, int PER_SIMD>
+template <int T, int DP, bool F32>
 hipError_t launch(const SharedArgs& a, hipStream_t s) {
+    constexpr int kWaves = wide_columns(DP, F32) / 32, kPerSimd = per_simd(DP, F32);
     const dim3 grid((unsigned)a.wide_groups), block(64 * kWaves);
-    if (a.c.dim == DP) hipLaunchKernelGGL((attn_shared_wide_kernel<T, DP, F32, PER_SIMD, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((attn_shared_wide_kernel<T, DP, F32, PER_SIMD, false>), grid, block, 0, s, a);
+    if (a.c.dim == DP) hipLaunchKernelGGL((attn_shared_wide_kernel<T, DP, F32, kPerSimd, kWaves, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((attn_shared_wide_kernel<T, DP, F32, kPerSimd, kWaves, false>), grid, block, 0, s, a);
     return hipGetLastError();
 }
 
 template <int T, bool F32>
 hipError_t launch_dim(const SharedArgs& a, hipStream_t s) {
-    if (a.c.dim <= 64) return launch<T, 64, F32, per_simd(64, F32)>(a, s);
-    if (a.c.dim <= 128) return launch<T, 128, F32, per_simd(128, F32)>(a, s);
-    return launch<T, 256, F32, per_simd(256, F32)>(a, s);
+    if (a.c.dim <= 64) return launch<T, 64, F32>(a, s);
+    if (a.c.dim <= 128) return launch<T, 128, F32>(a, s);
+    return launch<T, 256, F32>(a, s);
 }
 
 }  // namespace
 
+// One round of work groups; with their columns at most kSharedGroups times 128.
 int attn_shared_wide_groups(int dim, bool f32) {
-    const int groups = per_simd(dim, f32) * device_cus();
-    return groups < kSharedGroups ? groups : kSharedGroups;
+    const int waves = wide_columns(dim, f32) / 32, groups = 4 * per_simd(dim, f32) / waves * device_cus(), most = kSharedGroups * 4 / waves;
+    return groups < most ? groups : most;
 }
 
 hipError_t launch_attn_shared_wide(const SharedArgs& a, int dtype, bool f32, hipStream_t s) {
