@@ -116,20 +116,20 @@ __device__ __forceinline__ Keys keys_of(int begin, int end, int low, int n_sink)
 
 __device__ __forceinline__ int behind(const SharedArgs& a, int len) { return a.window > 0 && len > a.window ? len - a.window : 0; }
 
+// a / b of numbers that are not negative: a 64-bit division is a hundred instructions and more.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
 // The line: a row of n units costs start + n cost, and nothing where it has none.
 __device__ __forceinline__ int64_t line_cost(int units, int cost, int start) { return units == 0 ? 0 : start + (int64_t)units * cost; }
 // The first unit of a row that starts `before` or later in it: the first at 0, the others behind the start's cost.
 __device__ __forceinline__ int64_t line_unit(int64_t before, int cost, int start) {
-    return before <= 0 ? 0 : before <= start + cost ? 1 : (before - start + cost - 1) / cost;
+    return before <= 0 ? 0 : before <= start + cost ? 1 : divide(before - start + cost - 1, cost);
 }
 // The share of every work group; none lies within one unit, nor within a start.
 __device__ __forceinline__ int64_t line_share(int64_t all, int groups, int64_t least) {
     const int64_t want = (all + groups - 1) / groups;
     return want < least ? least : want;
-}
-// a / b of numbers that are not negative: a 64-bit division is a hundred instructions and more.
-__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
-    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 // Where a row's parts lie: shares first .. first + count - 1 (a row of up to `whole` units is one part).
 struct Parts {

@@ -31,13 +31,12 @@ __host__ __device__ constexpr int most_tiles(int dim) { return dim <= 64 ? 4 : 2
 // What a unit of a row of one, two and four tiles costs, and what its start does (q, pages and first keys are three reads in a row,
 // and in the end the waves' states become one).
 __host__ __device__ constexpr int cost_of(int tiles) { return tiles == 1 ? 4 : tiles == 2 ? 5 : 7; }
-constexpr int kMostCost = 7, kStartCost = 20;
-// Rows of up to so many units are never split: the share that a row starts in takes it whole.
-#ifndef WH
-#define WH 12
+#ifndef SC
+#define SC 24
 #endif
-constexpr int kWholeUnits = WH;
-constexpr int64_t kLeastShare = kStartCost + 2 * kMostCost;
+constexpr int kStartCost = SC;
+// Rows of up to so many units are never split: the share that a row starts in takes it whole.
+constexpr int kWholeUnits = 12;
 __host__ __device__ __forceinline__ int tiles_of(int columns) { return columns <= 16 ? 1 : columns <= 32 ? 2 : 4; }
 
 __device__ __forceinline__ int unit_key(const Keys& k, int u) {
@@ -153,7 +152,10 @@ __device__ void build_index(const SharedArgs& a, Index& x, int64_t (&wave_cost)[
     __syncthreads();
 }
 
-__device__ __forceinline__ int64_t share_of(int64_t all) { return line_share(all, gridDim.x, kLeastShare); }
+// No share lies within a unit, nor within a start; a short row costs about as much, so that few shares start two of them.
+__device__ __forceinline__ int64_t share_of(const SharedArgs& a, int64_t all) {
+    return line_share(all, gridDim.x, kStartCost + cost_of(tiles_of(a.columns)));
+}
 
 // A row, and the units [u0, u1) of it that the share from pos to end holds.
 struct Place {
@@ -645,7 +647,7 @@ __device__ __noinline__ void redo(uint64_t args, const Index* x) {
     args = (uint64_t)high << 32 | low;
     const SharedArgs a = *(const SharedArgs*)(const __attribute__((address_space(4))) void*)args;
     const int dim = a.c.dim, d = 4 * (threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t all = x->start[a.n_seqs], share = share_of(all);
+    const int64_t all = x->start[a.n_seqs], share = share_of(a, all);
     int64_t pos = blockIdx.x * share;
     const int64_t end = pos + share < all ? pos + share : all;
     while (pos < end) {
@@ -681,7 +683,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_shared_kernel
     if (tid == 0) lds.odd = 0;
     build_index(a, lds.index, lds.wave_cost, lds.wave_lead);
     const Index& x = lds.index;
-    const int64_t all = x.start[a.n_seqs], share = share_of(all);
+    const int64_t all = x.start[a.n_seqs], share = share_of(a, all);
     if (blockIdx.x == 0) {
         Header* h = reinterpret_cast<Header*>(a.ws);
         if (tid == 0) {
