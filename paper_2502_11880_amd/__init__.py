@@ -413,17 +413,30 @@ class _Rotation(ctypes.Structure):         # bitnet_rotation
 
 
 def _rotation(freqs, interleaved, gain):
+    return _Rotation(_ptr(freqs, "freqs", _widths()[3]), 2 * freqs.numel(), 1 if interleaved else 0, gain)
+
+
+@functools.lru_cache(maxsize=None)
+def _current_device():
+    """A call that returns the current device's number (torch.cuda.current_device asks first whether torch is initialised)."""
     import torch
-    return _Rotation(_ptr(freqs, "freqs", torch.float64), 2 * freqs.numel(), 1 if interleaved else 0, gain)
+    torch.cuda.init()
+    return getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _here(*tensors) -> None:
     """A call runs on the current device: its tensors have to be there."""
-    import torch
-    now = torch.cuda.current_device()
+    now = _current_device()()
     for t in tensors:
-        if t is not None and t.get_device() not in (now, -1):        # tensors of the host have been refused, or will be
+        if t is not None and t.get_device() != now:
             raise ValueError(f"tensors must be on the current device {now}, got one on {t.get_device()}")
+
+
+@functools.lru_cache(maxsize=None)
+def _widths():
+    """float32, int8, int32, float64."""
+    import torch
+    return torch.float32, torch.int8, torch.int32, torch.float64
 
 
 def bitnet_norm_quantize(x, gamma, eps: float, xq=None, x_scale=None, x_rowsum=None, residual=None, residual_out=None, y=None,
@@ -432,25 +445,24 @@ def bitnet_norm_quantize(x, gamma, eps: float, xq=None, x_scale=None, x_rowsum=N
     the residual's addition before it (residual_out: the sum, in the residual's type) and the int8 codes of a product's activation behind it (xq, x_scale,
     x_rowsum as bitnet_quantize_act writes them).  y: the normed rows themselves, in any of the three types.  gamma: float32
     [K], or None."""
-    import torch
-    if x.dim() != 2:
-        raise ValueError(f"x must be [M, K], got {tuple(x.shape)}")
-    M, K = x.shape
+    f32, i8, i32, _ = _widths()
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError(f"x must be [M, K], got {tuple(shape)}")
+    M, K = shape
     for t, name in ((residual, "residual"), (residual_out, "residual_out"), (y, "y"), (xq, "xq")):
-        if t is not None and t.shape != x.shape:
-            raise ValueError(f"{name} must have x's shape {tuple(x.shape)}, got {tuple(t.shape)}")
+        if t is not None and t.shape != shape:
+            raise ValueError(f"{name} must have x's shape {tuple(shape)}, got {tuple(t.shape)}")
     for t, name, n in ((gamma, "gamma", K), (x_scale, "x_scale", M), (x_rowsum, "x_rowsum", M)):
         if t is not None and t.numel() != n:
             raise ValueError(f"{name} must have {n} entries, got {t.numel()}")
     if residual_out is not None and residual is not None and residual_out.dtype != residual.dtype:
         raise TypeError(f"residual_out must be {residual.dtype}, got {residual_out.dtype}")
-    pointers = (_ptr(x, "x"), _ptr(residual, "residual"), _ptr(residual_out, "residual_out"), _ptr(gamma, "gamma", torch.float32),
-                _ptr(y, "y"), _ptr(xq, "xq", torch.int8), _ptr(x_scale, "x_scale", torch.float32),
-                _ptr(x_rowsum, "x_rowsum", torch.int32))
+    a, b, c, d, e = _ptr(x, "x"), _ptr(residual, "residual"), _ptr(residual_out, "residual_out"), _ptr(gamma, "gamma", f32), _ptr(y, "y")
+    f, g, h = _ptr(xq, "xq", i8), _ptr(x_scale, "x_scale", f32), _ptr(x_rowsum, "x_rowsum", i32)
     _here(x, residual, residual_out, gamma, y, xq, x_scale, x_rowsum)
-    st = lib().bitnet_norm_quantize(pointers[0], _dtype(x, "x"), pointers[1], pointers[2],
-                                    0 if residual is None else _dtype(residual, "residual"), pointers[3], eps, M, K, pointers[4],
-                                    0 if y is None else _dtype(y, "y"), pointers[5], pointers[6], pointers[7], _stream(stream))
+    st = lib().bitnet_norm_quantize(a, _dtype(x, "x"), b, c, 0 if residual is None else _dtype(residual, "residual"), d, eps, M, K, e,
+                                    0 if y is None else _dtype(y, "y"), f, g, h, _stream(stream))
     _check("bitnet_norm_quantize", st)
 
 
@@ -458,9 +470,8 @@ def bitnet_rope_freqs(freqs, theta: float, scaling="none", factor: float = 1.0, 
                       high: float = 32.0, stream=None) -> None:
     """Turns a position of each pair of a rotation of 2 * freqs.numel() channels, into freqs (float64): theta^(-2i / rot_dim) /
     2 pi, stretched for contexts longer than `original` as `scaling` says (none, linear, base, turns or index)."""
-    import torch
     kind = ROPE_SCALINGS[scaling] if isinstance(scaling, str) else int(scaling)
-    pointer = _ptr(freqs, "freqs", torch.float64)
+    pointer = _ptr(freqs, "freqs", _widths()[3])
     _here(freqs)
     st = lib().bitnet_rope_freqs(kind, theta, 2 * freqs.numel(), factor, original, low, high, pointer, _stream(stream))
     _check("bitnet_rope_freqs", st)

@@ -31,10 +31,7 @@ __host__ __device__ constexpr int most_tiles(int dim) { return dim <= 64 ? 4 : 2
 // What a unit of a row of one, two and four tiles costs, and what its start does (q, pages and first keys are three reads in a row,
 // and in the end the waves' states become one).
 __host__ __device__ constexpr int cost_of(int tiles) { return tiles == 1 ? 4 : tiles == 2 ? 5 : 7; }
-#ifndef SC
-#define SC 24
-#endif
-constexpr int kStartCost = SC;
+constexpr int kStartCost = 24;
 // Rows of up to so many units are never split: the share that a row starts in takes it whole.
 constexpr int kWholeUnits = 12;
 __host__ __device__ __forceinline__ int tiles_of(int columns) { return columns <= 16 ? 1 : columns <= 32 ? 2 : 4; }
