@@ -11,6 +11,10 @@
 // Memory bounds it: a row is read once into registers (up to 16 quads a thread), summed, normed and quantised there, and
 // written once; 13 bytes an element with everything in 32 bits.  Two reductions over the work group stand in between.
 // Rows that are longer, which no linear of a model has, take three passes over memory.
+//
+// Measured (kernel times): 8192 rows of 4096, all in 32 bits, 76.8 us (5.7 TB/s; a large copy reaches 4.9, and here more is read
+// than written) with 256 lanes a row, 512 the same, 128 79, 64 81, 1024 84; 333 rows of 8640, 32 bits onto a residual in bf16, 7.6 us
+// with 512 lanes of five quads, 8.3 of eight, 9.1 with 1024 lanes; one row of 4096 3.3 us, of which an empty launch takes 1.7.
 #include "rows.hpp"
 
 namespace bitnet {
@@ -214,6 +218,8 @@ void launch_quads(const NormArgs& a, int rows, int64_t total_rows, hipStream_t s
         if (quads <= 512) return launch_rows<X, R, QUAD, 128, 4>(a, rows, s);
         if (quads <= 1024) return launch_rows<X, R, QUAD, 256, 4>(a, rows, s);
         if (quads <= 2048) return launch_rows<X, R, QUAD, 512, 4>(a, rows, s);
+        if (quads <= 2560) return launch_rows<X, R, QUAD, 512, 5>(a, rows, s);
+        if (quads <= 4096) return launch_rows<X, R, QUAD, 512, 8>(a, rows, s);
     }
     if (quads <= 4096) return launch_rows<X, R, QUAD, 1024, 4>(a, rows, s);
     if (quads <= 16384) return launch_rows<X, R, QUAD, 1024, 16>(a, rows, s);

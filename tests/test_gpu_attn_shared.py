@@ -137,6 +137,63 @@ def test_many_and_long(groups, tail, H, Hkv, D, page, dtype, io):
     Groups(groups, lens, Hkv, D, page, dtype, seed=3).run_and_check(H, io, seed=3, rows=rows)
 
 
+# Prefixes that go through shared memory: many columns (members times heads of a kv head) behind enough keys.
+WIDE = [(4, 256, 1, 64, 16, "bf16", "bf16", 6000), (6, 200, 1, 48, 64, "f16", "f16", 5003), (9, 256, 1, 64, 32, "bf16", "f32", 8011),
+        (5, 256, 1, 128, 32, "bf16", "bf16", 9001), (7, 150, 1, 100, 16, "f16", "f16", 12000), (16, 256, 1, 128, 64, "bf16", "f32", 9000),
+        (16, 256, 1, 100, 16, "f16", "f32", 6100), (5, 256, 1, 256, 128, "bf16", "bf16", 6007), (12, 256, 1, 132, 32, "f16", "f32", 9000)]
+
+
+@pytest.mark.parametrize("members,H,Hkv,D,page,dtype,io,prefix", WIDE)
+def test_wide_prefixes(members, H, Hkv, D, page, dtype, io, prefix):
+    """Beside a group of one sequence and a small one; a member as long as the prefix, one that is shorter, one longer."""
+    _announce("shared wide", members, H, D, page, dtype, io, prefix)
+    tails = [37, 0, -100, 300] + [5] * (members - 4)
+    lens = [40] + [prefix + t for t in tails] + [70, 90, 64]
+    Groups([(1, 0), (members, prefix), (3, 64)], lens, Hkv, D, page, dtype, seed=14).run_and_check(H, io, seed=14, rows=[0, 1, 2, 3, 4, members, members + 3])
+
+
+@pytest.mark.parametrize("window,sinks", [(4000, 0), (5950, 100), (64, 64 * 90), (10 ** 6, 4)])
+def test_wide_prefixes_behind_windows(window, sinks):
+    _announce("shared wide window", window, sinks)
+    lens = [6000 + t for t in (0, 1, 63, 64, 700, 2000, 30, 5)]
+    g = Groups([(8, 6000)], lens, 1, 64, 32, "bf16", seed=15)
+    g.run_and_check(256, "bf16", seed=15, window=window, sinks=sinks, rows=[0, 1, 4, 5])
+    g.b.table[0, 20] = -1                    # a page that is gone, and one that was never of the pool
+    g.b.table[0, 180] = 10 ** 7
+    g.run_and_check(256, "bf16", seed=15, window=window, sinks=sinks, rows=[0, 3, 5])
+
+
+@pytest.mark.parametrize("dtype,io", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f32")])
+def test_wide_prefixes_with_values_that_are_not_finite(dtype, io):
+    _announce("shared wide infinite", dtype, io)
+    prefix = 9000
+    g = Groups([(9, prefix)], [prefix + t for t in (0, 3, 64, 200, 1, 2, 3, 4, 5)], 1, 64, 32, dtype, seed=16)
+    b = g.b
+    for s, at, ch, x in ((0, 3, 1, INF), (0, 5000, 2, -INF), (0, 8999, 0, NAN), (0, 100, 5, INF), (0, 7000, 5, -INF), (1, prefix + 1, 3, INF),
+                         (3, prefix + 150, 2, INF), (3, prefix + 151, 60, -INF)):
+        b.v[s][at, 0, ch] = x
+    g.write()
+    g.run_and_check(256, io, seed=16, scale=0.1, rows=[0, 1, 2, 3, 8])
+    k, v, table, lens = b.on(DEV)            # what lies behind the prefix and in other pages changes no bit
+    q = torch.randn(9, 256 * 64, generator=torch.Generator().manual_seed(1)).to(M.DTYPES[io]).to(DEV)
+    outs = []
+    for fill in (0.0, INF, 3.0):
+        v2 = v.clone()
+        spare = [i for i in range(b.pages) if not bool((b.table == i).any())]
+        v2[spare] = fill
+        outs.append(g.run(256, q, 0.1, tensors=(k, v2, table, lens)))
+    assert all(torch.equal(torch.nan_to_num(o, 7.0, 8.0, 9.0), torch.nan_to_num(outs[0], 7.0, 8.0, 9.0)) for o in outs)
+
+
+def test_a_wide_prefix_among_more_sequences_than_a_launch_takes():
+    """A group on both sides of the 1024th sequence whose prefix is wide in either launch."""
+    _announce("shared wide 1100 sequences")
+    prefix = 5000
+    groups = [(900, 20), (200, prefix)]
+    lens = [20 + i % 7 for i in range(900)] + [prefix + i % 9 for i in range(200)]
+    Groups(groups, lens, 1, 64, 32, "bf16", seed=17).run_and_check(16, "bf16", seed=17, rows=[0, 899, 900, 1000, 1023, 1024, 1025, 1099])
+
+
 def test_more_sequences_than_a_launch_takes():
     """Groups that lie on both sides of the 1024th sequence, and one of more than that."""
     _announce("shared 2500 sequences")

@@ -47,7 +47,7 @@ def _run(x, gamma, eps, res=None, y="f32", codes=True, rowsum=True, stored=True)
 
 
 # every form of the kernel: one wave to 16 a row, one to 16 quads a thread, single values where rows are no quads, long rows
-WIDTHS = [1, 2, 3, 4, 5, 63, 64, 67, 255, 256, 1023, 1024, 1028, 1030, 2048, 2052, 3200, 4096, 4097, 4100, 8190, 8192, 8640, 14336, 16384,
+WIDTHS = [1, 2, 3, 4, 5, 63, 64, 67, 255, 256, 1023, 1024, 1028, 1030, 2048, 2052, 3200, 4096, 4097, 4100, 8190, 8192, 8640, 10240, 10244, 14336, 16384,
           16387, 16388, 33024, 65536, 65537, 65540, 70001]
 
 
