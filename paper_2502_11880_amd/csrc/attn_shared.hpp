@@ -15,9 +15,9 @@ constexpr int kNarrowColumns = 64;   // up to so many: always the former
 constexpr int wide_columns(int dim, bool f32) { return !f32 && dim > 64 && dim <= 128 ? 256 : 128; }
 // What decides past that: picoseconds a key and kv head of a pass of either, and the microseconds that the second launch costs by
 // itself.  Measured on 8 kv heads of 4 query heads (us, in registers / in shared memory):
-//   heads of 128, bf16 throughout: 128 columns behind 1024 keys 30 / 41, 6016 41 / 46, 32768 103 / 67; 256 columns 36 / 45,
-//   47 / 53, 177 / 89; q from 32 bits over bf16, 128 columns 33 / 51, 44 / 57, 108 / 98, 256 columns 39 / 55, 51 / 69, 191 / 160; over
-//   f16, 256 columns 37 / 52, 49 / 63, 186 / 138;
+//   heads of 128, bf16 throughout: 80 columns behind 1024 keys 29 / 40, 6016 39 / 44, 32768 80 / 69; 128 columns 33 / 42, 44 / 47,
+//   92 / 71; 256 columns 37 / 48, 57 / 56, 144 / 87; q from 32 bits over bf16, 128 columns 33 / 51, 44 / 57, 108 / 98, 256 columns
+//   39 / 55, 51 / 69, 191 / 160; over f16, 256 columns 37 / 52, 49 / 63, 186 / 138;
 //   heads of 64, bf16, 256 columns 36 / 36, 47 / 42, 109 / 67, from 32 bits 38 / 42, 48 / 49, 115 / 92;
 //   heads of 256, bf16, 256 columns behind 1024 keys 62 / 71, 6016 112 / 88, from 32 bits 68 / 102, 122 / 135.
 struct WideRule {
@@ -25,7 +25,7 @@ struct WideRule {
 };
 constexpr WideRule wide_rule(int dim, bool f32, bool three_parts) {
     if (dim <= 64) return f32 ? WideRule{76, 100, 4} : WideRule{72, 61, 2};
-    if (dim <= 128) return three_parts ? WideRule{75, 205, 18} : f32 ? WideRule{73, 168, 15} : WideRule{69, 88, 12};
+    if (dim <= 128) return three_parts ? WideRule{75, 205, 18} : f32 ? WideRule{73, 168, 15} : WideRule{55, 115, 14};
     return f32 ? WideRule{167, 412, 37} : WideRule{157, 211, 16};
 }
 __host__ __device__ __forceinline__ bool worth_wide(const WideRule& r, int64_t columns, int narrow_columns, int wide_columns, int64_t keys,
