@@ -108,8 +108,11 @@ __device__ void build_index(const SharedArgs& a, Index& x, int64_t (&wave_cost)[
         x.len[s] = seq_len(a.c, a.first_seq + s);
     }
     __syncthreads();
-    for (int g = tid; g < a.n_groups; g += kThreads) {
+    // groups from the one that the launch's first sequence belongs to
+    const int first_group = a.first_seq == 0 ? 0 : find_last(a.n_groups, a.first_seq, [&](int i) { return a.group_start[i]; });
+    for (int g = first_group + tid; g < a.n_groups; g += kThreads) {
         const int b0 = a.group_start[g], b1 = a.group_start[g + 1];
+        if (b0 >= a.first_seq + a.n_seqs) break;
         if (b0 < 0 || b1 <= b0 || b1 > a.c.n_seqs) continue;
         const int s0 = max(b0 - a.first_seq, 0), s1 = min(b1 - a.first_seq, a.n_seqs);
         if (s0 >= s1) continue;
@@ -837,10 +840,11 @@ hipError_t launch_dim(const SharedArgs& a, hipStream_t s) {
 
 }  // namespace
 
-size_t attn_shared_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim) {
+size_t attn_shared_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim, int64_t keys) {
     const int64_t n = n_seqs < kSharedSeqs ? n_seqs : kSharedSeqs, group = heads / kv_heads;
+    const int narrow = columns_of(n, (int)group, dim);
     // (work groups times columns of the launch for wide prefixes: as many with 128 columns as with 256)
-    const int64_t columns = columns_of(n, (int)group, dim) + (n * group > kNarrowColumns ? 128 : 0);
+    const int64_t columns = narrow + (wide_possible(n * group, narrow, keys, kv_heads, dim) ? 128 : 0);
     const int64_t records = 2 * n * heads + 2 * kSharedGroups * columns;
     return (size_t)kHeaderBytes + (size_t)records * record_floats(dim) * 4;
 }

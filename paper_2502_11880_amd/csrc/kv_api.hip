@@ -230,7 +230,7 @@ size_t bitnet_attn_decode_shared_workspace_bytes(int64_t n_seqs, int64_t n_heads
     if (shift_of(page_size) < 0 || !heads_ok(n_kv_heads, head_dim) || !rows_ok(n_seqs, max_pages, page_size) || n_heads < 1 ||
         n_heads > kMaxHeads || n_heads % n_kv_heads || window < 0 || n_sink < 0)
         return 0;
-    return bitnet::attn_shared_workspace_bytes(n_seqs, (int)n_heads, (int)n_kv_heads, (int)head_dim);
+    return bitnet::attn_shared_workspace_bytes(n_seqs, (int)n_heads, (int)n_kv_heads, (int)head_dim, max_pages * page_size);
 }
 
 bitnet_status bitnet_attn_decode_shared(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads,

@@ -265,8 +265,8 @@ struct AttnArgs {
 size_t attn_decode_workspace_bytes(int heads, int kv_heads, int dim, int page_size, int64_t max_pages, int window, int n_sink);
 bool attn_decode_splits(int64_t n_seqs, int heads, int kv_heads, int page_size, int64_t max_pages, int window, int n_sink);
 hipError_t launch_attn_decode(const KvCache& c, int dtype, const AttnArgs& a, void* ws, hipStream_t s);
-// Decode of groups of sequences that share their first keys (args.q_start: the groups' first sequences).
-size_t attn_shared_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim);
+// Decode of groups of sequences that share their first keys (args.q_start: the groups' first sequences).  keys: of a row of the table.
+size_t attn_shared_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim, int64_t keys);
 hipError_t launch_attn_shared(const KvCache& c, int dtype, const AttnArgs& args, const int32_t* prefix_len, int n_groups, void* ws,
                               hipStream_t s);
 // Prefill: ws null or smaller than this: nothing is split.
