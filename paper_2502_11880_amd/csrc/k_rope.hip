@@ -4,6 +4,9 @@
 //
 // Memory bounds it: x is read and written once.  A work group takes some heads of one token: its threads work out the token's
 // angles (in 64 bits, see turn_of), share them through LDS, and each then keeps its place in a head while it walks the heads.
+//
+// Measured (kernel times): 6001 tokens of 32 heads of 100, 48 channels turned, f16, 14.6 us (5.3 TB/s); seven tokens of 32 heads of 128
+// 2.7, of which an empty launch takes 1.7.
 #include "rows.hpp"
 
 namespace bitnet {
