@@ -108,21 +108,26 @@ __device__ __forceinline__ void sum_line(int n, F cost_at, int64_t* start, int64
 // All of it worked out by every work group: the groups' marks, then sums and the last mark before each sequence in one scan.
 __device__ void build_index(const SharedArgs& a, Index& x, int64_t (&wave_cost)[kWaves], int (&wave_lead)[kWaves]) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, most = a.c.max_pages << a.c.shift;
+    // groups from the one that the launch's first sequence belongs to; the first ones' bounds are asked for beside the lengths
+    const int first_group = a.first_seq == 0 ? 0 : find_last(a.n_groups, a.first_seq, [&](int i) { return a.group_start[i]; });
+    int g = first_group + tid, b0 = 0, b1 = 0, p = 0;
+    auto ask = [&] {
+        if (g >= a.n_groups) return;
+        b0 = a.group_start[g];
+        b1 = a.group_start[g + 1];
+        p = a.prefix_len[g];
+    };
+    ask();
     for (int s = tid; s < a.n_seqs; s += kThreads) {
         x.members[s] = 0;
         x.low[s] = a.window > 0 ? most : 0;
         x.len[s] = seq_len(a.c, a.first_seq + s);
     }
     __syncthreads();
-    // groups from the one that the launch's first sequence belongs to
-    const int first_group = a.first_seq == 0 ? 0 : find_last(a.n_groups, a.first_seq, [&](int i) { return a.group_start[i]; });
-    for (int g = first_group + tid; g < a.n_groups; g += kThreads) {
-        const int b0 = a.group_start[g], b1 = a.group_start[g + 1];
-        if (b0 >= a.first_seq + a.n_seqs) break;
+    for (; g < a.n_groups && b0 < a.first_seq + a.n_seqs; g += kThreads, ask()) {
         if (b0 < 0 || b1 <= b0 || b1 > a.c.n_seqs) continue;
         const int s0 = max(b0 - a.first_seq, 0), s1 = min(b1 - a.first_seq, a.n_seqs);
         if (s0 >= s1) continue;
-        const int p = a.prefix_len[g];
         x.members[s0] = (uint16_t)(s1 - s0);
         x.prefix[s0] = p < 0 ? 0 : p < most ? p : most;
         if (s0 == 0) x.first_row = b0;
@@ -690,7 +695,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_shared_kernel
     build_index(a, lds.index, lds.wave_cost, lds.wave_lead);
     const Index& x = lds.index;
     const int64_t all = x.start[a.n_seqs], share = share_of(a, all);
-    if (blockIdx.x == 0) {
+    if (blockIdx.x == gridDim.x - 1) {                    // the last one, which has the least to do
         Header* h = reinterpret_cast<Header*>(a.ws);
         if (tid == 0) {
             h->share = share;
