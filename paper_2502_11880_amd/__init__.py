@@ -412,8 +412,8 @@ class _Rotation(ctypes.Structure):         # bitnet_rotation
     _fields_ = [("freqs", ctypes.c_void_p), ("rot_dim", ctypes.c_int64), ("interleaved", ctypes.c_int32), ("gain", ctypes.c_float)]
 
 
-def _rotation(freqs, interleaved, gain):
-    return _Rotation(_ptr(freqs, "freqs", _widths()[3]), 2 * freqs.numel(), 1 if interleaved else 0, gain)
+def _rotation(freqs, interleaved, gain, now):
+    return _Rotation(_on(freqs, "freqs", now, _widths()[3]), 2 * freqs.numel(), 1 if interleaved else 0, gain)
 
 
 @functools.lru_cache(maxsize=None)
@@ -424,12 +424,26 @@ def _current_device():
     return getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _here(*tensors) -> None:
-    """A call runs on the current device: its tensors have to be there."""
-    now = _current_device()()
-    for t in tensors:
-        if t is not None and t.get_device() != now:
-            raise ValueError(f"tensors must be on the current device {now}, got one on {t.get_device()}")
+def _here(now, *cache) -> None:
+    """A call runs on the current device: the cache's tensors have to be there."""
+    for t in cache:
+        if t.get_device() != now:
+            raise ValueError(f"the cache must be on the current device {now}, got a tensor on {t.get_device()}")
+
+
+def _on(t, name, now, dtype=None):
+    """_ptr of a tensor that has to be on device `now`, the current one."""
+    if t is None:
+        return None
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != now:
+        if not t.is_cuda:
+            raise TypeError(f"{name} must be a device tensor")
+        raise ValueError(f"{name} must be on the current device {now}, got {t.get_device()}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 @functools.lru_cache(maxsize=None)
@@ -458,11 +472,12 @@ def bitnet_norm_quantize(x, gamma, eps: float, xq=None, x_scale=None, x_rowsum=N
             raise ValueError(f"{name} must have {n} entries, got {t.numel()}")
     if residual_out is not None and residual is not None and residual_out.dtype != residual.dtype:
         raise TypeError(f"residual_out must be {residual.dtype}, got {residual_out.dtype}")
-    a, b, c, d, e = _ptr(x, "x"), _ptr(residual, "residual"), _ptr(residual_out, "residual_out"), _ptr(gamma, "gamma", f32), _ptr(y, "y")
-    f, g, h = _ptr(xq, "xq", i8), _ptr(x_scale, "x_scale", f32), _ptr(x_rowsum, "x_rowsum", i32)
-    _here(x, residual, residual_out, gamma, y, xq, x_scale, x_rowsum)
-    st = lib().bitnet_norm_quantize(a, _dtype(x, "x"), b, c, 0 if residual is None else _dtype(residual, "residual"), d, eps, M, K, e,
-                                    0 if y is None else _dtype(y, "y"), f, g, h, _stream(stream))
+    now = _current_device()()
+    st = lib().bitnet_norm_quantize(_on(x, "x", now), _dtype(x, "x"), _on(residual, "residual", now),
+                                    _on(residual_out, "residual_out", now), 0 if residual is None else _dtype(residual, "residual"),
+                                    _on(gamma, "gamma", now, f32), eps, M, K, _on(y, "y", now), 0 if y is None else _dtype(y, "y"),
+                                    _on(xq, "xq", now, i8), _on(x_scale, "x_scale", now, f32), _on(x_rowsum, "x_rowsum", now, i32),
+                                    _stream(stream))
     _check("bitnet_norm_quantize", st)
 
 
@@ -471,9 +486,8 @@ def bitnet_rope_freqs(freqs, theta: float, scaling="none", factor: float = 1.0, 
     """Turns a position of each pair of a rotation of 2 * freqs.numel() channels, into freqs (float64): theta^(-2i / rot_dim) /
     2 pi, stretched for contexts longer than `original` as `scaling` says (none, linear, base, turns or index)."""
     kind = ROPE_SCALINGS[scaling] if isinstance(scaling, str) else int(scaling)
-    pointer = _ptr(freqs, "freqs", _widths()[3])
-    _here(freqs)
-    st = lib().bitnet_rope_freqs(kind, theta, 2 * freqs.numel(), factor, original, low, high, pointer, _stream(stream))
+    st = lib().bitnet_rope_freqs(kind, theta, 2 * freqs.numel(), factor, original, low, high,
+                                 _on(freqs, "freqs", _current_device()(), _widths()[3]), _stream(stream))
     _check("bitnet_rope_freqs", st)
 
 
@@ -486,9 +500,12 @@ def bitnet_rope(x, pos, freqs, out, head_dim: int, interleaved: bool = False, ga
     heads, rest = divmod(x.numel(), max(1, n) * head_dim) if n else (1, 0)
     if rest:
         raise ValueError(f"x {tuple(x.shape)} must have rows of whole heads of {head_dim}")
-    r, pointers = _rotation(freqs, interleaved, gain), (_ptr(x, "x"), _list(pos, "pos", n), _ptr(out, "out"))
-    _here(x, pos, freqs, out)
-    st = lib().bitnet_rope(ctypes.byref(r), pointers[0], _dtype(x, "x"), n, heads, head_dim, pointers[1], pointers[2], _stream(stream))
+    if pos.numel() != n:
+        raise ValueError(f"pos must have {n} entries, got {pos.numel()}")
+    now = _current_device()()
+    r = _rotation(freqs, interleaved, gain, now)
+    st = lib().bitnet_rope(ctypes.byref(r), _on(x, "x", now), _dtype(x, "x"), n, heads, head_dim, _on(pos, "pos", now, _types()[0]),
+                           _on(out, "out", now), _stream(stream))
     _check("bitnet_rope", st)
 
 
@@ -507,11 +524,14 @@ def bitnet_kv_append_rope(k, v, q_start, k_cache, v_cache, table, kv_len, freqs,
         if q.shape[0] != n:
             raise ValueError(f"q must have one row for each of the {n} tokens, got {q.shape[0]}")
         heads = _heads(q, q_out, c, n)
-    r = _rotation(freqs, interleaved, gain)
-    pointers = (_ptr(q, "q"), _ptr(k, "k"), _ptr(v, "v"), None if q_start is None else _q_start(q_start, c.n_seqs), _ptr(q_out, "q_out"))
-    _here(k, v, q_start, k_cache, v_cache, table, kv_len, freqs, q, q_out)
-    st = lib().bitnet_kv_append_rope(ctypes.byref(c), ctypes.byref(r), pointers[0], heads, pointers[1], pointers[2],
-                                     _dtype(k, "k"), pointers[3], n, pointers[4], _stream(stream))
+    if q_start is not None and q_start.numel() != c.n_seqs + 1:
+        raise ValueError(f"q_start must have {c.n_seqs + 1} entries, got {q_start.numel()}")
+    now = _current_device()()
+    r = _rotation(freqs, interleaved, gain, now)
+    _here(now, k_cache, v_cache, table, kv_len)
+    st = lib().bitnet_kv_append_rope(ctypes.byref(c), ctypes.byref(r), _on(q, "q", now), heads, _on(k, "k", now), _on(v, "v", now),
+                                     _dtype(k, "k"), _on(q_start, "q_start", now, _types()[0]), n, _on(q_out, "q_out", now),
+                                     _stream(stream))
     _check("bitnet_kv_append_rope", st)
 
 
@@ -561,12 +581,11 @@ def bitnet_attn_decode_shared(q, group_start, prefix_len, k_cache, v_cache, tabl
     groups = prefix_len.numel()
     if group_start.numel() != groups + 1:
         raise ValueError(f"group_start must have {groups + 1} entries, got {group_start.numel()}")
-    i32 = _types()[0]
-    pointers = (_ptr(q, "q"), _ptr(group_start, "group_start", i32), _ptr(prefix_len, "prefix_len", i32), _ptr(out, "out"), _ptr(ws, "ws"))
-    heads, dtype = _heads(q, out, c, c.n_seqs), _dtype(q, "q")
-    _here(q, group_start, prefix_len, k_cache, v_cache, table, kv_len, out, ws)
-    st = lib().bitnet_attn_decode_shared(ctypes.byref(c), pointers[0], dtype, heads, pointers[1], pointers[2], groups, scale,
-                                         window, n_sink, pointers[3], pointers[4],
+    i32, now = _types()[0], _current_device()()
+    _here(now, k_cache, v_cache, table, kv_len)
+    st = lib().bitnet_attn_decode_shared(ctypes.byref(c), _on(q, "q", now), _dtype(q, "q"), _heads(q, out, c, c.n_seqs),
+                                         _on(group_start, "group_start", now, i32), _on(prefix_len, "prefix_len", now, i32), groups, scale,
+                                         window, n_sink, _on(out, "out", now), _on(ws, "ws", now),
                                          0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
     _check("bitnet_attn_decode_shared", st)
 
