@@ -355,3 +355,41 @@ def test_binding_refusals():
     out = torch.full_like(q, 3.0)
     B.bitnet_attn_decode_shared(q, i(0), i(), k, v, table, kv_len, out, 1.0, ws=ws)     # no groups: nothing written
     assert bool((out == 3.0).all())
+
+
+def test_pages_past_four_gib():
+    """The same pages at the lowest and at the highest numbers of a pool of 5 GiB of keys and as much of values, for prefixes in
+    registers and in shared memory: the same bits; and tokens appended there."""
+    _announce("shared pages past 4 GiB")
+    Hkv, D, page, pages = 8, 128, 256, 10300
+    k = torch.empty(pages, Hkv, D // 8, page, 8, dtype=torch.bfloat16, device=DEV)
+    v = torch.empty(pages, Hkv, page // 8, D, 8, dtype=torch.bfloat16, device=DEV)
+    assert k.numel() * 2 > 5 << 30
+    g = torch.Generator(device=DEV).manual_seed(5)
+    used = 90
+    k[:used].copy_(torch.randn(used, *k.shape[1:], device=DEV, generator=g))
+    v[:used].copy_(torch.randn(used, *v.shape[1:], device=DEV, generator=g))
+    high = pages - 1 - torch.arange(used, device=DEV)
+    k[high], v[high] = k[:used].clone(), v[:used].clone()
+    i32 = dict(dtype=torch.int32, device=DEV)
+    for prefix, H in ((700, 16), (20000, 256)):
+        first = -(-prefix // page)
+        rows = [list(range(first)) + [first + 2 * s, first + 2 * s + 1] for s in range(4)]
+        lens = torch.tensor([first * page + 10 + 70 * s for s in range(4)], **i32)
+        q = torch.randn(4, H * D, device=DEV, generator=g).to(torch.bfloat16)
+        outs = []
+        for ids in (torch.arange(used, device=DEV), high):
+            table = ids[torch.tensor(rows, device=DEV)].to(torch.int32).contiguous()
+            out = torch.empty_like(q)
+            ws = torch.empty(B.bitnet_attn_decode_shared_workspace_bytes(4, H, Hkv, D, page, table.shape[1]), dtype=torch.uint8, device=DEV)
+            B.bitnet_attn_decode_shared(q, torch.tensor([0, 4], **i32), torch.tensor([prefix], **i32), k, v, table, lens, out, 0.09, ws=ws)
+            outs.append(out)
+        assert torch.equal(*outs) and bool(torch.isfinite(outs[0]).all()), prefix
+    freqs = torch.empty(64, dtype=torch.float64, device=DEV)
+    B.bitnet_rope_freqs(freqs, 10000.0)
+    kn, vn = torch.randn(20, Hkv * D, device=DEV, generator=g), torch.randn(20, Hkv * D, device=DEV, generator=g)
+    lens, start = torch.tensor([520], **i32), torch.tensor([0, 20], **i32)
+    for ids in (torch.arange(3, device=DEV), high[:3]):
+        B.bitnet_kv_append_rope(kn, vn, start, k, v, ids[None].to(torch.int32).contiguous(), lens, freqs)
+    assert torch.equal(k[:3], k[high[:3]]) and torch.equal(v[:3], v[high[:3]])
+    assert torch.equal(v[2, :, 0, :, 0].reshape(-1), vn[12].to(torch.bfloat16))     # position 512 is the third page's first
