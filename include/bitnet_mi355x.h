@@ -416,9 +416,8 @@ size_t bitnet_attn_decode_shared_workspace_bytes(int64_t n_seqs, int64_t n_heads
  *                 first sequence, and are read from that one's pages; what the others' rows of the table name there is not looked
  *                 at.  Any number of tokens, 0 among them; a sequence that is shorter sees its first kv_len only.
  *   0 <= n_groups <= n_seqs.  ws: bitnet_attn_decode_shared_workspace_bytes(...) bytes, any contents, nothing kept (9 to 35 MB with
- *   heads of 128, 70 more where a prefix could be long and of many columns, and twice the size of out in 32 bits).  All else (types, what is visible, what is not finite, one result for one call) as
- *   bitnet_attn_decode, but that over a long prefix of more than 64 columns (sequences times query heads of a kv head), with q and out of
- *   the cache's type, the weights are rounded to it once and summed as rounded, as in bitnet_attn_prefill.
+ *   heads of 128, 70 more where a prefix could be long and of many columns, and twice the size of out in 32 bits).  All else (types, precision, what is visible, what is not finite, one result for one
+ *   call) as bitnet_attn_decode.
  */
 bitnet_status bitnet_attn_decode_shared(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads,
                                         const int32_t* group_start, const int32_t* prefix_len, int64_t n_groups, float scale,

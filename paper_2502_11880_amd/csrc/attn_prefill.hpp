@@ -59,7 +59,9 @@ template <int T, int DP, bool F32, int WAVES, bool FULL, int MODE>
 struct Prefill {
     static constexpr bool SPLIT = MODE != kWhole;
     static constexpr int kQParts = F32 ? Elem<T>::kExactParts : 1;
-    static constexpr int kPParts = kQParts;
+    // Weights in as many parts as q; over a shared prefix in two at least, as the decode's are (a sequence's result must not be less
+    // exact for its neighbours).
+    static constexpr int kPParts = MODE == kPrefix && !F32 ? 2 : kQParts;
     static constexpr int kThreads = 64 * WAVES, kColumns = 32 * WAVES;
     static constexpr int kSteps = DP / 16, kBlocks = (DP + 31) / 32;
     static constexpr int kWords = kTile * DP / 8;         // 16-byte words of a tile's keys (and at most of its values)
