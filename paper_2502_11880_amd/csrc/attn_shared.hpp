@@ -34,17 +34,9 @@ __host__ __device__ __forceinline__ bool worth_wide(const WideRule& r, int64_t c
     const int64_t narrow = (columns + narrow_columns - 1) / narrow_columns * r.narrow, wide = (columns + wide_columns - 1) / wide_columns * r.wide;
     return keys * kv_heads * (narrow - wide) > (int64_t)r.start * 1000000;
 }
-// Whether it could be for some group of up to `columns` columns, in any type of q: the difference grows with them but for where a
-// wide pass begins.
-inline bool wide_possible(int64_t columns, int narrow_columns, int64_t keys, int kv_heads, int dim) {
-    for (int f32 = 0; f32 < 2; ++f32)
-        for (int three = 0; three <= f32; ++three) {
-            const int width = wide_columns(dim, f32 != 0);
-            for (const int64_t c : {columns, columns / width * width})
-                if (worth_wide(wide_rule(dim, f32 != 0, three != 0), c, narrow_columns, width, keys, kv_heads)) return true;
-        }
-    return false;
-}
+// Whether it could be for some group of up to `columns` columns behind up to `keys`: the difference grows with the columns but for where a
+// wide pass begins.  What the launch for wide prefixes goes by, and the workspace (for any type of q).  (keys: of a row of the table)
+bool attn_shared_may_be_wide(int64_t columns, int64_t keys, int kv_heads, int dim, bool f32, bool three_parts);
 constexpr int kWideTile = 64;        // keys
 constexpr int kWideCost = 2, kWideStart = 6;   // of a tile, and of a row's start
 

@@ -825,8 +825,7 @@ hipError_t launch_page(SharedArgs a, hipStream_t s) {
     for (int at = 0; at < total; at += kSharedSeqs) {
         a.first_seq = at;
         a.n_seqs = total - at < kSharedSeqs ? total - at : kSharedSeqs;
-        // the most that the launch's sequences could share
-        const bool wide = worth_wide(a.rule, (int64_t)a.n_seqs * a.group, a.columns, a.wide_columns, (int64_t)a.c.max_pages << a.c.shift, a.c.kv_heads);
+        const bool wide = attn_shared_may_be_wide((int64_t)a.n_seqs * a.group, (int64_t)a.c.max_pages << a.c.shift, a.c.kv_heads, a.c.dim, F32, F32 && T == kBf16);
         a.wide_groups = wide ? attn_shared_wide_groups(a.c.dim, F32) : 0;
         hipLaunchKernelGGL((attn_shared_kernel<T, DP, F32, FULL, PAGE16>), dim3((unsigned)groups), dim3(kThreads), 0, s, a);
         if (a.wide_groups) {
@@ -853,11 +852,21 @@ hipError_t launch_dim(const SharedArgs& a, hipStream_t s) {
 
 }  // namespace
 
+bool attn_shared_may_be_wide(int64_t columns, int64_t keys, int kv_heads, int dim, bool f32, bool three_parts) {
+    const int width = wide_columns(dim, f32);
+    for (const int64_t c : {columns, columns / width * width})
+        if (worth_wide(wide_rule(dim, f32, three_parts), c, 16 * most_tiles(dim), width, keys, kv_heads)) return true;
+    return false;
+}
+
 size_t attn_shared_workspace_bytes(int64_t n_seqs, int heads, int kv_heads, int dim, int64_t keys) {
     const int64_t n = n_seqs < kSharedSeqs ? n_seqs : kSharedSeqs, group = heads / kv_heads;
     const int narrow = columns_of(n, (int)group, dim);
     // (work groups times columns of the launch for wide prefixes: as many with 128 columns as with 256)
-    const int64_t columns = narrow + (wide_possible(n * group, narrow, keys, kv_heads, dim) ? 128 : 0);
+    bool wide = false;
+    for (int f32 = 0; f32 < 2; ++f32)
+        for (int three = 0; three <= f32; ++three) wide |= attn_shared_may_be_wide(n * group, keys, kv_heads, dim, f32 != 0, three != 0);
+    const int64_t columns = narrow + (wide ? 128 : 0);
     const int64_t records = 2 * n * heads + 2 * kSharedGroups * columns;
     return (size_t)kHeaderBytes + (size_t)records * record_floats(dim) * 4;
 }

@@ -1,0 +1,42 @@
+"""What decode over shared prefixes decides on the host, on the CPU: whether a launch could have a group whose prefix goes through shared
+memory, and the workspace that goes by it."""
+import ctypes
+
+import pytest
+
+import paper_2502_11880_amd as B
+
+KEYS = (1024, 6016, 20000, 65536, 1 << 20)
+
+
+def _may(columns, keys, kv_heads, dim, f32, three_parts):
+    fn = B.lib()["_ZN6bitnet23attn_shared_may_be_wideElliibb"]
+    fn.restype, fn.argtypes = ctypes.c_bool, [ctypes.c_int64, ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_bool, ctypes.c_bool]
+    return fn(columns, keys, kv_heads, dim, f32, three_parts)
+
+
+@pytest.mark.parametrize("f32,three_parts", [(False, False), (True, False), (True, True)])
+@pytest.mark.parametrize("dim", [4, 64, 80, 128, 132, 256])
+@pytest.mark.parametrize("kv_heads", [1, 8, 32])
+def test_other_sequences_never_keep_a_group_from_shared_memory(kv_heads, dim, f32, three_parts):
+    """A launch may have any group of up to its own columns: what is worth it for one of them stays so beside others."""
+    for keys in KEYS:
+        may = [_may(c, keys, kv_heads, dim, f32, three_parts) for c in range(1, 2050)]
+        first = may.index(True) if True in may else len(may)
+        assert all(may[first:]), (keys, first + 1, may.index(False, first) + 1)
+        assert not any(may[:64]), "up to 64 columns go through registers"
+
+
+def test_some_prefixes_go_through_shared_memory():
+    """Thousands of columns behind a long prefix do, in every type."""
+    for dim in (64, 128, 256):
+        for f32, three_parts in ((False, False), (True, False), (True, True)):
+            assert _may(2048, 1 << 20, 8, dim, f32, three_parts)
+
+
+@pytest.mark.parametrize("dim", [64, 100, 128, 256])
+def test_workspace_grows_with_the_batch(dim):
+    for heads, kv_heads in ((32, 8), (32, 32), (64, 1)):
+        for max_pages in (10, 100, 1024, 4096):
+            sizes = [B.bitnet_attn_decode_shared_workspace_bytes(n, heads, kv_heads, dim, 64, max_pages) for n in range(1, 1100)]
+            assert sizes == sorted(sizes)
