@@ -24,6 +24,10 @@ struct WideRule {
     int narrow, wide, start;
 };
 constexpr WideRule wide_rule(int dim, bool f32, bool three_parts) {
+    // Heads between 128 and 256 never: their words past D and the masks take the registers (185 to 318 spilled).  128 columns behind 32768
+    // keys, 8 kv heads, in registers / in shared memory: heads of 132 191 / 322, of 192 203 / 363, of 192 from 32 bits 213 / 417; 512 columns
+    // 732 / 1111, 786 / 1205 and 810 / 1405.
+    if (dim > 128 && dim < 256) return WideRule{0, 0, 0};
     if (dim <= 64) return f32 ? WideRule{76, 100, 4} : WideRule{72, 61, 2};
     if (dim <= 128) return three_parts ? WideRule{75, 205, 18} : f32 ? WideRule{73, 168, 15} : WideRule{55, 115, 14};
     return f32 ? WideRule{167, 412, 37} : WideRule{157, 211, 16};

@@ -81,8 +81,8 @@ template <int T, int DP, bool F32>
 hipError_t launch(const SharedArgs& a, hipStream_t s) {
     constexpr int kWaves = wide_columns(DP, F32) / 32, kPerSimd = per_simd(DP, F32);
     const dim3 grid((unsigned)a.wide_groups), block(64 * kWaves);
-    if (a.c.dim == DP) hipLaunchKernelGGL((attn_shared_wide_kernel<T, DP, F32, kPerSimd, kWaves, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((attn_shared_wide_kernel<T, DP, F32, kPerSimd, kWaves, false>), grid, block, 0, s, a);
+    if (DP == 256 || a.c.dim == DP) hipLaunchKernelGGL((attn_shared_wide_kernel<T, DP, F32, kPerSimd, kWaves, true>), grid, block, 0, s, a);
+    else if constexpr (DP < 256) hipLaunchKernelGGL((attn_shared_wide_kernel<T, DP, F32, kPerSimd, kWaves, false>), grid, block, 0, s, a);
     return hipGetLastError();
 }
 
@@ -90,7 +90,7 @@ template <int T, bool F32>
 hipError_t launch_dim(const SharedArgs& a, hipStream_t s) {
     if (a.c.dim <= 64) return launch<T, 64, F32>(a, s);
     if (a.c.dim <= 128) return launch<T, 128, F32>(a, s);
-    return launch<T, 256, F32>(a, s);
+    return launch<T, 256, F32>(a, s);                     // 256: others past 128 have no wide prefixes (wide_rule)
 }
 
 }  // namespace
