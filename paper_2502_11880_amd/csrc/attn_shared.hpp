@@ -14,12 +14,14 @@ constexpr int kNarrowColumns = 64;   // up to so many: always the former
 // Columns of a wide pass: four waves' or eight waves' (q in one part leaves registers for two waves a SIMD).
 constexpr int wide_columns(int dim, bool f32) { return !f32 && dim > 64 && dim <= 128 ? 256 : 128; }
 // What decides past that: picoseconds a key and kv head of a pass of either, and the microseconds that the second launch costs by
-// itself.  Measured on 8 kv heads of 4 query heads (us, in registers / in shared memory):
-//   heads of 128, bf16 throughout: 80 columns behind 1024 keys 29 / 40, 6016 39 / 44, 32768 80 / 69; 128 columns 33 / 42, 44 / 47,
-//   92 / 71; 256 columns 37 / 48, 57 / 56, 144 / 87; q from 32 bits over bf16, 128 columns 33 / 51, 44 / 57, 108 / 98, 256 columns
-//   39 / 55, 51 / 69, 191 / 160; over f16, 256 columns 37 / 52, 49 / 63, 186 / 138;
-//   heads of 64, bf16, 256 columns 36 / 36, 47 / 42, 109 / 67, from 32 bits 38 / 42, 48 / 49, 115 / 92;
-//   heads of 256, bf16, 256 columns behind 1024 keys 62 / 71, 6016 112 / 88, from 32 bits 68 / 102, 122 / 135.
+// itself, fitted to 576 pairs of calls that were sent either way (heads of 32 to 256; 80, 128, 256 and 512 columns; 1, 8 and 32 kv
+// heads; 1024, 6016 and 32768 keys).  Past heads of 64 the slower side was taken 4% too slow at the worst, up to them 14% (one kv
+// head or 32 have not the costs of 8).  us, in registers / in shared memory, 8 kv heads, behind 1024, 6016 and 32768 keys:
+//   heads of 64, bf16: 80 columns 22 / 33, 31 / 34, 55 / 50; 256 columns 32 / 35, 44 / 41, 94 / 68, from 32 bits 35 / 37, 48 / 46, 96 / 83;
+//   heads of 128, bf16: 80 columns 27 / 38, 38 / 41, 79 / 69; 256 columns 32 / 49, 58 / 56, 182 / 90; 512 columns 44 / 61, 90 / 73, 351 / 147,
+//     from 32 bits 46 / 63, 92 / 91, 347 / 251, from 32 bits over f16 45 / 59, 92 / 80, 350 / 198;
+//   heads of 256, bf16: 80 columns 49 / 65, 66 / 76, 178 / 150; 512 columns 98 / 111, 207 / 166, 930 / 437, from 32 bits 110 / 144, 216 / 248,
+//     894 / 773, from 32 bits over f16 103 / 128, 209 / 215, 912 / 642.
 struct WideRule {
     int narrow, wide, start;
 };
@@ -28,9 +30,9 @@ constexpr WideRule wide_rule(int dim, bool f32, bool three_parts) {
     // keys, 8 kv heads, in registers / in shared memory: heads of 132 191 / 322, of 192 203 / 363, of 192 from 32 bits 213 / 417; 512 columns
     // 732 / 1111, 786 / 1205 and 810 / 1405.
     if (dim > 128 && dim < 256) return WideRule{0, 0, 0};
-    if (dim <= 64) return f32 ? WideRule{76, 100, 4} : WideRule{72, 61, 2};
-    if (dim <= 128) return three_parts ? WideRule{75, 205, 18} : f32 ? WideRule{73, 168, 15} : WideRule{55, 115, 14};
-    return f32 ? WideRule{167, 412, 37} : WideRule{157, 211, 16};
+    if (dim <= 64) return three_parts ? WideRule{66, 86, 4} : f32 ? WideRule{66, 68, 4} : WideRule{66, 60, 3};
+    if (dim <= 128) return three_parts ? WideRule{67, 166, 20} : f32 ? WideRule{67, 143, 12} : WideRule{58, 83, 13};
+    return three_parts ? WideRule{230, 792, 50} : f32 ? WideRule{230, 704, 50} : WideRule{230, 410, 40};
 }
 __host__ __device__ __forceinline__ bool worth_wide(const WideRule& r, int64_t columns, int narrow_columns, int wide_columns, int64_t keys,
                                                     int kv_heads) {

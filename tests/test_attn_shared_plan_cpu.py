@@ -47,3 +47,18 @@ def test_workspace_grows_with_the_batch(dim):
 def test_heads_between_128_and_256_go_through_registers(dim, f32, three_parts):
     """Measured there 1.2 to 2.4 times as fast, at 128 to 512 columns of 1 to 32 kv heads behind 6016 and 32768 keys."""
     assert not any(_may(c, keys, kv_heads, dim, f32, three_parts) for c in (128, 256, 512, 2048) for keys in KEYS for kv_heads in (1, 8, 32))
+
+
+# Sent both ways on the device: where the difference was more than 12% of the time, the rule takes the faster one.
+@pytest.mark.parametrize("dim,f32,three_parts,columns,kv_heads,keys,shared", [
+    (64, 0, 0, 256, 1, 32768, True), (64, 0, 0, 512, 8, 1024, False), (64, 0, 0, 80, 1, 6016, False), (64, 0, 0, 256, 32, 6016, True),
+    (32, 0, 0, 512, 32, 6016, True), (64, 1, 0, 80, 8, 6016, False), (64, 1, 0, 256, 8, 32768, True), (64, 1, 0, 512, 8, 1024, False),
+    (64, 1, 1, 80, 8, 6016, False), (64, 1, 1, 128, 32, 32768, True), (64, 1, 1, 256, 32, 1024, False), (48, 1, 1, 512, 32, 6016, True),
+    (128, 0, 0, 80, 8, 32768, True), (128, 0, 0, 256, 1, 32768, False), (112, 0, 0, 512, 8, 6016, True), (80, 0, 0, 128, 8, 6016, False),
+    (128, 1, 0, 80, 1, 32768, False), (128, 1, 0, 128, 32, 6016, True), (80, 1, 0, 128, 8, 32768, True), (100, 1, 0, 80, 8, 16000, False),
+    (128, 1, 1, 128, 8, 32768, True), (128, 1, 1, 80, 32, 6016, False), (100, 1, 1, 512, 1, 32768, False), (112, 1, 1, 512, 32, 6016, True),
+    (256, 0, 0, 80, 8, 6016, False), (256, 0, 0, 80, 8, 32768, True), (256, 0, 0, 512, 32, 1024, True), (256, 0, 0, 128, 1, 32768, False),
+    (256, 1, 0, 80, 8, 32768, False), (256, 1, 0, 512, 32, 6016, True), (256, 1, 0, 256, 8, 32768, True), (256, 1, 0, 256, 32, 1024, False),
+    (256, 1, 1, 80, 32, 32768, False), (256, 1, 1, 128, 32, 32768, True), (256, 1, 1, 512, 8, 6016, False), (256, 1, 1, 512, 8, 32768, True)])
+def test_the_rule_takes_the_faster_way(dim, f32, three_parts, columns, kv_heads, keys, shared):
+    assert _may(columns, keys, kv_heads, dim, bool(f32), bool(three_parts)) is shared
