@@ -415,9 +415,10 @@ size_t bitnet_attn_decode_shared_workspace_bytes(int64_t n_seqs, int64_t n_heads
  *   prefix_len    device int32 [n_groups]: the first prefix_len[g] keys and values of every sequence of the group are those of its
  *                 first sequence, and are read from that one's pages; what the others' rows of the table name there is not looked
  *                 at.  Any number of tokens, 0 among them; a sequence that is shorter sees its first kv_len only.
- *   0 <= n_groups <= n_seqs.  ws: bitnet_attn_decode_shared_workspace_bytes(...) bytes, any contents, nothing kept (9 to 35 MB with
- *   heads of 128, 70 more where a prefix could be long and of many columns, and twice the size of out in 32 bits).  All else (types, precision, what is visible, what is not finite, one result for one
- *   call) as bitnet_attn_decode.
+ *   0 <= n_groups <= n_seqs.  ws: bitnet_attn_decode_shared_workspace_bytes(...) bytes, any contents, nothing kept: 4 to 18 MB with
+ *   heads of 64, 9 to 18 of 128, 17 to 35 of 256; 36, 70 and 137 more where a prefix could be long and of many columns (sequences times
+ *   query heads of a kv head); and twice the size of out in 32 bits, of 1024 sequences at most.
+ *   All else (types, precision, what is visible, what is not finite, one result for one call) as bitnet_attn_decode.
  */
 bitnet_status bitnet_attn_decode_shared(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads,
                                         const int32_t* group_start, const int32_t* prefix_len, int64_t n_groups, float scale,

@@ -49,6 +49,17 @@ def test_heads_between_128_and_256_go_through_registers(dim, f32, three_parts):
     assert not any(_may(c, keys, kv_heads, dim, f32, three_parts) for c in (128, 256, 512, 2048) for keys in KEYS for kv_heads in (1, 8, 32))
 
 
+@pytest.mark.parametrize("dim,least,most,wide", [(64, 4, 18, 36), (128, 9, 18, 70), (256, 17, 35, 137)])
+def test_workspace_has_the_stated_size(dim, least, most, wide):
+    """In MB: what the header says, with and without prefixes that could go through shared memory, and the records of whole rows."""
+    for heads, kv_heads in ((1, 1), (32, 8), (32, 32), (64, 1), (96, 12)):
+        for n in (1, 7, 64, 1024, 5000):
+            for max_pages in (1, 20, 1024, 1 << 18):
+                got = B.bitnet_attn_decode_shared_workspace_bytes(n, heads, kv_heads, dim, 64, max_pages) / 1e6
+                twice = 2 * min(n, 1024) * heads * (dim + 4) * 4 / 1e6
+                assert least - 0.5 < got - twice <= most or least + wide - 1 < got - twice <= most + wide, (heads, kv_heads, n, max_pages)
+
+
 # Sent both ways on the device: where the difference was more than 12% of the time, the rule takes the faster one.
 @pytest.mark.parametrize("dim,f32,three_parts,columns,kv_heads,keys,shared", [
     (64, 0, 0, 256, 1, 32768, True), (64, 0, 0, 512, 8, 1024, False), (64, 0, 0, 80, 1, 6016, False), (64, 0, 0, 256, 32, 6016, True),
