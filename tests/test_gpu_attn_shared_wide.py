@@ -257,3 +257,43 @@ def test_shares_of_many_units(H, D, page, dtype, io, scale, window, sinks):
         at[1] = 512 * 32 - 5
         return torch.where(at < sinks, at, at - sinks + length - window) if window else at
     g.run(H, io, scale, pick, window, sinks, rows=range(0, n, 3))
+
+
+@pytest.mark.parametrize("D,dtype,io", [(128, "bf16", "bf16"), (100, "f16", "f32"), (64, "bf16", "f32"), (256, "bf16", "bf16")])
+def test_the_same_bits_in_every_replay_and_on_another_stream(D, dtype, io):
+    """A wide call captured into a graph and replayed over other contents, with eager calls and other work on its workspace between."""
+    print("case: wide graph", D, dtype, io, flush=True)
+    H, Hkv, members, prefix = 128, 2, 24, 9000
+    assert _goes_wide(members * H // Hkv, prefix, Hkv, D, dtype, io)
+    g = Keyed([(members, prefix, [50 + i for i in range(members)]), (3, 40, [5, 60, 7])], Hkv, D, 64, dtype, seed=D)
+    n, i32 = members + 3, dict(dtype=torch.int32, device=DEV)
+    first = torch.randn(n, H * D, generator=g.gen, device=DEV).to(M.DTYPES[io])
+    second = torch.randn(n, H * D, generator=g.gen, device=DEV).to(M.DTYPES[io])
+    start, prefixes, lens = torch.tensor(g.start, **i32), torch.tensor(g.prefix, **i32), torch.tensor(g.lens, **i32)
+    need = B.bitnet_attn_decode_shared_workspace_bytes(n, H, Hkv, D, 64, g.table.shape[1])
+    q, out, ws = first.clone(), torch.empty_like(first), torch.empty(need, dtype=torch.uint8, device=DEV)
+    call = lambda q, out, ws: B.bitnet_attn_decode_shared(q, start, prefixes, g.k_cache, g.v_cache, g.table, lens, out, 0.08, ws=ws)  # noqa: E731
+    want = {}
+    for name, x in (("first", first), ("second", second)):
+        want[name] = torch.empty_like(x)
+        call(x, want[name], torch.full_like(ws, 0xFF))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(q, out, ws)
+        assert torch.equal(out, want["first"])
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            call(q, out, ws)
+    torch.cuda.synchronize()
+    for turn in range(4):
+        name, x = (("second", second), ("first", first))[turn % 2]
+        q.copy_(x)
+        ws.fill_(0x7F + turn)
+        out.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[name]), turn
+        again = torch.empty_like(out)
+        call(x, again, torch.empty_like(ws))
+        assert torch.equal(again, want[name]), turn
