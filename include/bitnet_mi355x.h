@@ -341,7 +341,7 @@ typedef struct {
  *   TURNS   w f_i + (1 - w) f_i / factor, w = clamp((original f_i - low) / (high - low), 0, 1): pairs of few turns over the original
  *           context are stretched, those of many are not;
  *   INDEX   the same with w = 1 - clamp((i - lo) / (hi - lo), 0, 1): lo and hi are the indices at which a pair would make `high` and
- *           `low` turns, rounded down and up, and kept within 0 and rot_dim - 1.
+ *           `low` turns, rounded down and up, and kept within 0 and rot_dim - 1 (hi - lo counts as 0.001 at least).
  * theta > 1, factor > 0, original > 0, 0 < low < high.  freqs: device [rot_dim / 2], rot_dim even and up to 256.
  */
 typedef enum {
@@ -418,7 +418,9 @@ size_t bitnet_attn_decode_shared_workspace_bytes(int64_t n_seqs, int64_t n_heads
  *   0 <= n_groups <= n_seqs.  ws: bitnet_attn_decode_shared_workspace_bytes(...) bytes, any contents, nothing kept: 4 to 18 MB with
  *   heads of 64, 9 to 18 of 128, 17 to 35 of 256; 36, 70 and 137 more where a prefix could be long and of many columns (sequences times
  *   query heads of a kv head); and twice the size of out in 32 bits, of 1024 sequences at most.
- *   All else (types, precision, what is visible, what is not finite, one result for one call) as bitnet_attn_decode.
+ *   All else (types, precision, what is visible, what is not finite, one result for one call) as bitnet_attn_decode, which may be called
+ *   over the same tables where the members' rows name the prefix's pages too, and is faster with few or short prefixes: with 8 kv heads of
+ *   128, behind 1024 shared keys (2 to 64 sequences); 16 behind 2048, 8 behind 4096 and 2 behind 16384 take the same either way, more less here.
  */
 bitnet_status bitnet_attn_decode_shared(const bitnet_kv_cache* cache, const void* q, int dtype, int64_t n_heads,
                                         const int32_t* group_start, const int32_t* prefix_len, int64_t n_groups, float scale,

@@ -6,9 +6,10 @@
 // group takes an equal share of its tiles.  Results go to records, as those of the other rows.  Weights go in two parts at least, as in the
 // other rows (rounded once, they were 2^-9 off in bf16, for the sequences with enough neighbours only; the call took 131 us then).
 //
-// Measured: 64 sequences of 4 query heads a kv head behind 65536 keys, bf16 throughout, 153 us the whole call; in registers (32 columns a
-// pass) 475.  Before the second part the kernel took 99 to 104, with one tile of keys on its way 109, with 128 columns a pass 113; the
-// matrix cores were busy 33% of the time, a wave waited 51% of its own: each work group reads keys that no other is about to.
+// Measured: 64 sequences of 4 query heads a kv head behind 65536 keys, bf16 throughout, 130 us (68.7 GFLOP, 529 TFLOP/s, 793 in its parts),
+// the whole call 154; in registers (32 columns a pass) 475.  The matrix cores are busy 40% of the time, a wave waits 49% of its own: each
+// work group reads keys that no other is about to.  With weights in one part it took 99 to 104, with one tile of keys on its way 109 then,
+// with 128 columns a pass 113.
 #include "attn_prefill.hpp"
 #include "attn_shared.hpp"
 

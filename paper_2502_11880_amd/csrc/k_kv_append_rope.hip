@@ -6,8 +6,9 @@
 // turn_of), shared through LDS, and used by all heads that it takes.
 //
 // Measured (kernel times): five prompts of up to 3001 tokens, 32 heads of 8 kv heads of 128, 32 bits into bf16, 79 us (381 MB, 4.8
-// TB/s; a large copy reaches 5.0); one token each of 64 sequences 6.3; nine chunks of up to 509 tokens, 32 heads of 100, f16, pages
-// of 16, 22 us where the pages are in the last cache, 30 a pass where they are not (3.1 TB/s).
+// TB/s; a large copy reaches 5.0); one token each of 64 sequences 6.3; nine chunks of up to 509 tokens, 32 heads of 100, f16, 22 us
+// where the pages are in the last cache, 30 to 31 a pass where they are not (3.1 TB/s), in pages of 16 as of 256; from 32 bits 40 (3.8
+// TB/s): values of 16-bit rows are read two bytes a lane.
 #include "rows.hpp"
 
 namespace bitnet {

@@ -8,13 +8,17 @@
 // value each, as those of the quantiser have; and squares of any 32-bit value fit it.  64-bit operations are as cheap as loads
 // here: two an element, where the memory gives a CU less than one element a clock.
 //
-// Memory bounds it: a row is read once into registers (up to 16 quads a thread), summed, normed and quantised there, and
-// written once; 13 bytes an element with everything in 32 bits.  Two reductions over the work group stand in between.
-// Rows that are longer, which no linear of a model has, take three passes over memory.
+// Memory bounds it: a row is read once into registers (up to 8 quads a thread; rows past 16384 values 16, of which 1024 lanes spill 20 to
+// 102 registers to scratch memory), summed, normed and quantised there, and written once; 13 bytes an element with everything in 32
+// bits.  Two reductions over the work group stand in between.  Rows past 65536, which no linear of a model has, take three passes over
+// memory.
 //
 // Measured (kernel times): 8192 rows of 4096, all in 32 bits, 76.8 us (5.7 TB/s; a large copy reaches 4.9, and here more is read
 // than written) with 256 lanes a row, 512 the same, 128 79, 64 81, 1024 84; 333 rows of 8640, 32 bits onto a residual in bf16, 7.6 us
 // with 512 lanes of five quads, 8.3 of eight, 9.1 with 1024 lanes; one row of 4096 3.3 us, of which an empty launch takes 1.7.
+// Calls, all in 32 bits: 1000 rows of 20000 89 us (2.9 TB/s; three passes 97), 512 of 65536 112 (166), 256 of 100000 201; widths that are no
+// multiple of four, by single values: 4096 rows of 4099 47 us (4.7 TB/s), 333 of 8641 11, 512 of 65535 132 (three passes 166), but 1000 of
+// 20001 114 (97).
 #include "rows.hpp"
 
 namespace bitnet {
